@@ -17,7 +17,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 _SO = os.path.join(_HERE, "libblendstep.so")
-_HEADERS = [os.path.join(_ROOT, "include", "blendstep.h"), os.path.join(_ROOT, "include", "blendstep_builder.h")]
+_HEADERS = [os.path.join(_ROOT, "include", h) for h in ("blendstep.h", "blendstep_builder.h", "blendstep_stream.h")]
 
 _i32p = C.POINTER(C.c_int32)
 
@@ -52,6 +52,10 @@ class OverlapKnobs(C.Structure):
 class Division(C.Structure):
     _fields_ = [("items", C.c_int32), ("wide_items", C.c_int32), ("longest_item_tokens", C.c_int32 * 2), ("prefill_rows", C.c_int32),
                 ("states", C.c_int64), ("descriptor_words", C.c_int64)]
+
+
+class WindowParts(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("units", "longest_pages", "split_rows", "wide_blocks", "wide_cut")] + [("pages", C.c_int64)]
 
 
 class SplitInfo(C.Structure):
@@ -170,6 +174,33 @@ def raw():
         lib.bs_sched_last_error.restype = C.c_char_p
         lib.bs_sched_next.argtypes = [C.c_void_p, C.POINTER(C.POINTER(BatchOwned))]
         lib.bs_sched_get_stats.argtypes = [C.c_void_p, C.POINTER(SchedStats)]
+        _i64, _i32, _p = C.c_int64, C.c_int32, C.c_void_p
+        lib.bs_window_create.argtypes = [_p, C.POINTER(_p)]
+        lib.bs_window_destroy.argtypes = [_p]
+        lib.bs_window_destroy.restype = None
+        lib.bs_window_plan.argtypes = [_p, C.POINTER(BatchDesc), _i64, _i32, _i32, _i32, _i32p, _i32p, _p]
+        lib.bs_rope_append.argtypes = [_p, _p, _i64, _p, _i64, _p, _p]
+        lib.bs_window_attention.argtypes = [_p, _p, _i64, _p, _i64, _p, _p]
+        lib.bs_window_division.argtypes = [_p, C.POINTER(WindowParts)]
+        lib.bs_w4_bytes.argtypes = [_i64, _i64, _i32, _i32]
+        lib.bs_w4_bytes.restype = _i64
+        lib.bs_w4_pack.argtypes = [_p, _p, _p, _p, _i64, _i64, _i32, _p, _p]
+        lib.bs_w4_linear.argtypes = [_p, _p, _i64, _p, _i64, _i64, _i64, _i32, _i32, _p, _i64, _p]
+        lib.bs_pages_create.argtypes = [_i32, C.POINTER(_p)]
+        lib.bs_pages_destroy.argtypes = [_p]
+        lib.bs_pages_destroy.restype = None
+        lib.bs_pages_last_error.argtypes = [_p]
+        lib.bs_pages_last_error.restype = C.c_char_p
+        lib.bs_pages_open.argtypes = [_p, _i32, _i32p]
+        lib.bs_pages_fork.argtypes = [_p, _i32p, _i32, _i32, _i32p]
+        lib.bs_pages_extend.argtypes = [_p, _i32p, _i32p, _i32, _i32p, _i32p, _i32p]
+        lib.bs_pages_trim.argtypes = [_p, _i32p, _i32, _i32, _i32]
+        lib.bs_pages_free.argtypes = [_p, _i32p, _i32]
+        lib.bs_pages_compact.argtypes = [_p, _i32p, _i32p, _i32p, _i32p]
+        lib.bs_pages_tables.argtypes = [_p, _i32p, _i32, _i32p, _i32p, _i32p]
+        lib.bs_pages_stats.argtypes = [_p, _i32p, _i32p]
+        lib.bs_kv_copy_pages.argtypes = [_p, C.POINTER(_p), _i32, _i64, _i32p, _i32p, _i32, _p]
+        lib.bs_kv_compact.argtypes = [_p, C.POINTER(_p), _i32, _i64, _i32p, _i64, _i32p, _i32p, _p]
         lib.bs_batch_free.argtypes = [C.POINTER(BatchOwned)]
         lib.bs_batch_free.restype = None
         _lib = lib
@@ -424,6 +455,251 @@ class Layer:
         return out
 
 
+    # -- streams (blendstep_stream.h) ---------------------------------------------------
+    def window_plan(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages: Optional[int] = None, stream=None):
+        """The plan of a step for window_attention and rope_append (bs_window_plan): one for all layers with this window.
+        positions [n_axes, n_rows] and axis_of_pair [head_dim / 2]: rotary positions with several axes."""
+        return WindowPlan(self, batch, window, sinks, positions, axis_of_pair, n_pages, stream)
+
+    def window_attention(self, plan: "WindowPlan", q, kv_pool, out=None, stream=None):
+        """Sliding-window attention with sinks of the plan's rows; q and out: [n_rows, Hq * dh] bf16, rows at any stride."""
+        if out is None:
+            out = self.torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        self._check_rows(plan, (q, out))
+        self._check_pool(plan, kv_pool)
+        self._check(self.lib.bs_window_attention(plan.h, q.data_ptr(), q.stride(0), out.data_ptr(), out.stride(0), kv_pool.data_ptr(),
+                                                 self._raw_stream(stream)))
+        return out
+
+    def rope_append(self, plan: "WindowPlan", qkv, kv_pool, q=None, stream=None):
+        """Turns queries and keys of fused rows [n_rows, (Hq + 2 Hkv) * dh] and appends keys and values to kv_pool; the
+        turned queries [n_rows, Hq * dh] (q: where they go; qkv[:, :Hq * dh] for in place)."""
+        width = self.shape.n_q_heads * self.shape.head_dim
+        if q is None:
+            q = self.torch.empty((plan.n_rows, width), dtype=qkv.dtype, device=qkv.device)
+        self._check_rows(plan, (q,))
+        self._check_rows(plan, (qkv,), width + 2 * self.shape.n_kv_heads * self.shape.head_dim)
+        self._check_pool(plan, kv_pool)
+        self._check(self.lib.bs_rope_append(plan.h, qkv.data_ptr(), qkv.stride(0), q.data_ptr(), q.stride(0), kv_pool.data_ptr(),
+                                            self._raw_stream(stream)))
+        return q
+
+    def _raw_stream(self, stream):
+        return (stream if stream is not None else self.torch.cuda.current_stream(self.device)).cuda_stream
+
+    def _check_rows(self, plan, tensors, width=None):
+        width = width if width is not None else self.shape.n_q_heads * self.shape.head_dim
+        for t in tensors:
+            if t.dtype != self.torch.bfloat16 or t.dim() != 2 or t.shape[0] != plan.n_rows or t.shape[1] != width or t.stride(1) != 1:
+                raise ValueError("expected bf16 rows [%d, %d], got %s %s" % (plan.n_rows, width, t.dtype, tuple(t.shape)))
+
+    def _check_pool(self, plan, kv_pool):
+        if kv_pool.dtype != self.torch.bfloat16 or not kv_pool.is_contiguous() or kv_pool.numel() * 2 < plan.n_pages * self.page_bytes():
+            raise ValueError("the pool is smaller than the %d pages of the plan, or not contiguous bf16" % plan.n_pages)
+
+    def w4_pack(self, packed, scales, zeros=None, stream=None):
+        """Lays 4-bit weights out for w4_linear (bs_w4_pack).  packed: uint8 [n, k / 2], the even input in the low four bits;
+        scales: bf16 [n, k / group]; zeros: uint8 [n, k / group] or None (8 everywhere)."""
+        torch = self.torch
+        n, k = packed.shape[0], packed.shape[1] * 2
+        groups = scales.shape[1]
+        group = k // groups if groups else 128
+        if not packed.is_contiguous() or not scales.is_contiguous() or (zeros is not None and not zeros.is_contiguous()):
+            raise ValueError("w4_pack: contiguous tensors")
+        if packed.dtype != torch.uint8 or scales.dtype != torch.bfloat16 or tuple(scales.shape) != (n, k // group if group else 0) or \
+                (zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != scales.shape)):
+            raise ValueError("w4_pack: uint8 [n, k / 2], bf16 scales and uint8 zeros [n, k / group]")
+        size = int(self.lib.bs_w4_bytes(n, k, group, int(zeros is not None)))
+        data = torch.empty(max(16, size), dtype=torch.uint8, device=packed.device)
+        self._check(self.lib.bs_w4_pack(self.h, packed.data_ptr(), scales.data_ptr(), zeros.data_ptr() if zeros is not None else None, n, k,
+                                        group, data.data_ptr(), self._raw_stream(stream)))
+        return W4Weight(data, n, k, group, zeros is not None)
+
+    def w4_linear(self, x, weight: "W4Weight", out=None, stream=None):
+        """x [m, k] bf16 times a laid-out 4-bit weight: [m, n] bf16."""
+        if x.dtype != self.torch.bfloat16 or x.dim() != 2 or x.shape[1] != weight.k or (x.stride(1) != 1 and x.numel()):
+            raise ValueError("w4_linear: bf16 rows of %d inputs, got %s %s" % (weight.k, x.dtype, tuple(x.shape)))
+        m = x.shape[0]
+        if out is None:
+            out = self.torch.empty((m, weight.n), dtype=x.dtype, device=x.device)
+        elif out.dtype != x.dtype or tuple(out.shape) != (m, weight.n) or out.stride(1) != 1:
+            raise ValueError("w4_linear: out is not bf16 [%d, %d]" % (m, weight.n))
+        self._check(self.lib.bs_w4_linear(self.h, x.data_ptr(), x.stride(0) if x.numel() else 0, weight.data.data_ptr(), m, weight.n, weight.k, weight.group,
+                                          weight.with_zeros, out.data_ptr(), out.stride(0), self._raw_stream(stream)))
+        return out
+
+    def _pools(self, pools):
+        """(addresses, how many, pages of each) of a tensor [n_pools, elements] or a list of flat pools."""
+        pools = [pools[i] for i in range(pools.shape[0])] if hasattr(pools, "shape") else list(pools)
+        size = self.page_bytes() // 2
+        for p in pools:
+            if p.dtype != self.torch.bfloat16 or not p.is_contiguous() or p.numel() != pools[0].numel() or p.numel() % size:
+                raise ValueError("pools are contiguous bf16 tensors of one size, whole pages each")
+        return (C.c_void_p * len(pools))(*[p.data_ptr() for p in pools]), len(pools), pools[0].numel() // size if pools else 0
+
+    def copy_pages(self, pools, src, dst, stream=None):
+        """Page src[i] to page dst[i] in every pool (one per layer: a list, or a tensor [n_layers, elements])."""
+        at, n, n_pages = self._pools(pools)
+        src, dst = _i32(src), _i32(dst)
+        if src.shape != dst.shape:
+            raise ValueError("copy_pages: %d sources, %d destinations" % (src.size, dst.size))
+        self._check(self.lib.bs_kv_copy_pages(self.h, at, n, n_pages, _ptr(src), _ptr(dst), src.size, self._raw_stream(stream)))
+
+    def compact_pages(self, pools, tables, stream=None):
+        """Moves the pages that `tables` names to the front of every pool: (the tables with the new numbers, pages named)."""
+        at, n, n_pages = self._pools(pools)
+        tables = _i32(tables)
+        out, live = np.empty_like(tables), C.c_int32()
+        self._check(self.lib.bs_kv_compact(self.h, at, n, n_pages, _ptr(tables), tables.size, _ptr(out), C.byref(live), self._raw_stream(stream)))
+        return out, live.value
+
+
+def _i32(a) -> np.ndarray:
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+@dataclass
+class W4Weight:
+    """A laid-out 4-bit weight [n, k] (Layer.w4_pack)."""
+    data: "object"
+    n: int
+    k: int
+    group: int
+    with_zeros: bool
+
+
+class WindowPlan:
+    """The plan of one step (bs_window): made once, used by every layer with its window and sinks."""
+
+    def __init__(self, layer: Layer, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages=None, stream=None):
+        self.layer = layer
+        self.n_rows = self.n_pages = 0
+        h = C.c_void_p()
+        layer._check(layer.lib.bs_window_create(layer.h, C.byref(h)))
+        self.h = h
+        self.update(batch, window, sinks, positions, axis_of_pair, n_pages, stream)
+
+    def update(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages=None, stream=None):
+        """Plans another step on the same buffers."""
+        lay = self.layer
+        d, keep = marshal_batch(batch)
+        axes, pos, axis = 0, None, None
+        if positions is not None or axis_of_pair is not None:
+            if positions is None or axis_of_pair is None:
+                raise ValueError("positions and axis_of_pair come together")
+            pos, axis = np.atleast_2d(_i32(positions)), _i32(axis_of_pair)
+            axes = pos.shape[0]
+            if pos.shape[1] != batch.n_rows or axis.size != lay.shape.head_dim // 2:
+                raise ValueError("positions [n_axes, %d] and axis_of_pair [%d]" % (batch.n_rows, lay.shape.head_dim // 2))
+        pages = batch.n_pages if n_pages is None else n_pages
+        where = lay._raw_stream(stream) if lay.device >= 0 else None
+        lay._check(lay.lib.bs_window_plan(self.h, C.byref(d), pages, window, sinks, axes, None if pos is None else _ptr(pos),
+                                          None if axis is None else _ptr(axis), where))
+        self.n_rows, self.n_pages = batch.n_rows, pages
+        return self
+
+    def division(self) -> WindowParts:
+        out = WindowParts()
+        self.layer._check(self.layer.lib.bs_window_division(self.h, C.byref(out)))
+        return out
+
+    def close(self):
+        if getattr(self, "h", None):
+            self.layer.lib.bs_window_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Pages:
+    """Book-keeping of a cache's pages (bs_pages_*): tables, forks, growth, what falls behind a window, compaction."""
+
+    def __init__(self, n_pages: int):
+        self.lib = raw()
+        self.n_pages = int(n_pages)
+        h = C.c_void_p()
+        rc = self.lib.bs_pages_create(self.n_pages, C.byref(h))
+        if rc != 0:
+            raise BlendStepError(rc, (self.lib.bs_pages_last_error(None) or b"").decode())
+        self.h = h
+
+    def close(self):
+        if getattr(self, "h", None):
+            self.lib.bs_pages_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, rc):
+        if rc != 0:
+            raise BlendStepError(rc, (self.lib.bs_pages_last_error(self.h) or b"").decode())
+
+    def open(self, n: int = 1) -> np.ndarray:
+        """Ids of n new, empty sequences."""
+        ids = np.zeros(max(1, n), dtype=np.int32)
+        self._check(self.lib.bs_pages_open(self.h, n, _ptr(ids)))
+        return ids[:n]
+
+    def fork(self, parents, children: int = 1) -> np.ndarray:
+        """Ids of `children` new sequences for each parent, which share its pages."""
+        parents = _i32(parents).reshape(-1)
+        out = np.zeros(max(1, parents.size * max(0, children)), dtype=np.int32)
+        self._check(self.lib.bs_pages_fork(self.h, _ptr(parents), parents.size, children, _ptr(out)))
+        return out[:parents.size * children]
+
+    def extend(self, ids, tokens):
+        """Room for further tokens; (src, dst) of the pages to copy in every pool before they are written to."""
+        ids = _i32(ids).reshape(-1)
+        tokens = np.ascontiguousarray(np.broadcast_to(_i32(tokens), ids.shape))
+        src, dst, n = np.zeros(max(1, ids.size), dtype=np.int32), np.zeros(max(1, ids.size), dtype=np.int32), C.c_int32()
+        self._check(self.lib.bs_pages_extend(self.h, _ptr(ids), _ptr(tokens), ids.size, _ptr(src), _ptr(dst), C.byref(n)))
+        return src[:n.value], dst[:n.value]
+
+    def trim(self, ids, window: int, sinks: int = 0):
+        ids = _i32(ids).reshape(-1)
+        self._check(self.lib.bs_pages_trim(self.h, _ptr(ids), ids.size, window, sinks))
+
+    def free(self, ids):
+        ids = _i32(ids).reshape(-1)
+        self._check(self.lib.bs_pages_free(self.h, _ptr(ids), ids.size))
+
+    def compact(self):
+        """(src, dst) of the moves, and the number of live pages."""
+        src, dst = np.zeros(max(1, self.n_pages), dtype=np.int32), np.zeros(max(1, self.n_pages), dtype=np.int32)
+        moves, live = C.c_int32(), C.c_int32()
+        self._check(self.lib.bs_pages_compact(self.h, _ptr(src), _ptr(dst), C.byref(moves), C.byref(live)))
+        return src[:moves.value], dst[:moves.value], live.value
+
+    def lengths(self, ids) -> np.ndarray:
+        return self._tables(ids, False)[0]
+
+    def tables(self, ids):
+        """(page_start, page_ids) of the sequences, as a batch holds them."""
+        return self._tables(ids, True)[1:]
+
+    def _tables(self, ids, whole):
+        ids = _i32(ids).reshape(-1)
+        tokens, start = np.zeros(max(1, ids.size), dtype=np.int32), np.zeros(ids.size + 1, dtype=np.int32)
+        self._check(self.lib.bs_pages_tables(self.h, _ptr(ids), ids.size, _ptr(tokens), _ptr(start), None))
+        pages = np.zeros(max(1, int(start[-1])), dtype=np.int32)
+        if whole:
+            self._check(self.lib.bs_pages_tables(self.h, _ptr(ids), ids.size, _ptr(tokens), _ptr(start), _ptr(pages)))
+        return tokens[:ids.size], start, pages[:int(start[-1])]
+
+    def stats(self) -> dict:
+        free, live = C.c_int32(), C.c_int32()
+        self._check(self.lib.bs_pages_stats(self.h, C.byref(free), C.byref(live)))
+        return {"free": free.value, "sequences": live.value}
+
+
 class Builder:
     """Host-side batch builder (prefix tree, layer-wise sort, dual scan)."""
 
@@ -573,6 +849,9 @@ class _Api:
     Layer = Layer
     Builder = Builder
     Scheduler = Scheduler
+    Pages = Pages
+    WindowPlan = WindowPlan
+    W4Weight = W4Weight
     binding_device_state = DeviceState
     BlendStepError = BlendStepError
     FLAG_SERIAL = FLAG_SERIAL

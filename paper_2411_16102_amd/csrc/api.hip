@@ -17,6 +17,7 @@
 
 #include "../../include/blendstep.h"
 #include "attn.hpp"
+#include "context.hpp"
 #include "gemm.hpp"
 #include "misc.hpp"
 #include "room.hpp"
@@ -41,26 +42,6 @@ std::mutex g_scratch_mutex;
 
 constexpr long STAGE_HALF = 2 * BS_NOALLOC_BLOB_BYTES / 4;  // 32-bit words of either half of the staging buffer, at first
 constexpr long STAGE_RING = 5 * BS_NOALLOC_BLOB_BYTES / 4;  // and of the ring for captured calls: bs_attention_noalloc never has to grow it
-
-struct HipRuntime {  // what Staging asks of the runtime
-  typedef hipStream_t Stream;
-  typedef hipEvent_t Event;
-  int create(Event *e) { return hipEventCreateWithFlags(e, hipEventDisableTiming); }
-  int destroy(Event e) { return hipEventDestroy(e); }
-  int alloc(int32_t **p, long words) {
-    return hipHostMalloc(reinterpret_cast<void **>(p), (size_t)words * sizeof(int32_t), hipHostMallocDefault);
-  }
-  int release(int32_t *p) { return hipHostFree(p); }
-  int record(Event e, Stream s) { return hipEventRecord(e, s); }
-  int wait(Event e) { return hipEventSynchronize(e); }
-  int wait_all() { return hipDeviceSynchronize(); }
-  int capturing(Stream s, bool *yes) {
-    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    const hipError_t e = hipStreamIsCapturing(s, &status);
-    *yes = status == hipStreamCaptureStatusActive;
-    return e;
-  }
-};
 
 constexpr long TRACE_CAP = 8192;  // workgroups per launch that a timeline can hold
 std::string g_create_error;
@@ -1279,6 +1260,31 @@ int check_cfg(const bs_layer_cfg *g) {
 }
 
 }  // namespace
+
+// ---------------------------------------------------------------------------------
+// what the entry points of other files use of a context
+// ---------------------------------------------------------------------------------
+namespace bs {
+
+CtxView ctx_view(const bs_ctx *c) {
+  return {&c->cfg, c->device, c->rope_cos, c->rope_sin, c->sk_ws, c->sk_cnt, gemm_sk_workspace_floats(), (int)gemm_sk_counters(), c->n_cu};
+}
+
+int ctx_fail(bs_ctx *c, int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(c, code, "%s", buf);
+}
+
+int ctx_stage(bs_ctx *c, long words, hipStream_t stream, int32_t **out) {
+  const int e = c->stage.place(whole_units(words), stream, out);
+  return e ? staging_failed(c, e) : BS_OK;
+}
+
+}  // namespace bs
 
 extern "C" {
 

@@ -1,0 +1,387 @@
+// Entry points of the window operators: validation, the plan of a step, and the launches that work from it.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+#include "../../include/blendstep_stream.h"
+#include "context.hpp"
+#include "misc.hpp"
+#include "window.hpp"
+
+using namespace bs;
+
+namespace {
+
+constexpr int PAGE = 16;
+constexpr int MOST_UNIT_PAGES = 64;     // a lane of a wavefront holds one page of its unit
+constexpr int MAX_AXES = 8;
+constexpr int32_t MAX_LEN = 1 << 30;    // of lengths and rows, so that sums of two stay in 32 bits
+constexpr long STAGE_WORDS = 1 << 16;   // of the plan's pinned memory at first (it grows with the plans)
+
+// What the kernels of a planned step need to know beside the arrays on the device.
+struct Planned {
+  bool made = false, has_angles = false;
+  int n_rows = 0, n_items = 0, n_joins = 0, window = 1;
+  int32_t longest = 0, split_rows = 0;
+  int64_t n_pool_pages = 0;
+  long states = 0, pages = 0;
+  long off_items = 0, off_pages = 0, off_joins = 0, off_row_page = 0, off_row_slot = 0, off_positions = 0, off_axis = 0, words = 0;
+};
+
+}  // namespace
+
+struct bs_window {
+  bs_ctx *ctx = nullptr;
+  Planned p;
+  Staging<HipRuntime> stage;
+  int32_t *d_words = nullptr;
+  long cap_words = 0;
+  float *d_states = nullptr;
+  long cap_states = 0;
+  // host scratch reused across plans
+  std::vector<int32_t> words, refs, item_pages, joins;
+  std::vector<WindowItem> items;
+};
+
+namespace {
+
+int check_batch(bs_ctx *c, const bs_batch *b, int64_t n_pages) {
+  if (!b) return ctx_fail(c, BS_EINVAL, "batch is NULL");
+  if (b->n_seq < 0 || b->n_rows < 0 || b->n_rows > MAX_LEN) return ctx_fail(c, BS_EINVAL, "bad counts: n_seq=%d n_rows=%d", b->n_seq, b->n_rows);
+  if (n_pages < 0 || n_pages > (int64_t)0x7fffffff) return ctx_fail(c, BS_EINVAL, "n_pages=%lld out of range", (long long)n_pages);
+  if (b->n_seq == 0) return b->n_rows == 0 ? BS_OK : ctx_fail(c, BS_EINVAL, "n_rows=%d with no sequences", b->n_rows);
+  if (!b->row_start || !b->kv_len || !b->page_start) return ctx_fail(c, BS_EINVAL, "a required array is NULL");
+  if (b->row_start[0] != 0 || b->page_start[0] != 0) return ctx_fail(c, BS_EINVAL, "CSR arrays must start at 0");
+  for (int s = 0; s < b->n_seq; ++s) {
+    const int64_t rows = (int64_t)b->row_start[s + 1] - b->row_start[s], pages = (int64_t)b->page_start[s + 1] - b->page_start[s];
+    if (rows < 0 || b->row_start[s + 1] > b->n_rows) return ctx_fail(c, BS_EINVAL, "row_start not monotone within n_rows at sequence %d", s);
+    if (pages < 0) return ctx_fail(c, BS_EINVAL, "page_start not monotone at sequence %d", s);
+    if (b->kv_len[s] < 0 || b->kv_len[s] > MAX_LEN) return ctx_fail(c, BS_EINVAL, "sequence %d: kv_len %d out of range", s, b->kv_len[s]);
+    if (pages * PAGE < b->kv_len[s]) return ctx_fail(c, BS_EINVAL, "sequence %d: kv_len %d exceeds its %lld pages", s, b->kv_len[s], (long long)pages);
+  }
+  if (b->row_start[b->n_seq] != b->n_rows) return ctx_fail(c, BS_EINVAL, "row_start ends at %d, n_rows is %d", b->row_start[b->n_seq], b->n_rows);
+  if (b->page_start[b->n_seq] > 0 && !b->page_ids) return ctx_fail(c, BS_EINVAL, "a required array is NULL");
+  for (int i = 0; i < b->page_start[b->n_seq]; ++i)
+    if (b->page_ids[i] != BS_PAGE_NONE && (b->page_ids[i] < 0 || b->page_ids[i] >= n_pages))
+      return ctx_fail(c, BS_EINVAL, "page_ids[%d]=%d outside the pool of %lld pages", i, b->page_ids[i], (long long)n_pages);
+  return BS_OK;
+}
+
+// pages that a step appends to are there, and named once
+int check_appends(bs_window *w, const bs_batch *b, int64_t n_pages) {
+  w->refs.assign((size_t)n_pages, 0);
+  for (int i = 0; b->n_seq > 0 && i < b->page_start[b->n_seq]; ++i)
+    if (b->page_ids[i] >= 0) ++w->refs[b->page_ids[i]];
+  for (int s = 0; s < b->n_seq; ++s) {
+    const int rows = b->row_start[s + 1] - b->row_start[s];
+    if (rows == 0 || b->kv_len[s] == 0) continue;
+    for (int pg = std::max(0, b->kv_len[s] - rows) / PAGE; pg <= (b->kv_len[s] - 1) / PAGE; ++pg) {
+      const int id = b->page_ids[b->page_start[s] + pg];
+      if (id < 0) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d appends to page %d of its table, which was given up", s, pg);
+      if (w->refs[id] != 1) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d appends into page %d, which is referenced more than once", s, id);
+    }
+  }
+  return BS_OK;
+}
+
+// The pages that rows at positions [p0, p1] see: the first n_sink, then [first, last].
+struct Seen {
+  int n_sink, first, last;
+  int pages() const { return n_sink + last - first + 1; }
+  int left_out() const { return PAGE * (first - n_sink); }  // tokens between the two parts
+};
+Seen seen_by(int p0, int p1, int window, int sinks) {
+  if (p1 < 0) return {0, 0, -1};
+  const int first = std::max(0, p0 - window + 1) / PAGE;
+  return {std::min((int)(((int64_t)sinks + PAGE - 1) / PAGE), first), first, p1 / PAGE};
+}
+
+// Cuts the rows of every sequence into units; chunk: pages of a unit.
+int plan_units(bs_window *w, const bs_batch *b, int window, int sinks, int rows_per_unit, int chunk) {
+  Planned &p = w->p;
+  w->items.clear();
+  w->item_pages.clear();
+  w->joins.clear();
+  for (int s = 0; s < b->n_seq; ++s) {
+    const int r0 = b->row_start[s], rows = b->row_start[s + 1] - r0;
+    const int32_t *table = b->page_ids + b->page_start[s];
+    for (int j = 0; j < rows; j += rows_per_unit) {
+      const int n = std::min(rows_per_unit, rows - j), p0 = b->kv_len[s] - rows + j, p1 = p0 + n - 1;
+      const Seen seen = seen_by(p0, p1, window, sinks);
+      const int n_pages = seen.pages(), n_chunks = std::max(1, (n_pages + chunk - 1) / chunk);
+      for (int i = 0; i < n_pages; ++i) {
+        const int pg = i < seen.n_sink ? i : seen.first + i - seen.n_sink;
+        if (table[pg] < 0) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d: a row sees page %d of its table, which was given up", s, pg);
+      }
+      for (int k = 0; k < n_chunks; ++k) {
+        // chunks of nearly equal lengths
+        const int lo = (int)((int64_t)n_pages * k / n_chunks), hi = (int)((int64_t)n_pages * (k + 1) / n_chunks);
+        WindowItem it{};
+        it.row0 = r0 + j;
+        it.n_rows = n;
+        it.page_off = (int32_t)w->item_pages.size();
+        it.n_pages = hi - lo;
+        it.at = p0 - seen.left_out() - PAGE * lo;
+        it.sinks = std::max(0, std::min(sinks - PAGE * lo, PAGE * (hi - lo)));
+        it.state = n_chunks > 1 ? (int32_t)(p.states + (long)k * n) : -1;
+        w->items.push_back(it);
+        for (int i = lo; i < hi; ++i) w->item_pages.push_back(table[i < seen.n_sink ? i : seen.first + i - seen.n_sink]);
+        p.longest = std::max(p.longest, it.n_pages);
+      }
+      if (n_chunks > 1) {
+        for (int i = 0; i < n; ++i) w->joins.insert(w->joins.end(), {r0 + j + i, (int32_t)(p.states + i), n, n_chunks});
+        p.states += (long)n_chunks * n;
+        p.split_rows += n;
+      }
+      if (p.states > MAX_LEN || w->item_pages.size() > (size_t)MAX_LEN) return ctx_fail(w->ctx, BS_EUNSUPPORTED, "the step is too large for one plan");
+    }
+  }
+  p.n_items = (int)w->items.size();
+  p.n_joins = (int)w->joins.size() / 4;
+  p.pages = (long)w->item_pages.size();
+  return BS_OK;
+}
+
+template <class T>
+int grow(bs_ctx *c, T **at, long *cap, long want, size_t each) {
+  if (want <= *cap) return BS_OK;
+  const long room = want + want / 4 + 1024;
+  if (*at) CTX_HIP_TRY(c, hipFree(*at));
+  *at = nullptr;
+  *cap = 0;
+  const hipError_t e = hipMalloc(reinterpret_cast<void **>(at), (size_t)room * each);
+  if (e != hipSuccess) {
+    *at = nullptr;
+    return ctx_fail(c, BS_ENOMEM, "hipMalloc of %zu bytes: %s", (size_t)room * each, hipGetErrorString(e));
+  }
+  *cap = room;
+  return BS_OK;
+}
+
+int stream_is_capturing(bs_ctx *c, hipStream_t st, bool *yes) {
+  if (const int e = HipRuntime().capturing(st, yes)) return ctx_fail(c, BS_EHIP, "hipStreamIsCapturing: %s", hipGetErrorString((hipError_t)e));
+  return BS_OK;
+}
+
+AttnShape shape_of(const bs_layer_cfg &g) {
+  AttnShape s;
+  s.n_q_heads = g.n_q_heads; s.n_kv_heads = g.n_kv_heads; s.head_dim = g.head_dim; s.page_size = g.page_size;
+  s.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)g.head_dim));
+  return s;
+}
+
+bool aligned(const void *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
+
+// the checks that every call on a plan makes first
+int check_call(bs_window *w, const char *what) {
+  if (ctx_view(w->ctx).device == BS_DEVICE_NONE) return ctx_fail(w->ctx, BS_EINVAL, "host-only context");
+  if (!w->p.made) return ctx_fail(w->ctx, BS_EINVAL, "%s: nothing is planned", what);
+  return BS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int bs_window_create(bs_ctx *c, bs_window **out) {
+  if (out) *out = nullptr;
+  if (!c) return BS_EINVAL;
+  return ctx_guarded(c, [&]() -> int {
+    if (!out) return ctx_fail(c, BS_EINVAL, "out is NULL");
+    bs_window *w = new bs_window();
+    w->ctx = c;
+    const CtxView v = ctx_view(c);
+    if (v.device != BS_DEVICE_NONE) {
+      hipError_t e = hipSetDevice(v.device);
+      if (e == hipSuccess) e = (hipError_t)w->stage.open(STAGE_WORDS, 16);
+      if (e != hipSuccess) {
+        w->stage.close();
+        delete w;
+        return ctx_fail(c, e == hipErrorOutOfMemory ? BS_ENOMEM : BS_EHIP, "pinned memory of a plan: %s", hipGetErrorString(e));
+      }
+    }
+    *out = w;
+    return BS_OK;
+  });
+}
+
+void bs_window_destroy(bs_window *w) {
+  if (!w) return;
+  const int device = ctx_view(w->ctx).device;
+  if (device != BS_DEVICE_NONE) {
+    (void)hipSetDevice(device);
+    (void)hipDeviceSynchronize();
+    if (w->d_words) (void)hipFree(w->d_words);
+    if (w->d_states) (void)hipFree(w->d_states);
+    w->stage.close();
+  }
+  delete w;
+}
+
+int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t window, int32_t sinks, int32_t n_axes,
+                   const int32_t *positions, const int32_t *axis_of_pair, void *stream) {
+  if (!w) return BS_EINVAL;
+  bs_ctx *c = w->ctx;
+  return ctx_guarded(c, [&]() -> int {
+    const CtxView v = ctx_view(c);
+    const bs_layer_cfg &g = *v.cfg;
+    const hipStream_t st = (hipStream_t)stream;
+    w->p = Planned();
+    if (window < 1 || sinks < 0) return ctx_fail(c, BS_EINVAL, "window %d must be at least 1 and sinks %d at least 0", window, sinks);
+    if (n_axes < 0 || n_axes > MAX_AXES || (n_axes > 0) != (positions != nullptr) || (n_axes > 0) != (axis_of_pair != nullptr))
+      return ctx_fail(c, BS_EINVAL, "n_axes %d: 1 to %d with positions and axis_of_pair, or 0 without", n_axes, MAX_AXES);
+    if (const int rc = check_batch(c, b, n_pages)) return rc;
+    if (const int rc = check_appends(w, b, n_pages)) return rc;
+    const int half = g.head_dim / 2, rows = b->n_rows;
+    for (int i = 0; n_axes > 0 && i < half; ++i)
+      if (axis_of_pair[i] < 0 || axis_of_pair[i] >= n_axes) return ctx_fail(c, BS_EINVAL, "axis_of_pair[%d]=%d of %d axes", i, axis_of_pair[i], n_axes);
+    for (int64_t i = 0; i < (int64_t)n_axes * rows; ++i)
+      if (positions[i] < 0 || positions[i] >= g.max_positions)
+        return ctx_fail(c, BS_EINVAL, "positions[%lld]=%d outside [0, %d)", (long long)i, positions[i], g.max_positions);
+
+    Planned &p = w->p;
+    p.n_rows = rows;
+    p.n_pool_pages = n_pages;
+    // (longer windows and more sinks than any length change nothing)
+    p.window = std::min(window, MAX_LEN);
+    sinks = std::min(sinks, MAX_LEN);
+    const int per_unit = std::max(1, 16 / (g.n_q_heads / g.n_kv_heads));
+    if (const int rc = plan_units(w, b, p.window, sinks, per_unit, MOST_UNIT_PAGES)) { w->p = Planned(); return rc; }
+    if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff) { w->p = Planned(); return ctx_fail(c, BS_EUNSUPPORTED, "the step is too large for one plan"); }
+
+    p.has_angles = n_axes > 0;
+    const int axes = std::max(1, n_axes);
+    p.off_pages = 8L * p.n_items;
+    p.off_joins = p.off_pages + whole_units(p.pages);
+    p.off_row_page = p.off_joins + 4L * p.n_joins;
+    p.off_row_slot = p.off_row_page + rows;
+    p.off_axis = p.off_row_slot + rows;
+    p.off_positions = p.off_axis + half;
+    p.words = whole_units(p.off_positions + (long)axes * rows);
+    std::vector<int32_t> &words = w->words;
+    words.assign((size_t)p.words, 0);
+    if (p.n_items) std::memcpy(&words[p.off_items], w->items.data(), sizeof(WindowItem) * p.n_items);
+    if (p.pages) std::memcpy(&words[p.off_pages], w->item_pages.data(), sizeof(int32_t) * p.pages);
+    if (p.n_joins) std::memcpy(&words[p.off_joins], w->joins.data(), sizeof(int32_t) * w->joins.size());
+    bool turned = true;
+    for (int s = 0; s < b->n_seq; ++s) {
+      const int r0 = b->row_start[s], n = b->row_start[s + 1] - r0;
+      for (int j = 0; j < n; ++j) {
+        const int at = b->kv_len[s] - n + j;
+        words[p.off_row_page + r0 + j] = at < 0 ? -1 : b->page_ids[b->page_start[s] + at / PAGE];
+        words[p.off_row_slot + r0 + j] = at < 0 ? 0 : at % PAGE;
+        if (n_axes == 0) {
+          words[p.off_positions + r0 + j] = std::max(0, at);
+          turned = turned && at < g.max_positions;
+        }
+      }
+    }
+    p.has_angles = turned;
+    if (n_axes > 0) {
+      std::memcpy(&words[p.off_positions], positions, sizeof(int32_t) * (size_t)n_axes * rows);
+      std::memcpy(&words[p.off_axis], axis_of_pair, sizeof(int32_t) * half);
+    }
+    if (v.device == BS_DEVICE_NONE) { p.made = true; return BS_OK; }
+
+    const auto fail_with = [&](int rc) { w->p = Planned(); return rc; };
+    bool capturing = false;
+    if (hipError_t e = hipSetDevice(v.device)) return fail_with(ctx_fail(c, BS_EHIP, "hipSetDevice: %s", hipGetErrorString(e)));
+    if (const int rc = stream_is_capturing(c, st, &capturing)) return fail_with(rc);
+    if (capturing) return fail_with(ctx_fail(c, BS_EINVAL, "bs_window_plan cannot be captured: plan first, then capture the calls that use the plan"));
+    if (const int rc = grow(c, &w->d_words, &w->cap_words, p.words, sizeof(int32_t))) return fail_with(rc);
+    const size_t state_bytes = sizeof(float) * g.n_q_heads * (size_t)(g.head_dim + 2);
+    if (const int rc = grow(c, &w->d_states, &w->cap_states, p.states, state_bytes)) return fail_with(rc);
+    int32_t *pinned = nullptr;
+    if (const int e = w->stage.place(p.words, st, &pinned))
+      return fail_with(ctx_fail(c, e == hipErrorOutOfMemory ? BS_ENOMEM : BS_EHIP, "pinned memory of a plan: %s", hipGetErrorString((hipError_t)e)));
+    std::memcpy(pinned, words.data(), sizeof(int32_t) * (size_t)p.words);
+    Upload up;
+    up.src = reinterpret_cast<const uint4 *>(pinned);
+    up.dst = reinterpret_cast<uint4 *>(w->d_words);
+    up.n16 = (int)(p.words / 4);
+    up.blocks = (up.n16 + 255) / 256;
+    if (hipError_t e = launch_upload(up, st)) return fail_with(ctx_fail(c, BS_EHIP, "the plan's upload: %s", hipGetErrorString(e)));
+    p.made = true;
+    return BS_OK;
+  });
+}
+
+int bs_rope_append(bs_window *w, const void *qkv, int64_t qkv_stride, void *q, int64_t q_stride, void *kv_pool, void *stream) {
+  if (!w) return BS_EINVAL;
+  bs_ctx *c = w->ctx;
+  return ctx_guarded(c, [&]() -> int {
+    if (const int rc = check_call(w, "bs_rope_append")) return rc;
+    const Planned &p = w->p;
+    const CtxView v = ctx_view(c);
+    const bs_layer_cfg &g = *v.cfg;
+    if (p.n_rows == 0) return BS_OK;
+    if (!p.has_angles) return ctx_fail(c, BS_EINVAL, "bs_rope_append: a row stands beyond max_positions %d: plan with positions of its own", g.max_positions);
+    if (!qkv || !q || !kv_pool) return ctx_fail(c, BS_EINVAL, "bs_rope_append: NULL pointer");
+    const int64_t q_row = (int64_t)g.n_q_heads * g.head_dim, qkv_row = q_row + 2 * (int64_t)g.n_kv_heads * g.head_dim;
+    if (qkv_stride < qkv_row || q_stride < q_row || !aligned(qkv, qkv_stride) || !aligned(q, q_stride) || !aligned(kv_pool, 0))
+      return ctx_fail(c, BS_EINVAL, "bs_rope_append: rows of %lld and %lld elements at strides %lld and %lld (16-byte aligned, strides multiples of 8)",
+                      (long long)qkv_row, (long long)q_row, (long long)qkv_stride, (long long)q_stride);
+    if (q == qkv && q_stride != qkv_stride) return ctx_fail(c, BS_EINVAL, "bs_rope_append: in place, but with another stride");
+    CTX_HIP_TRY(c, hipSetDevice(v.device));
+    RopeArgs a{};
+    a.n_rows = p.n_rows; a.n_q_heads = g.n_q_heads; a.n_kv_heads = g.n_kv_heads; a.head_dim = g.head_dim;
+    a.cos = v.rope_cos; a.sin = v.rope_sin;
+    a.positions = w->d_words + p.off_positions;
+    a.axis_of_pair = w->d_words + p.off_axis;
+    a.row_page = w->d_words + p.off_row_page;
+    a.row_slot = w->d_words + p.off_row_slot;
+    a.qkv = (const uint16_t *)qkv; a.q = (uint16_t *)q; a.kv_pool = (uint16_t *)kv_pool;
+    a.qkv_stride = qkv_stride; a.q_stride = q_stride;
+    CTX_HIP_TRY(c, launch_rope_append(a, (hipStream_t)stream));
+    return BS_OK;
+  });
+}
+
+int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out, int64_t out_stride, const void *kv_pool, void *stream) {
+  if (!w) return BS_EINVAL;
+  bs_ctx *c = w->ctx;
+  return ctx_guarded(c, [&]() -> int {
+    if (const int rc = check_call(w, "bs_window_attention")) return rc;
+    const Planned &p = w->p;
+    const CtxView v = ctx_view(c);
+    const bs_layer_cfg &g = *v.cfg;
+    if (p.n_rows == 0) return BS_OK;
+    if (!q || !out || (!kv_pool && p.pages > 0)) return ctx_fail(c, BS_EINVAL, "bs_window_attention: NULL pointer");
+    const int64_t row = (int64_t)g.n_q_heads * g.head_dim;
+    if (q_stride < row || out_stride < row || !aligned(q, q_stride) || !aligned(out, out_stride) || !aligned(kv_pool, 0))
+      return ctx_fail(c, BS_EINVAL, "bs_window_attention: rows of %lld elements at strides %lld and %lld (16-byte aligned, strides multiples of 8)",
+                      (long long)row, (long long)q_stride, (long long)out_stride);
+    if (q == out && q_stride != out_stride) return ctx_fail(c, BS_EINVAL, "bs_window_attention: in place, but with another stride");
+    CTX_HIP_TRY(c, hipSetDevice(v.device));
+    const hipStream_t st = (hipStream_t)stream;
+    WindowArgs a{};
+    a.s = shape_of(g);
+    a.items = reinterpret_cast<const WindowItem *>(w->d_words + p.off_items);
+    a.item_pages = w->d_words + p.off_pages;
+    a.n_items = p.n_items; a.window = p.window;
+    a.q = (const uint16_t *)q; a.kv_pool = (const uint16_t *)kv_pool; a.out = (uint16_t *)out;
+    a.q_stride = q_stride; a.out_stride = out_stride;
+    a.joins = w->d_words + p.off_joins;
+    a.n_joins = p.n_joins;
+    a.part_acc = w->d_states;
+    a.part_m = a.part_acc + (size_t)p.states * g.n_q_heads * g.head_dim;
+    a.part_l = a.part_m + (size_t)p.states * g.n_q_heads;
+    CTX_HIP_TRY(c, launch_window_units(a, st));
+    CTX_HIP_TRY(c, launch_window_join(a, st));
+    return BS_OK;
+  });
+}
+
+int bs_window_division(const bs_window *w, bs_window_parts *out) {
+  if (!w) return BS_EINVAL;
+  if (!out) return ctx_fail(w->ctx, BS_EINVAL, "out is NULL");
+  if (!w->p.made) return ctx_fail(w->ctx, BS_EINVAL, "bs_window_division: nothing is planned");
+  const Planned &p = w->p;
+  *out = {p.n_items, p.longest, p.split_rows, 0, 0, p.pages};
+  return BS_OK;
+}
+
+}  // extern "C"
