@@ -150,10 +150,23 @@ __device__ __forceinline__ void merge_decode_unit(const MergeArgs &a, int unit, 
   *reinterpret_cast<u32x2_t *>(a.out + (size_t)a.row_start[seq] * (hq * DH) + head * DH + li * 4) = o2;
 }
 
+// elements of a row of the queries and of the result
+template <int DH, class Args>
+__device__ __forceinline__ size_t q_row(const Args &a) {
+  if constexpr (std::is_same_v<Args, WindowPrefillArgs>) return (size_t)a.q_stride;
+  else return (size_t)(a.s.n_q_heads * DH);
+}
+template <int DH, class Args>
+__device__ __forceinline__ size_t out_row(const Args &a) {
+  if constexpr (std::is_same_v<Args, WindowPrefillArgs> || std::is_same_v<Args, WindowMergeArgs>) return (size_t)a.out_stride;
+  else return (size_t)(a.s.n_q_heads * DH);
+}
+
 // The same for prefill work whose context is cut: a wavefront merges, of 32 query rows and one head, the 8 output columns
 // that lie in one accumulator register group of the ring kernel's wavefront, in that kernel's layout.
-template <int DH>
-__device__ __forceinline__ void merge_prefill_unit(const MergeArgs &a, int unit, int lane) {
+template <int DH, class Args>
+__device__ __forceinline__ void merge_prefill_unit(const Args &a, int unit, int lane) {
+  constexpr bool WINDOW = std::is_same_v<Args, WindowMergeArgs>;
   constexpr int GROUPS = DH / 8;  // register groups of a block of 32 rows
   const int wg_per_work = a.s.n_q_heads / a.cut_heads;
   const int group = unit % GROUPS, qb = unit / GROUPS % 2, region = unit / (2 * GROUPS);
@@ -192,11 +205,11 @@ __device__ __forceinline__ void merge_prefill_unit(const MergeArgs &a, int unit,
     }
   }
   if (row0 + lr >= q_len) return;
-  const float inv = 1.f / ls;
+  const float inv = WINDOW && ls == 0.f ? 0.f : 1.f / ls;  // (a row in front of its sequence sees nothing)
   u32x2_t o2;
   o2.x = pack_bf16x2(acc[0] * inv, acc[1] * inv);
   o2.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-  *reinterpret_cast<u32x2_t *>(a.out + (size_t)(r0 + row0 + lr) * (a.s.n_q_heads * DH) + head * DH + group * 8 + 4 * (lane >> 5)) = o2;
+  *reinterpret_cast<u32x2_t *>(a.out + (size_t)(r0 + row0 + lr) * out_row<DH>(a) + head * DH + group * 8 + 4 * (lane >> 5)) = o2;
 }
 
 template <int DH>
@@ -206,6 +219,12 @@ __global__ __launch_bounds__(256) void merge_kernel(const MergeArgs a, int n_dec
     merge_decode_unit<DH>(a, unit, lane);
   else if (unit < n_units)
     merge_prefill_unit<DH>(a, unit - n_decode_units, lane);
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) void window_merge_kernel(const WindowMergeArgs a, int n_units) {
+  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit < n_units) merge_prefill_unit<DH>(a, unit, threadIdx.x & 63);
 }
 
 // ------------------------------------------------------------------------------
@@ -256,17 +275,16 @@ __device__ __forceinline__ void score_mfma(f32x16_t &s, bf16x8_t k, bf16x8_t q) 
 }
 
 // out = o / l of 64 query rows (two blocks of 32, of which the first n_q exist) from row `row` on, one head
-template <int DH>
-__device__ __forceinline__ void store_prefill_rows(const PrefillArgs &a, const f32x16_t (&o)[2][DH / 32], const float (&l)[2],
+template <int DH, class Args>
+__device__ __forceinline__ void store_prefill_rows(const Args &a, const f32x16_t (&o)[2][DH / 32], const float (&l)[2],
                                                    const int (&n_q)[2], int row, int head, int lr, int g2) {
-  const int hq = a.s.n_q_heads;
 #pragma unroll
   for (int qb = 0; qb < 2; ++qb) {
     float ls = l[qb];
     ls += __shfl_xor(ls, 32, 64);
     if (lr < n_q[qb]) {
-      const float inv = 1.f / ls;
-      uint16_t *dst = a.out + (size_t)(row + qb * 32 + lr) * (hq * DH) + head * DH;
+      const float inv = std::is_same_v<Args, WindowPrefillArgs> && ls == 0.f ? 0.f : 1.f / ls;
+      uint16_t *dst = a.out + (size_t)(row + qb * 32 + lr) * out_row<DH>(a) + head * DH;
 #pragma unroll
       for (int db = 0; db < DH / 32; ++db)
 #pragma unroll
@@ -304,8 +322,10 @@ __device__ __forceinline__ void store_prefill_state(const PrefillArgs &a, const 
   }
 }
 
-template <int DH>
-__device__ __forceinline__ void prefill_workgroup(const PrefillArgs &a, int heads_per_wg, int b, int wave, int lane, unsigned char *smem) {
+template <int DH, class Args>
+__device__ __forceinline__ void prefill_workgroup(const Args &a, int heads_per_wg, int b, int wave, int lane, unsigned char *smem) {
+  constexpr bool WINDOW = std::is_same_v<Args, WindowPrefillArgs>;
+  constexpr float HIDDEN = WINDOW ? -INFINITY : NEG_BIG;  // (a row may see nothing of its first block: weights of zero, not of one)
   constexpr int KC = DH / 16;  // k-steps of the 32x32x16 score MFMA
   constexpr int DB = DH / 32;  // 32-row blocks of the output
   constexpr int NQ = 2;        // blocks of 32 query rows per wavefront
@@ -316,15 +336,25 @@ __device__ __forceinline__ void prefill_workgroup(const PrefillArgs &a, int head
   const int hkv = a.s.n_kv_heads, hq = a.s.n_q_heads, grp = hq / hkv;
   const int wg_per_work = hq / heads_per_wg;
   const int w = b / wg_per_work;
-  const int32_t *work = a.work + (a.cut ? 4 : 2) * w;
+  const bool cut = WINDOW || a.cut;
+  const int32_t *work = a.work + (cut ? 4 : 2) * w;
   const int seq = work[0], qblk = work[1];  // block of 64 * (4 / heads_per_wg) query rows
   // blocks of 32 tokens [t0, t1) of the context (t1 = 0: to its end)
-  const int t0 = a.cut ? work[2] & 0xFFFF : 0, t1 = a.cut ? (int)((unsigned)work[2] >> 16) : 0, state = a.cut ? work[3] : -1;
+  const int t0 = cut ? work[2] & 0xFFFF : 0, t1 = cut ? (int)((unsigned)work[2] >> 16) : 0, state = cut ? work[3] : -1;
   const int head = (b % wg_per_work) * heads_per_wg + wave % heads_per_wg;
   const int kvh = head / grp;
   const int r0 = a.row_start[seq], q_len = a.row_start[seq + 1] - r0;
+  // WINDOW: the pages between the sink pages and the first that the workgroup's first row sees are left out
+  int n_sink = 0, left_out = 0, window = 0, sinks = 0;
+  if constexpr (WINDOW) {
+    const int first = max(0, a.kv_len[seq] - q_len + qblk * 64 * (4 / heads_per_wg) - a.window + 1) >> 4;
+    n_sink = min((int)(((unsigned)a.sinks + 15) >> 4), first);
+    left_out = first - n_sink;
+    window = a.window;
+    sinks = a.sinks - 32 * t0;
+  }
   // tokens are counted from the range's first one: the range ends at kv_len, row 0 of the segment stands at `before`
-  const int whole_len = a.kv_len[seq], before = whole_len - q_len - 32 * t0;
+  const int whole_len = a.kv_len[seq] - 16 * left_out, before = whole_len - q_len - 32 * t0;
   const int kv_len = (t1 ? 32 * t1 : whole_len) - 32 * t0;
   const int lr = lane & 31, g2 = lane >> 5;
   // (through the constant address space: nobody writes the page table, and its loads stay on the scalar
@@ -352,7 +382,11 @@ __device__ __forceinline__ void prefill_workgroup(const PrefillArgs &a, int head
       src[i] = (uint32_t)(tok * DH * 2 + (((p % CPR) ^ f) << 4));
     }
   }
-  auto page_of = [&](int tb) __attribute__((always_inline)) { return pages[min(2 * tb + (wave >> 1), n_pg - 1)]; };
+  auto page_of = [&](int tb) __attribute__((always_inline)) {
+    const int at = min(2 * tb + (wave >> 1), n_pg - 1);
+    if constexpr (WINDOW) return pages[at + (at + 2 * t0 < n_sink ? 0 : left_out)];
+    else return pages[at];
+  };
   const unsigned char *tiles = reinterpret_cast<const unsigned char *>(a.kv_pool) + (size_t)((wave & 1) * hkv + kvh) * TILE;
   const uint32_t page_stride = (uint32_t)(2 * hkv * TILE);
   auto request = [&](int page, int slot) __attribute__((always_inline)) {
@@ -373,7 +407,7 @@ __device__ __forceinline__ void prefill_workgroup(const PrefillArgs &a, int head
     first_pos[qb] = before + row0;
     my_pos[qb] = min(first_pos[qb] + lr, kv_len - 1);
     const bool ok = lr < n_q[qb];
-    const uint16_t *p = a.q + (size_t)(r0 + (ok ? row0 + lr : 0)) * (hq * DH) + head * DH + 8 * g2;
+    const uint16_t *p = a.q + (size_t)(r0 + (ok ? row0 + lr : 0)) * q_row<DH>(a) + head * DH + 8 * g2;
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
       u32x4_t v = {0u, 0u, 0u, 0u};
@@ -417,9 +451,17 @@ __device__ __forceinline__ void prefill_workgroup(const PrefillArgs &a, int head
       const int lim = my_pos[qb] - tb * 32 - 8 * g2;
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (16 * (r >> 3) + (r & 7) > lim) s[r] = NEG_BIG;
+        if (16 * (r >> 3) + (r & 7) > lim) s[r] = HIDDEN;
       mx = max_of(s);
     }
+    if constexpr (WINDOW)
+      if (tb * 32 <= first_pos[qb] + 31 - window && tb * 32 + 31 >= sinks) {  // and tokens in front of some query's window
+        const int lim = my_pos[qb] - window - tb * 32 - 8 * g2, sink_lim = sinks - tb * 32 - 8 * g2;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (16 * (r >> 3) + (r & 7) <= lim && 16 * (r >> 3) + (r & 7) >= sink_lim) s[r] = HIDDEN;
+        mx = max_of(s);
+      }
     mx *= a.s.scale_log2e;  // the scale is positive: the maximum commutes with it
     if (__builtin_amdgcn_ballot_w64(mx > m[qb] + TAU) != 0) {
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -529,6 +571,14 @@ __device__ __forceinline__ void prefill_workgroup(const PrefillArgs &a, int head
 #pragma unroll
         for (int h = 0; h < 2; ++h) va[db][h] = mask_tokens8(va[db][h], tb * 32 + 16 * h + 8 * g2, kv_len);
     }
+    if constexpr (WINDOW) {
+      const int unseen = before + wg_row0 - window + 1;  // tokens [sinks, unseen) are seen by no row of the workgroup
+      if (tb * 32 < unseen && tb * 32 + 32 > sinks)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) va[db][h] = mask_between8(va[db][h], tb * 32 + 16 * h + 8 * g2, sinks, unseen);
+    }
     float mx0 = 0.f, mx1 = 0.f;  // maxima of s_nxt: its last MFMA is N_PV MFMAs old when they are taken
     auto pv = [&](int qb, int j) __attribute__((always_inline)) {
       const int db = j % DB, h = j / DB;
@@ -585,6 +635,14 @@ __device__ __forceinline__ void prefill_workgroup(const PrefillArgs &a, int head
 // groups, 128 segments: 16 rows 24 against 17 us, 64 rows 36 against 30, 64 rows behind 500 tokens 86 against 65).
 template <int DH>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, DH == 64 ? 2 : 1))) void prefill_attn_kernel(const PrefillArgs a, int heads_per_wg) {
+  extern __shared__ __align__(256) unsigned char attn_smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  prefill_workgroup<DH>(a, heads_per_wg, blockIdx.x, wave, threadIdx.x & 63, attn_smem);
+}
+
+// The same on rows that see a window and sinks.
+template <int DH>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, DH == 64 ? 2 : 1))) void window_prefill_kernel(const WindowPrefillArgs a, int heads_per_wg) {
   extern __shared__ __align__(256) unsigned char attn_smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   prefill_workgroup<DH>(a, heads_per_wg, blockIdx.x, wave, threadIdx.x & 63, attn_smem);
@@ -910,6 +968,24 @@ hipError_t launch_merge(const MergeArgs &a, hipStream_t stream) {
     hipLaunchKernelGGL((merge_kernel<64>), dim3((n_units + 3) / 4), dim3(256), 0, stream, a, n_decode_units, n_units);
   else
     return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_window_prefill(const WindowPrefillArgs &a, int heads, hipStream_t stream) {
+  if (a.n_work <= 0) return hipSuccess;
+  const int grid = a.n_work * (a.s.n_q_heads / heads);
+  static OncePerDevice once[2];
+  if (a.s.head_dim == 128) return launch_with_lds(window_prefill_kernel<128>, once[0], grid, PF_LDS(128), stream, a, heads);
+  if (a.s.head_dim == 64) return launch_with_lds(window_prefill_kernel<64>, once[1], grid, PF_LDS(64), stream, a, heads);
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_window_merge(const WindowMergeArgs &a, hipStream_t stream) {
+  if (a.n_cut <= 0) return hipSuccess;
+  const int n_units = a.n_cut * (a.s.n_q_heads / a.cut_heads) * 4 * 2 * (a.s.head_dim / 8);
+  if (a.s.head_dim == 128) hipLaunchKernelGGL(window_merge_kernel<128>, dim3((n_units + 3) / 4), dim3(256), 0, stream, a, n_units);
+  else if (a.s.head_dim == 64) hipLaunchKernelGGL(window_merge_kernel<64>, dim3((n_units + 3) / 4), dim3(256), 0, stream, a, n_units);
+  else return hipErrorInvalidValue;
   return hipGetLastError();
 }
 

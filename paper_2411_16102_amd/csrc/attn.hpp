@@ -101,6 +101,20 @@ struct PrefillRoute {
 PrefillRoute prefill_route(const AttnShape &s, int n_prefill, const int32_t *row_start, const int32_t *kv_len);
 hipError_t launch_prefill_attn(const PrefillArgs &a, const PrefillRoute &route, hipStream_t stream);
 
+// The ring kernel on rows that see a window and sinks (see window.hip): the context that a workgroup walks is its sink pages
+// and its window pages, one behind the other, and blocks of 32 tokens, ranges and masks count along that list.  Rows may
+// stand in front of their sequence (kv_len below the rows), though not all of a workgroup's; a row may see nothing of a range.
+// work is [n_work][4] always; entries of page_ids that no row sees are not read.
+struct WindowPrefillArgs : PrefillArgs {
+  int window, sinks;
+  int64_t q_stride, out_stride;  // elements of a row
+};
+hipError_t launch_window_prefill(const WindowPrefillArgs &a, int heads, hipStream_t stream);
+struct WindowMergeArgs : MergeArgs {
+  int64_t out_stride;
+};
+hipError_t launch_window_merge(const WindowMergeArgs &a, hipStream_t stream);
+
 // both kinds in one launch (prefill workgroups dealt evenly among the decode ones); needs a step with
 // prefill work and decode items, and a group size that is a multiple of four
 bool blended_attn_possible(const AttnShape &s);

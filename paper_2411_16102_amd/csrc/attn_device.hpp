@@ -46,6 +46,14 @@ __device__ __forceinline__ u32x4_t mask_tokens8(u32x4_t v, int t0, int limit) {
   return u32x4_t{lo.x, lo.y, hi.x, hi.y};
 }
 
+// zero those of eight tokens t0 .. t0+7 that lie in [lo, hi)
+__device__ __forceinline__ u32x4_t mask_between8(u32x4_t v, int t0, int lo, int hi) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (t0 + i >= lo && t0 + i < hi) v[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+  return v;
+}
+
 // acc *= alpha for MFMA accumulators that live in the accumulation registers (kernels that run one
 // wavefront per SIMD).  Written out by hand so that the only vector-ALU use of the output
 // accumulators inside the token loop is this rarely taken path: left to the compiler, the register

@@ -24,11 +24,14 @@ constexpr long STAGE_WORDS = 1 << 16;   // of the plan's pinned memory at first 
 // What the kernels of a planned step need to know beside the arrays on the device.
 struct Planned {
   bool made = false, has_angles = false;
-  int n_rows = 0, n_items = 0, n_joins = 0, window = 1;
+  int n_rows = 0, n_items = 0, n_joins = 0, window = 1, sinks = 0;
+  int n_work = 0, n_cut = 0, wide_blocks = 0;   // wide work: workgroups per group of heads, blocks of rows that several share, all blocks
   int32_t longest = 0, split_rows = 0;
-  int64_t n_pool_pages = 0;
-  long states = 0, pages = 0;
+  long states = 0, cut_states = 0, pages = 0;
   long off_items = 0, off_pages = 0, off_joins = 0, off_row_page = 0, off_row_slot = 0, off_positions = 0, off_axis = 0, words = 0;
+  long off_work = 0, off_cut = 0, off_row_start = 0, off_kv_len = 0, off_page_start = 0, off_page_ids = 0;
+  // partial states, in floats
+  long at_m = 0, at_l = 0, at_cut_acc = 0, at_cut_m = 0, at_cut_l = 0, state_floats = 0;
 };
 
 }  // namespace
@@ -42,8 +45,10 @@ struct bs_window {
   float *d_states = nullptr;
   long cap_states = 0;
   // host scratch reused across plans
-  std::vector<int32_t> words, refs, item_pages, joins;
+  std::vector<int32_t> words, refs, item_pages, joins, cut, wide_start, wide_pages;
   std::vector<WindowItem> items;
+  struct Work { int blocks, seq, block, t0, t1, state; };
+  std::vector<Work> work;
 };
 
 namespace {
@@ -92,6 +97,7 @@ struct Seen {
   int n_sink, first, last;
   int pages() const { return n_sink + last - first + 1; }
   int left_out() const { return PAGE * (first - n_sink); }  // tokens between the two parts
+  int page(int i) const { return i < n_sink ? i : first + i - n_sink; }
 };
 Seen seen_by(int p0, int p1, int window, int sinks) {
   if (p1 < 0) return {0, 0, -1};
@@ -99,49 +105,110 @@ Seen seen_by(int p0, int p1, int window, int sinks) {
   return {std::min((int)(((int64_t)sinks + PAGE - 1) / PAGE), first), first, p1 / PAGE};
 }
 
-// Cuts the rows of every sequence into units; chunk: pages of a unit.
-int plan_units(bs_window *w, const bs_batch *b, int window, int sinks, int rows_per_unit, int chunk) {
+int check_seen(bs_window *w, int seq, const int32_t *table, const Seen &seen) {
+  for (int i = 0; i < seen.pages(); ++i) {
+    const int pg = seen.page(i);
+    if (table[pg] < 0) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d: a row sees page %d of its table, which was given up", seq, pg);
+  }
+  return BS_OK;
+}
+
+int too_large(bs_window *w) { return ctx_fail(w->ctx, BS_EUNSUPPORTED, "the step is too large for one plan"); }
+
+// Cuts rows [j, end) of a sequence into narrow units of at most `per_unit` rows and `chunk` pages.
+int add_units(bs_window *w, const bs_batch *b, int s, int j, int end, int per_unit, int chunk) {
+  Planned &p = w->p;
+  const int r0 = b->row_start[s], rows = b->row_start[s + 1] - r0;
+  const int32_t *table = b->page_ids + b->page_start[s];
+  for (; j < end; j += per_unit) {
+    const int n = std::min(per_unit, end - j), p0 = b->kv_len[s] - rows + j;
+    const Seen seen = seen_by(p0, p0 + n - 1, p.window, p.sinks);
+    if (const int rc = check_seen(w, s, table, seen)) return rc;
+    const int n_pages = seen.pages(), n_chunks = std::max(1, (n_pages + chunk - 1) / chunk);
+    for (int k = 0; k < n_chunks; ++k) {
+      // chunks of nearly equal lengths
+      const int lo = (int)((int64_t)n_pages * k / n_chunks), hi = (int)((int64_t)n_pages * (k + 1) / n_chunks);
+      WindowItem it{};
+      it.row0 = r0 + j;
+      it.n_rows = n;
+      it.page_off = (int32_t)w->item_pages.size();
+      it.n_pages = hi - lo;
+      it.at = p0 - seen.left_out() - PAGE * lo;
+      it.sinks = std::max(0, std::min(p.sinks - PAGE * lo, PAGE * (hi - lo)));
+      it.state = n_chunks > 1 ? (int32_t)(p.states + (long)k * n) : -1;
+      w->items.push_back(it);
+      for (int i = lo; i < hi; ++i) w->item_pages.push_back(table[seen.page(i)]);
+      p.longest = std::max(p.longest, it.n_pages);
+    }
+    if (n_chunks > 1) {
+      for (int i = 0; i < n; ++i) w->joins.insert(w->joins.end(), {r0 + j + i, (int32_t)(p.states + i), n, n_chunks});
+      p.states += (long)n_chunks * n;
+      p.split_rows += n;
+    }
+    if (p.states > MAX_LEN || w->item_pages.size() > (size_t)MAX_LEN) return too_large(w);
+  }
+  return BS_OK;
+}
+
+// How a step's rows are divided between the two kinds of work.
+struct Route {
+  int per_unit;   // rows of a narrow unit
+  int heads, rows;  // of a wide workgroup: query heads of one KV group, query rows
+};
+Route route_of(const bs_layer_cfg &g) {
+  const int grp = g.n_q_heads / g.n_kv_heads, heads = grp % 4 == 0 ? 4 : grp % 2 == 0 ? 2 : 1;
+  return {std::max(1, 16 / grp), heads, 64 * (4 / heads)};
+}
+bool is_wide(const Route &r, int rows) { return rows > 4 * r.per_unit; }
+
+// The rows of a longer segment as blocks for wide workgroups; rows of blocks that stand wholly in front of their sequence see nothing:
+// units without pages.
+int add_blocks(bs_window *w, const bs_batch *b, int s, const Route &r) {
+  Planned &p = w->p;
+  const int rows = b->row_start[s + 1] - b->row_start[s];
+  const int32_t *table = b->page_ids + b->page_start[s];
+  for (int k = 0; k * r.rows < rows; ++k) {
+    const int j = k * r.rows, end = std::min(rows, j + r.rows), p0 = b->kv_len[s] - rows + j, p1 = b->kv_len[s] - rows + end - 1;
+    if (p1 < 0) {
+      if (const int rc = add_units(w, b, s, j, end, r.per_unit, MOST_UNIT_PAGES)) return rc;
+      continue;
+    }
+    const Seen seen = seen_by(p0, p1, p.window, p.sinks);
+    if (const int rc = check_seen(w, s, table, seen)) return rc;
+    w->work.push_back({(seen.pages() + 1) / 2, s, k, 0, 0, -1});
+    p.pages += seen.pages();
+    ++p.wide_blocks;
+  }
+  return BS_OK;
+}
+
+int plan_work(bs_window *w, const bs_batch *b, const Route &r) {
   Planned &p = w->p;
   w->items.clear();
   w->item_pages.clear();
   w->joins.clear();
+  w->work.clear();
+  w->cut.clear();
+  w->wide_start.assign((size_t)b->n_seq + 1, 0);
+  w->wide_pages.clear();
   for (int s = 0; s < b->n_seq; ++s) {
-    const int r0 = b->row_start[s], rows = b->row_start[s + 1] - r0;
-    const int32_t *table = b->page_ids + b->page_start[s];
-    for (int j = 0; j < rows; j += rows_per_unit) {
-      const int n = std::min(rows_per_unit, rows - j), p0 = b->kv_len[s] - rows + j, p1 = p0 + n - 1;
-      const Seen seen = seen_by(p0, p1, window, sinks);
-      const int n_pages = seen.pages(), n_chunks = std::max(1, (n_pages + chunk - 1) / chunk);
-      for (int i = 0; i < n_pages; ++i) {
-        const int pg = i < seen.n_sink ? i : seen.first + i - seen.n_sink;
-        if (table[pg] < 0) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d: a row sees page %d of its table, which was given up", s, pg);
-      }
-      for (int k = 0; k < n_chunks; ++k) {
-        // chunks of nearly equal lengths
-        const int lo = (int)((int64_t)n_pages * k / n_chunks), hi = (int)((int64_t)n_pages * (k + 1) / n_chunks);
-        WindowItem it{};
-        it.row0 = r0 + j;
-        it.n_rows = n;
-        it.page_off = (int32_t)w->item_pages.size();
-        it.n_pages = hi - lo;
-        it.at = p0 - seen.left_out() - PAGE * lo;
-        it.sinks = std::max(0, std::min(sinks - PAGE * lo, PAGE * (hi - lo)));
-        it.state = n_chunks > 1 ? (int32_t)(p.states + (long)k * n) : -1;
-        w->items.push_back(it);
-        for (int i = lo; i < hi; ++i) w->item_pages.push_back(table[i < seen.n_sink ? i : seen.first + i - seen.n_sink]);
-        p.longest = std::max(p.longest, it.n_pages);
-      }
-      if (n_chunks > 1) {
-        for (int i = 0; i < n; ++i) w->joins.insert(w->joins.end(), {r0 + j + i, (int32_t)(p.states + i), n, n_chunks});
-        p.states += (long)n_chunks * n;
-        p.split_rows += n;
-      }
-      if (p.states > MAX_LEN || w->item_pages.size() > (size_t)MAX_LEN) return ctx_fail(w->ctx, BS_EUNSUPPORTED, "the step is too large for one plan");
+    const int rows = b->row_start[s + 1] - b->row_start[s];
+    w->wide_start[s] = (int32_t)w->wide_pages.size();
+    if (is_wide(r, rows)) {
+      if (const int rc = add_blocks(w, b, s, r)) return rc;
+      w->wide_pages.insert(w->wide_pages.end(), b->page_ids + b->page_start[s], b->page_ids + b->page_start[s + 1]);
+    } else if (const int rc = add_units(w, b, s, 0, rows, r.per_unit, MOST_UNIT_PAGES)) {
+      return rc;
     }
   }
+  w->wide_start[b->n_seq] = (int32_t)w->wide_pages.size();
   p.n_items = (int)w->items.size();
   p.n_joins = (int)w->joins.size() / 4;
-  p.pages = (long)w->item_pages.size();
+  p.pages += (long)w->item_pages.size();
+  // longest first: the short ones then fill the end of the launch
+  std::stable_sort(w->work.begin(), w->work.end(), [](const auto &x, const auto &y) { return x.blocks > y.blocks; });
+  p.n_work = (int)w->work.size();
+  p.n_cut = (int)w->cut.size() / 4;
   return BS_OK;
 }
 
@@ -244,19 +311,26 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
 
     Planned &p = w->p;
     p.n_rows = rows;
-    p.n_pool_pages = n_pages;
     // (longer windows and more sinks than any length change nothing)
     p.window = std::min(window, MAX_LEN);
-    sinks = std::min(sinks, MAX_LEN);
-    const int per_unit = std::max(1, 16 / (g.n_q_heads / g.n_kv_heads));
-    if (const int rc = plan_units(w, b, p.window, sinks, per_unit, MOST_UNIT_PAGES)) { w->p = Planned(); return rc; }
-    if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff) { w->p = Planned(); return ctx_fail(c, BS_EUNSUPPORTED, "the step is too large for one plan"); }
+    p.sinks = std::min(sinks, MAX_LEN);
+    const auto fail_with = [&](int rc) { w->p = Planned(); return rc; };
+    const Route route = route_of(g);
+    if (const int rc = plan_work(w, b, route)) return fail_with(rc);
+    if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff) return fail_with(too_large(w));
 
-    p.has_angles = n_axes > 0;
     const int axes = std::max(1, n_axes);
+    const long n_item_pages = (long)w->item_pages.size(), n_wide_pages = (long)w->wide_pages.size();
     p.off_pages = 8L * p.n_items;
-    p.off_joins = p.off_pages + whole_units(p.pages);
-    p.off_row_page = p.off_joins + 4L * p.n_joins;
+    p.off_joins = p.off_pages + whole_units(n_item_pages);
+    p.off_work = p.off_joins + 4L * p.n_joins;
+    p.off_cut = p.off_work + 4L * p.n_work;
+    p.off_row_start = p.off_cut + 4L * p.n_cut;
+    const long n_tab = p.n_work ? b->n_seq + 1 : 0;
+    p.off_kv_len = p.off_row_start + n_tab;
+    p.off_page_start = p.off_kv_len + n_tab;
+    p.off_page_ids = p.off_page_start + n_tab;
+    p.off_row_page = p.off_page_ids + n_wide_pages;
     p.off_row_slot = p.off_row_page + rows;
     p.off_axis = p.off_row_slot + rows;
     p.off_positions = p.off_axis + half;
@@ -264,7 +338,22 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     std::vector<int32_t> &words = w->words;
     words.assign((size_t)p.words, 0);
     if (p.n_items) std::memcpy(&words[p.off_items], w->items.data(), sizeof(WindowItem) * p.n_items);
-    if (p.pages) std::memcpy(&words[p.off_pages], w->item_pages.data(), sizeof(int32_t) * p.pages);
+    if (n_item_pages) std::memcpy(&words[p.off_pages], w->item_pages.data(), sizeof(int32_t) * n_item_pages);
+    for (int i = 0; i < p.n_work; ++i) {
+      const bs_window::Work &k = w->work[i];
+      int32_t *to = &words[p.off_work + 4L * i];
+      to[0] = k.seq;
+      to[1] = k.block;
+      to[2] = (int32_t)((uint32_t)k.t0 | (uint32_t)k.t1 << 16);
+      to[3] = k.state;
+    }
+    if (p.n_cut) std::memcpy(&words[p.off_cut], w->cut.data(), sizeof(int32_t) * w->cut.size());
+    if (p.n_work) {
+      std::memcpy(&words[p.off_row_start], b->row_start, sizeof(int32_t) * n_tab);
+      std::memcpy(&words[p.off_kv_len], b->kv_len, sizeof(int32_t) * b->n_seq);
+      std::memcpy(&words[p.off_page_start], w->wide_start.data(), sizeof(int32_t) * n_tab);
+      if (n_wide_pages) std::memcpy(&words[p.off_page_ids], w->wide_pages.data(), sizeof(int32_t) * n_wide_pages);
+    }
     if (p.n_joins) std::memcpy(&words[p.off_joins], w->joins.data(), sizeof(int32_t) * w->joins.size());
     bool turned = true;
     for (int s = 0; s < b->n_seq; ++s) {
@@ -286,14 +375,19 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     }
     if (v.device == BS_DEVICE_NONE) { p.made = true; return BS_OK; }
 
-    const auto fail_with = [&](int rc) { w->p = Planned(); return rc; };
     bool capturing = false;
     if (hipError_t e = hipSetDevice(v.device)) return fail_with(ctx_fail(c, BS_EHIP, "hipSetDevice: %s", hipGetErrorString(e)));
     if (const int rc = stream_is_capturing(c, st, &capturing)) return fail_with(rc);
     if (capturing) return fail_with(ctx_fail(c, BS_EINVAL, "bs_window_plan cannot be captured: plan first, then capture the calls that use the plan"));
     if (const int rc = grow(c, &w->d_words, &w->cap_words, p.words, sizeof(int32_t))) return fail_with(rc);
-    const size_t state_bytes = sizeof(float) * g.n_q_heads * (size_t)(g.head_dim + 2);
-    if (const int rc = grow(c, &w->d_states, &w->cap_states, p.states, state_bytes)) return fail_with(rc);
+    const long n = p.states * g.n_q_heads, n_cut = p.cut_states * route.rows * g.n_q_heads;  // state rows of a head
+    p.at_m = n * g.head_dim;
+    p.at_l = p.at_m + whole_units(n);
+    p.at_cut_acc = p.at_l + whole_units(n);
+    p.at_cut_m = p.at_cut_acc + n_cut * g.head_dim;
+    p.at_cut_l = p.at_cut_m + n_cut;
+    p.state_floats = p.at_cut_l + n_cut;
+    if (const int rc = grow(c, &w->d_states, &w->cap_states, p.state_floats, sizeof(float))) return fail_with(rc);
     int32_t *pinned = nullptr;
     if (const int e = w->stage.place(p.words, st, &pinned))
       return fail_with(ctx_fail(c, e == hipErrorOutOfMemory ? BS_ENOMEM : BS_EHIP, "pinned memory of a plan: %s", hipGetErrorString((hipError_t)e)));
@@ -367,8 +461,22 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
     a.joins = w->d_words + p.off_joins;
     a.n_joins = p.n_joins;
     a.part_acc = w->d_states;
-    a.part_m = a.part_acc + (size_t)p.states * g.n_q_heads * g.head_dim;
-    a.part_l = a.part_m + (size_t)p.states * g.n_q_heads;
+    a.part_m = w->d_states + p.at_m;
+    a.part_l = w->d_states + p.at_l;
+    if (p.n_work) {
+      const Route route = route_of(g);
+      WindowPrefillArgs f{};
+      f.s = a.s;
+      f.work = w->d_words + p.off_work;
+      f.n_work = p.n_work;
+      f.cut = p.n_cut > 0;
+      f.part_acc = w->d_states + p.at_cut_acc; f.part_m = w->d_states + p.at_cut_m; f.part_l = w->d_states + p.at_cut_l;
+      f.row_start = w->d_words + p.off_row_start; f.kv_len = w->d_words + p.off_kv_len;
+      f.page_start = w->d_words + p.off_page_start; f.page_ids = w->d_words + p.off_page_ids;
+      f.q = a.q; f.kv_pool = a.kv_pool; f.out = a.out;
+      f.window = p.window; f.sinks = p.sinks; f.q_stride = q_stride; f.out_stride = out_stride;
+      CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
+    }
     CTX_HIP_TRY(c, launch_window_units(a, st));
     CTX_HIP_TRY(c, launch_window_join(a, st));
     return BS_OK;
@@ -380,7 +488,7 @@ int bs_window_division(const bs_window *w, bs_window_parts *out) {
   if (!out) return ctx_fail(w->ctx, BS_EINVAL, "out is NULL");
   if (!w->p.made) return ctx_fail(w->ctx, BS_EINVAL, "bs_window_division: nothing is planned");
   const Planned &p = w->p;
-  *out = {p.n_items, p.longest, p.split_rows, 0, 0, p.pages};
+  *out = {p.n_items, p.longest, p.split_rows, p.wide_blocks, p.n_cut, p.pages};
   return BS_OK;
 }
 
