@@ -7,6 +7,8 @@
 //   sum x w = sum x (128 + w) - 128 sum x,
 // which joins the zero point: y += scale * (D - (128 + zero) * X), D the product over the group and X the sum of its x.  All in 32 bits:
 // D is at most some hundred times the result, which leaves 16 of its 24 bits.
+#include <algorithm>
+
 #include "../../include/blendstep_stream.h"
 #include "common.hpp"
 #include "context.hpp"
@@ -23,44 +25,296 @@ __device__ __forceinline__ bf16x8_t as_operand(uint32_t w) {
   return as_bf16x8(v);
 }
 
-// A wavefront per 16 outputs and 16 rows.
-template <int GROUP, bool ZEROS>
-__global__ __launch_bounds__(64) void w4_kernel(const W4Args a, const W4Layout l) {
-  constexpr int STEPS = GROUP / 32;  // matrix instructions of a group
-  const int lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
-  const int64_t nb = blockIdx.x;
-  const int m = blockIdx.y * 16 + j;
-  const uint16_t *x = a.x + m * a.x_stride + 8 * g4;
-  const u32x4_t ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-  f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t kb = 0; kb < l.k_blocks; ++kb) {
-    const u32x4_t w = *reinterpret_cast<const u32x4_t *>(a.weight + (nb * l.k_blocks + kb) * 1024 + lane * 16);
+constexpr u32x4_t ONES = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+
+// 16-byte accesses that all XCDs agree on (their L2 caches are their own): partial sums travel past those
+constexpr int SC1 = 16;
+__device__ __forceinline__ void put_part(const __amdgpu_buffer_rsrc_t &rs, unsigned at, f32x4_t v) {
+  const u32x4_t w = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  __builtin_amdgcn_raw_buffer_store_b128(w, rs, at, 0, SC1);
+}
+__device__ __forceinline__ f32x4_t get_part(const __amdgpu_buffer_rsrc_t &rs, unsigned at) {
+  const u32x4_t w = __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, SC1);
+  return f32x4_t{__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+}
+
+// Whether this workgroup is the last of `parts` to arrive at a counter (which it clears for the next launch).
+__device__ __forceinline__ bool last_of(unsigned *counter, unsigned parts, unsigned *flag) {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wavefront's part has arrived where all XCDs see it
+  __syncthreads();
+  if (threadIdx.x == 0) *flag = atomicAdd(counter, 1u);
+  __syncthreads();
+  if (*flag + 1u != parts) return false;
+  if (threadIdx.x == 0) atomicExch(counter, 0u);
+  return true;
+}
+
+// four outputs n0 .. n0 + 3 of row m
+__device__ __forceinline__ void store_four(const W4Args &a, int m, int n0, f32x4_t v, bool wide) {
+  if (m >= a.m) return;
+  uint16_t *y = a.y + m * a.y_stride + n0;
+  if (wide && n0 + 4 <= a.n) {
+    *reinterpret_cast<u32x2_t *>(y) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    return;
+  }
 #pragma unroll
-    for (int g = 0; g < 128 / GROUP; ++g) {
-      const int64_t at = nb * l.groups + kb * (128 / GROUP) + g;
-      f32x4_t d = {0.f, 0.f, 0.f, 0.f}, sum = {0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < 4; ++r)
+    if (n0 + r < a.n) y[r] = (uint16_t)pack_bf16x2(v[r], 0.f);
+}
+__device__ __forceinline__ bool wide_rows(const W4Args &a) { return (a.y_stride & 3) == 0 && (reinterpret_cast<uintptr_t>(a.y) & 7) == 0; }
+
+// Scales (and zero points) of four outputs in one group, as 32-bit numbers.
+template <bool ZEROS>
+struct Group {
+  u32x2_t s;
+  uint32_t z;
+  __device__ __forceinline__ void load(const W4Args &a, const W4Layout &l, int64_t at, int g4) {
+    s = *reinterpret_cast<const u32x2_t *>(a.weight + l.scales + at * 32 + 8 * g4);
+    if constexpr (ZEROS) z = *reinterpret_cast<const uint32_t *>(a.weight + l.zeros + at * 16 + 4 * g4);
+  }
+  __device__ __forceinline__ void here() {
+    asm volatile("" : "+v"(s));
+    if constexpr (ZEROS) asm volatile("" : "+v"(z));
+  }
+  __device__ __forceinline__ float scale(int r) const { return __uint_as_float(r & 1 ? s[r >> 1] & 0xFFFF0000u : s[r >> 1] << 16); }
+  // what the operands' offset and the zero point take off the product: the accumulators of a group begin at minus this times the sum of x
+  __device__ __forceinline__ f32x4_t offset(float sum) const {
+    if constexpr (!ZEROS) return f32x4_t{-136.f * sum, -136.f * sum, -136.f * sum, -136.f * sum};
+    f32x4_t c;
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        const int k0 = (int)kb * 128 + (g * STEPS + s) * 32;
-        u32x4_t xv = {0u, 0u, 0u, 0u};
-        if (m < a.m && k0 < a.k) xv = *reinterpret_cast<const u32x4_t *>(x + k0);  // (k is a multiple of 32)
-        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_operand(w[g * STEPS + s]), as_bf16x8(xv), d, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(ones), as_bf16x8(xv), sum, 0, 0, 0);
+    for (int r = 0; r < 4; ++r) c[r] = -(128.f + (float)((z >> (8 * r)) & 0xFFu)) * sum;
+    return c;
+  }
+};
+
+// ---- up to 16 rows: a workgroup of eight wavefronts takes NB blocks of 16 outputs, each a share of the inputs ----
+template <int GROUP, bool ZEROS, int NB, int U>
+__global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Layout l, int splits) {
+  constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32;  // groups of a block of inputs, matrix instructions of a group
+  __shared__ f32x4_t sums[8][NB][64];
+  __shared__ unsigned flag;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
+  const int tile = blockIdx.x, split = blockIdx.y, m0 = blockIdx.z * 16;
+  const int64_t nb0 = (int64_t)tile * NB;
+  const int n_kb = (int)l.k_blocks;
+  const int share = split * 8 + wave, kb0 = (int)((int64_t)n_kb * share / (8 * splits)), kb1 = (int)((int64_t)n_kb * (share + 1) / (8 * splits));
+  const bool row = m0 + j < a.m;
+  const uint16_t *x = a.x + (m0 + (row ? j : 0)) * a.x_stride + 8 * g4;
+  f32x4_t y[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) y[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int kb = kb0; kb < kb1; kb += U) {
+    u32x4_t w[U][NB], xv[U][4];
+    Group<ZEROS> gr[U][NB][GPB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = min(kb + u, kb1 - 1);  // (past the end: the last block again, not used)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int64_t nb = min(nb0 + b, l.n_blocks - 1);
+        w[u][b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(a.weight + (nb * n_kb + k) * 1024 + lane * 16));
+#pragma unroll
+        for (int g = 0; g < GPB; ++g) gr[u][b][g].load(a, l, nb * l.groups + k * GPB + g, g4);
       }
-      const u32x2_t sc = *reinterpret_cast<const u32x2_t *>(a.weight + l.scales + at * 32 + 8 * g4);
-      const uint32_t z = ZEROS ? *reinterpret_cast<const uint32_t *>(a.weight + l.zeros + at * 16 + 4 * g4) : 0x08080808u;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float s = __uint_as_float(r & 1 ? sc[r >> 1] & 0xFFFF0000u : sc[r >> 1] << 16);
-        y[r] += s * (d[r] - (128.f + (float)((z >> (8 * r)) & 0xFFu)) * sum[r]);
+      for (int s = 0; s < 4; ++s) {
+        xv[u][s] = u32x4_t{0u, 0u, 0u, 0u};
+        if (row && k * 128 + 32 * s < a.k) xv[u][s] = *reinterpret_cast<const u32x4_t *>(x + k * 128 + 32 * s);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (kb + u >= kb1) break;
+#pragma unroll
+      for (int g = 0; g < GPB; ++g) {
+        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(ONES), as_bf16x8(xv[u][g * STEPS + s]), sum, 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          f32x4_t d = gr[u][b][g].offset(sum[0]);
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s)
+            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_operand(w[u][b][g * STEPS + s]), as_bf16x8(xv[u][g * STEPS + s]), d, 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[b][r] = __builtin_fmaf(gr[u][b][g].scale(r), d[r], y[b][r]);
+        }
       }
     }
   }
-  if (m >= a.m) return;
-  const int64_t n0 = nb * 16 + 4 * g4;
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (n0 + r < a.n) a.y[m * a.y_stride + n0 + r] = (uint16_t)pack_bf16x2(y[r], 0.f);
+  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = y[b];
+  __syncthreads();
+  // wavefront b adds up block b
+  const bool mine = wave < NB;
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (mine)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += sums[i][wave][lane];
+  if (splits > 1) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(a.ws, 0, 0x7fffffff, 0x00020000);
+    const int cell = blockIdx.z * gridDim.x + tile;
+    const unsigned at = (unsigned)(((cell * splits) * NB + wave) * 64 + lane) * 16u, step = NB * 64 * 16u;
+    if (mine) put_part(rs, at + split * step, v);
+    if (!last_of(a.counters + cell, splits, &flag)) return;
+    if (mine) {
+      v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < splits; ++i) v += get_part(rs, at + i * step);
+    }
+  }
+  if (mine) store_four(a, m0 + j, (int)(nb0 + wave) * 16 + 4 * g4, v, wide_rows(a));
+}
+
+// ---- 17 to 64 rows: a workgroup of four wavefronts takes 16 * MB rows and 64 * NB outputs, NB blocks each wavefront ----
+// x travels to LDS as matrix operands (a wavefront's load of 1 KB is one operand of 16 rows by 32 inputs), in a ring of RING
+// blocks of 128 inputs that all four wavefronts read; weights go straight to registers, AHEAD blocks before they are used.
+constexpr int W4_RING = 4;
+
+__device__ __forceinline__ void x_to_lds(const void *src, unsigned char *lds) {
+  __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+}
+
+template <int GROUP, bool ZEROS, int MB, int NB>
+__global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4Layout l, int splits) {
+  constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32, BLK = 4 * MB * 1024;
+  // (dynamic: the compiler would let every read of a ring that it knows wait for all that is on the way to it)
+  extern __shared__ __align__(16) unsigned char ring[];
+  unsigned *flag = reinterpret_cast<unsigned *>(ring);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
+  const int tile = blockIdx.x, split = blockIdx.y, m0 = blockIdx.z * 64;
+  const int64_t nb0 = ((int64_t)tile * 4 + wave) * NB;
+  const int n_kb = (int)l.k_blocks, kb0 = (int)((int64_t)n_kb * split / splits), kb1 = (int)((int64_t)n_kb * (split + 1) / splits);
+  const uint16_t *x[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) x[i] = a.x + min(m0 + 16 * i + j, a.m - 1) * a.x_stride + 8 * g4;  // (rows past the last repeat it)
+  // wavefront w brings step w of a block (past the inputs: the last step again, under scales of zero)
+  auto request = [&](int kb) __attribute__((always_inline)) {
+    const int k0 = min(min(kb, kb1 - 1) * 128 + 32 * wave, a.k - 32);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) x_to_lds(x[i] + k0, ring + (kb % W4_RING) * BLK + (wave * MB + i) * 1024);
+  };
+  const unsigned char *wp[NB];
+  int64_t gp[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int64_t nb = min(nb0 + b, l.n_blocks - 1);
+    wp[b] = a.weight + nb * n_kb * 1024 + lane * 16;
+    gp[b] = nb * l.groups;
+  }
+  struct Block {
+    u32x4_t w[NB];
+    Group<ZEROS> g[NB][GPB];
+  };
+  auto load = [&](int kb, Block &f) __attribute__((always_inline)) {
+    const int k = min(kb, kb1 - 1);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      f.w[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(wp[b] + (int64_t)k * 1024));
+#pragma unroll
+      for (int g = 0; g < GPB; ++g) f.g[b][g].load(a, l, gp[b] + k * GPB + g, g4);
+    }
+  };
+  f32x4_t y[NB][MB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < MB; ++i) y[b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  auto compute = [&](int kb, Block &f) __attribute__((always_inline)) {
+    // scales are unpacked here, and not where they are loaded (which would wait for them there)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int g = 0; g < GPB; ++g) f.g[b][g].here();
+    const unsigned char *blk = ring + (kb % W4_RING) * BLK + lane * 16;
+#pragma unroll
+    for (int g = 0; g < GPB; ++g) {
+      bf16x8_t xv[STEPS][MB];
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) xv[s][i] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(blk + ((g * STEPS + s) * MB + i) * 1024));
+      f32x4_t sum[MB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        sum[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(ONES), xv[s][i], sum[i], 0, 0, 0);
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        f32x4_t d[MB];
+#pragma unroll
+        for (int i = 0; i < MB; ++i) d[i] = f.g[b][g].offset(sum[i][0]);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          const bf16x8_t w = as_operand(f.w[b][g * STEPS + s]);
+#pragma unroll
+          for (int i = 0; i < MB; ++i) d[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xv[s][i], d[i], 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[b][i][r] = __builtin_fmaf(f.g[b][g].scale(r), d[i][r], y[b][i][r]);
+      }
+    }
+  };
+  // Block kb: behind the barrier its x has landed for everybody, and the slot of block kb - 1 is free for kb + 3.  What may be
+  // in flight still: x of kb + 2 and weights of kb + 1, asked for behind the weights of kb.
+  constexpr int IN_FLIGHT = MB + NB * (1 + GPB * (ZEROS ? 2 : 1));
+  static_assert(IN_FLIGHT < 64, "the counter's range");
+  auto step = [&](int kb, Block &f) __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((IN_FLIGHT & 0xF) | ((IN_FLIGHT >> 4) << 14) | 0xF70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    request(kb + W4_RING - 1);
+    compute(kb, f);
+    __builtin_amdgcn_sched_barrier(0);
+    load(kb + 2, f);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int i = 0; i < W4_RING - 1; ++i) request(kb0 + i);
+  Block fa, fb;
+  load(kb0, fa);
+  load(kb0 + 1, fb);
+  int kb = kb0;
+  for (; kb + 1 < kb1; kb += 2) {
+    step(kb, fa);
+    step(kb + 1, fb);
+  }
+  if (kb < kb1) step(kb, fa);
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // the look-ahead has landed before the LDS is released
+  if (splits > 1) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(a.ws, 0, 0x7fffffff, 0x00020000);
+    const int cell = blockIdx.z * gridDim.x + tile;
+    const unsigned step_bytes = NB * MB * 256 * 16u, at = (unsigned)(cell * splits) * step_bytes + threadIdx.x * 16u;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < MB; ++i) put_part(rs, at + split * step_bytes + (b * MB + i) * 4096u, y[b][i]);
+    if (!last_of(a.counters + cell, splits, flag)) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < MB; ++i) y[b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < splits; ++p) {
+      f32x4_t v[NB][MB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) v[b][i] = get_part(rs, at + p * step_bytes + (b * MB + i) * 4096u);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) y[b][i] += v[b][i];
+    }
+  }
+  const bool wide = wide_rows(a);
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < MB; ++i) store_four(a, m0 + 16 * i + j, (int)(nb0 + b) * 16 + 4 * g4, y[b][i], wide);
 }
 
 // One 32-bit word of a block per thread, then a scale (and zero point) per thread.
@@ -88,12 +342,45 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *packed, con
   if (zeros) weight[l.zeros + e] = in ? zeros[row * (k / group) + g] : (unsigned char)0;
 }
 
-template <int GROUP>
-hipError_t launch_group(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  const dim3 grid((unsigned)l.n_blocks, (unsigned)((a.m + 15) / 16));
-  if (a.with_zeros) hipLaunchKernelGGL((w4_kernel<GROUP, true>), grid, dim3(64), 0, stream, a, l);
-  else hipLaunchKernelGGL((w4_kernel<GROUP, false>), grid, dim3(64), 0, stream, a, l);
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// splits of the inputs, within the workspace and the counters
+int within(const W4Args &a, int want, int cells, int floats_per_part) {
+  if (cells > a.n_counters) return 1;
+  return std::max(1, (int)std::min<int64_t>(want, (int64_t)(a.ws_floats / ((size_t)cells * floats_per_part))));
+}
+
+template <int GROUP, bool ZEROS, int NB, int U>
+hipError_t launch_few(const W4Args &a, const W4Layout &l, hipStream_t stream) {
+  const int tiles = ceil_div(l.n_blocks, NB), z = ceil_div(a.m, 16);
+  const int splits = within(a, std::min<int>(ceil_div(a.n_cu, tiles), (int)l.k_blocks / 16), tiles * z, NB * 256);
+  hipLaunchKernelGGL((w4_few_kernel<GROUP, ZEROS, NB, U>), dim3(tiles, splits, z), dim3(512), 0, stream, a, l, splits);
   return hipGetLastError();
+}
+
+template <int GROUP, bool ZEROS, int MB, int NB>
+hipError_t launch_tile(const W4Args &a, const W4Layout &l, hipStream_t stream) {
+  const int tiles = ceil_div(l.n_blocks, 4 * NB), z = ceil_div(a.m, 64);
+  const int splits = within(a, std::min<int>(ceil_div(a.n_cu, tiles), (int)l.k_blocks / 4), tiles * z, NB * MB * 1024);
+  hipLaunchKernelGGL((w4_tile_kernel<GROUP, ZEROS, MB, NB>), dim3(tiles, splits, z), dim3(256), W4_RING * 4 * MB * 1024, stream, a, l, splits);
+  return hipGetLastError();
+}
+
+template <int GROUP, bool ZEROS>
+hipError_t launch_group(const W4Args &a, const W4Layout &l, hipStream_t stream) {
+  if (a.m <= 16 || a.k < 32) {
+    if (l.n_blocks >= 4 * a.n_cu) return launch_few<GROUP, ZEROS, 4, 2>(a, l, stream);
+    if (l.n_blocks >= 2 * a.n_cu) return launch_few<GROUP, ZEROS, 2, 2>(a, l, stream);
+    return launch_few<GROUP, ZEROS, 1, 4>(a, l, stream);
+  }
+  if (a.m <= 32) return launch_tile<GROUP, ZEROS, 2, 4>(a, l, stream);
+  if (a.m <= 48) return launch_tile<GROUP, ZEROS, 3, 4>(a, l, stream);
+  return launch_tile<GROUP, ZEROS, 4, 4>(a, l, stream);
+}
+
+template <int GROUP>
+hipError_t launch_zeros(const W4Args &a, const W4Layout &l, hipStream_t stream) {
+  return a.with_zeros ? launch_group<GROUP, true>(a, l, stream) : launch_group<GROUP, false>(a, l, stream);
 }
 
 }  // namespace
@@ -101,9 +388,9 @@ hipError_t launch_group(const W4Args &a, const W4Layout &l, hipStream_t stream) 
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t stream) {
   if (a.m <= 0 || a.n <= 0) return hipSuccess;
   const W4Layout l = w4_layout(a.n, a.k, a.group, a.with_zeros);
-  if (a.group == 32) return launch_group<32>(a, l, stream);
-  if (a.group == 64) return launch_group<64>(a, l, stream);
-  if (a.group == 128) return launch_group<128>(a, l, stream);
+  if (a.group == 32) return launch_zeros<32>(a, l, stream);
+  if (a.group == 64) return launch_zeros<64>(a, l, stream);
+  if (a.group == 128) return launch_zeros<128>(a, l, stream);
   return hipErrorInvalidValue;
 }
 
@@ -158,7 +445,7 @@ int bs_w4_linear(bs_ctx *c, const void *x, int64_t x_stride, const void *weight,
   return ctx_guarded(c, [&]() -> int {
     const CtxView v = ctx_view(c);
     if (v.device == BS_DEVICE_NONE) return ctx_fail(c, BS_EINVAL, "host-only context");
-    if (!shape_ok(n, k, group) || m < 0 || m > 65535 * 16)
+    if (!shape_ok(n, k, group) || m < 0 || m > 65535 * 64)
       return ctx_fail(c, BS_EUNSUPPORTED, "bs_w4_linear: m=%lld n=%lld k=%lld group=%d (group 32, 64 or 128 and a divisor of k)", (long long)m, (long long)n, (long long)k, group);
     if (m == 0 || n == 0) return BS_OK;
     if (!y || (k > 0 && (!x || !weight))) return ctx_fail(c, BS_EINVAL, "bs_w4_linear: NULL pointer");
@@ -170,6 +457,7 @@ int bs_w4_linear(bs_ctx *c, const void *x, int64_t x_stride, const void *weight,
     a.x = (const uint16_t *)x; a.weight = (const unsigned char *)weight; a.y = (uint16_t *)y;
     a.x_stride = x_stride; a.y_stride = y_stride;
     a.m = (int)m; a.n = (int)n; a.k = (int)k; a.group = group; a.with_zeros = with_zeros != 0;
+    a.ws = v.ws; a.counters = v.counters; a.ws_floats = v.ws_floats; a.n_counters = v.n_counters; a.n_cu = v.n_cu;
     CTX_HIP_TRY(c, launch_w4_linear(a, (hipStream_t)stream));
     return BS_OK;
   });

@@ -34,6 +34,11 @@ struct W4Args {
   int64_t x_stride, y_stride;
   int m, n, k, group;
   bool with_zeros;
+  // partial sums of workgroups that share outputs, and their arrival counters (zero between launches)
+  float *ws;
+  unsigned *counters;
+  size_t ws_floats;
+  int n_counters, n_cu;
 };
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t stream);
 hipError_t launch_w4_pack(const uint8_t *packed, const uint16_t *scales, const uint8_t *zeros, int64_t n, int64_t k, int group,
