@@ -19,13 +19,23 @@ using namespace bs;
 namespace bs {
 namespace {
 
-__device__ __forceinline__ bf16x8_t as_operand(uint32_t w) {
-  constexpr uint32_t MASK = 0x000F000Fu, BASE = 0x43004300u;
-  const u32x4_t v = {(w & MASK) | BASE, ((w >> 4) & MASK) | BASE, ((w >> 8) & MASK) | BASE, ((w >> 12) & MASK) | BASE};
-  return as_bf16x8(v);
-}
+// The constants live in registers: as literals they would keep the and and the or apart.
+struct Unpack {
+  uint32_t mask = 0x000F000Fu, base = 0x43004300u;
+  __device__ __forceinline__ Unpack() { asm volatile("" : "+s"(mask), "+v"(base)); }
+  __device__ __forceinline__ bf16x8_t operator()(uint32_t w) const {
+    const u32x4_t v = {(w & mask) | base, ((w >> 4) & mask) | base, ((w >> 8) & mask) | base, ((w >> 12) & mask) | base};
+    return as_bf16x8(v);
+  }
+};
 
-constexpr u32x4_t ONES = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+// The operand whose product with x is the sum of x (ZEROS) or what the offset of the operands and the zero point 8 take off: -136
+// times it (136 is a bf16 number), in all four accumulators of a lane.
+template <bool ZEROS>
+__device__ __forceinline__ bf16x8_t sum_operand() {
+  constexpr uint32_t V = ZEROS ? 0x3F803F80u : 0xC308C308u;
+  return as_bf16x8(u32x4_t{V, V, V, V});
+}
 
 // 16-byte accesses that all XCDs agree on (their L2 caches are their own): partial sums travel past those
 constexpr int SC1 = 16;
@@ -47,6 +57,15 @@ __device__ __forceinline__ bool last_of(unsigned *counter, unsigned parts, unsig
   if (*flag + 1u != parts) return false;
   if (threadIdx.x == 0) atomicExch(counter, 0u);
   return true;
+}
+
+// Which outputs, inputs and rows a workgroup takes.
+struct Place {
+  int split, tile, z, cell;
+};
+__device__ __forceinline__ Place place(int splits, int tiles) {
+  const int tile = (int)blockIdx.x % tiles, rest = (int)blockIdx.x / tiles, z = rest / splits;
+  return {rest % splits, tile, z, z * tiles + tile};
 }
 
 // four outputs n0 .. n0 + 3 of row m
@@ -77,112 +96,136 @@ struct Group {
     if constexpr (ZEROS) asm volatile("" : "+v"(z));
   }
   __device__ __forceinline__ float scale(int r) const { return __uint_as_float(r & 1 ? s[r >> 1] & 0xFFFF0000u : s[r >> 1] << 16); }
-  // what the operands' offset and the zero point take off the product: the accumulators of a group begin at minus this times the sum of x
-  __device__ __forceinline__ f32x4_t offset(float sum) const {
-    if constexpr (!ZEROS) return f32x4_t{-136.f * sum, -136.f * sum, -136.f * sum, -136.f * sum};
+  // where the accumulators of a group begin, from the product with sum_operand
+  __device__ __forceinline__ f32x4_t first(f32x4_t sum) const {
+    if constexpr (!ZEROS) return sum;
     f32x4_t c;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] = -(128.f + (float)((z >> (8 * r)) & 0xFFu)) * sum;
+    for (int r = 0; r < 4; ++r) c[r] = -(128.f + (float)((z >> (8 * r)) & 0xFFu)) * sum[r];
     return c;
   }
 };
 
-// ---- up to 16 rows: a workgroup of eight wavefronts takes NB blocks of 16 outputs, each a share of the inputs ----
-template <int GROUP, bool ZEROS, int NB, int U>
-__global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Layout l, int splits) {
-  constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32;  // groups of a block of inputs, matrix instructions of a group
-  __shared__ f32x4_t sums[8][NB][64];
-  __shared__ unsigned flag;
+// ---- up to 8 rows: a workgroup of eight wavefronts, 8 / KW of them blocks of 16 outputs, KW a share each of the inputs ----
+// x of the workgroup's inputs lies in LDS, so that the vector memory path carries weights alone and wavefronts do not wait for each
+// other behind the first barrier; a wavefront has U blocks of weights in use and U on the way.
+template <int GROUP, bool ZEROS, int KW, int U>
+__global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Layout l, int splits, int tiles, int x_row) {
+  constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32, NW = 8 / KW;  // groups of a block of inputs, matrix instructions of a group
+  extern __shared__ __align__(16) unsigned char lds[];
+  uint16_t *xs = reinterpret_cast<uint16_t *>(lds);  // [rows][x_row]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
-  const int tile = blockIdx.x, split = blockIdx.y, m0 = blockIdx.z * 16;
-  const int64_t nb0 = (int64_t)tile * NB;
-  const int n_kb = (int)l.k_blocks;
-  const int share = split * 8 + wave, kb0 = (int)((int64_t)n_kb * share / (8 * splits)), kb1 = (int)((int64_t)n_kb * (share + 1) / (8 * splits));
-  const bool row = m0 + j < a.m;
-  const uint16_t *x = a.x + (m0 + (row ? j : 0)) * a.x_stride + 8 * g4;
-  f32x4_t y[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) y[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int kb = kb0; kb < kb1; kb += U) {
-    u32x4_t w[U][NB], xv[U][4];
-    Group<ZEROS> gr[U][NB][GPB];
+  const Place at = place(splits, tiles);
+  const int tile = at.tile, split = at.split, rows = a.m;
+  const int64_t block = (int64_t)tile * NW + wave / KW, nb = min(block, l.n_blocks - 1);
+  const int n_kb = (int)l.k_blocks, first = (int)((int64_t)n_kb * split / splits), n_mine = (int)((int64_t)n_kb * (split + 1) / splits) - first;
+  const int kb0 = first + n_mine * (wave % KW) / KW, kb1 = first + n_mine * (wave % KW + 1) / KW;
+  struct Blocks {
+    u32x4_t w[U];
+    Group<ZEROS> g[U][GPB];
+  };
+  const unsigned char *wp = a.weight + nb * n_kb * 1024 + lane * 16;
+  auto load = [&](int kb, Blocks &f) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int k = min(kb + u, kb1 - 1);  // (past the end: the last block again, not used)
+      const int k = max(min(kb + u, kb1 - 1), 0);  // (past the end: the last block again, not used)
+      f.w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(wp + (int64_t)k * 1024));
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int64_t nb = min(nb0 + b, l.n_blocks - 1);
-        w[u][b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(a.weight + (nb * n_kb + k) * 1024 + lane * 16));
-#pragma unroll
-        for (int g = 0; g < GPB; ++g) gr[u][b][g].load(a, l, nb * l.groups + k * GPB + g, g4);
-      }
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        xv[u][s] = u32x4_t{0u, 0u, 0u, 0u};
-        if (row && k * 128 + 32 * s < a.k) xv[u][s] = *reinterpret_cast<const u32x4_t *>(x + k * 128 + 32 * s);
-      }
+      for (int g = 0; g < GPB; ++g) f.g[u][g].load(a, l, nb * l.groups + k * GPB + g, g4);
     }
-    __builtin_amdgcn_sched_barrier(0);
+  };
+  Blocks fa, fb;
+  load(kb0, fa);
+  load(kb0 + U, fb);
+  __builtin_amdgcn_sched_barrier(0);
+  {  // inputs [128 first, 128 (first + n_mine)) of the rows; zeros past the last
+    const int per_row = n_mine * 16;
+    for (int i = threadIdx.x; i < rows * per_row; i += 512) {
+      const int r = i / per_row, c = i % per_row, k = first * 128 + c * 8;
+      u32x4_t v = {0u, 0u, 0u, 0u};
+      if (k < a.k) v = *reinterpret_cast<const u32x4_t *>(a.x + r * a.x_stride + k);
+      *reinterpret_cast<u32x4_t *>(xs + r * x_row + c * 8) = v;
+    }
+  }
+  __syncthreads();
+  const Unpack unpack;
+  const bf16x8_t summing = sum_operand<ZEROS>();
+  const uint16_t *x = xs + min(j, rows - 1) * x_row + 8 * g4 - first * 128;
+  f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+  auto compute = [&](int kb, Blocks &f) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (kb + u >= kb1) break;
+      if (kb + u >= kb1) break;  // wave-uniform
+#pragma unroll
+      for (int g = 0; g < GPB; ++g) f.g[u][g].here();
+      bf16x8_t xv[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) xv[s] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(x + (kb + u) * 128 + 32 * s));
 #pragma unroll
       for (int g = 0; g < GPB; ++g) {
-        f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+        f32x4_t d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(ONES), as_bf16x8(xv[u][g * STEPS + s]), sum, 0, 0, 0);
+        for (int s = 0; s < STEPS; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(summing, xv[g * STEPS + s], d, 0, 0, 0);
+        d = f.g[u][g].first(d);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          f32x4_t d = gr[u][b][g].offset(sum[0]);
+        for (int s = 0; s < STEPS; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack(f.w[u][g * STEPS + s]), xv[g * STEPS + s], d, 0, 0, 0);
 #pragma unroll
-          for (int s = 0; s < STEPS; ++s)
-            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_operand(w[u][b][g * STEPS + s]), as_bf16x8(xv[u][g * STEPS + s]), d, 0, 0, 0);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) y[b][r] = __builtin_fmaf(gr[u][b][g].scale(r), d[r], y[b][r]);
-        }
+        for (int r = 0; r < 4; ++r) y[r] = __builtin_fmaf(f.g[u][g].scale(r), d[r], y[r]);
       }
     }
+  };
+  for (int kb = kb0; kb < kb1; kb += 2 * U) {
+    compute(kb, fa);
+    __builtin_amdgcn_sched_barrier(0);
+    load(kb + 2 * U, fa);
+    __builtin_amdgcn_sched_barrier(0);
+    compute(kb + U, fb);
+    __builtin_amdgcn_sched_barrier(0);
+    load(kb + 3 * U, fb);
+    __builtin_amdgcn_sched_barrier(0);
   }
+  bool mine = block < l.n_blocks;
+  if constexpr (KW > 1) {  // the first wavefront of each block adds up its shares
+    __syncthreads();
+    f32x4_t *sums = reinterpret_cast<f32x4_t *>(lds);
+    sums[threadIdx.x] = y;
+    __syncthreads();
+    mine = mine && wave % KW == 0;
+    if (mine)
 #pragma unroll
-  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = y[b];
-  __syncthreads();
-  // wavefront b adds up block b
-  const bool mine = wave < NB;
-  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-  if (mine)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v += sums[i][wave][lane];
+      for (int i = 1; i < KW; ++i) y += sums[threadIdx.x + 64 * i];
+  }
   if (splits > 1) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(a.ws, 0, 0x7fffffff, 0x00020000);
-    const int cell = blockIdx.z * gridDim.x + tile;
-    const unsigned at = (unsigned)(((cell * splits) * NB + wave) * 64 + lane) * 16u, step = NB * 64 * 16u;
-    if (mine) put_part(rs, at + split * step, v);
-    if (!last_of(a.counters + cell, splits, &flag)) return;
+    const unsigned part = (unsigned)((at.cell * splits * NW + wave / KW) * 64 + lane) * 16u, step = NW * 64 * 16u;
+    if (mine) put_part(rs, part + split * step, y);
+    if (!last_of(a.counters + at.cell, splits, reinterpret_cast<unsigned *>(lds + 512 * 16))) return;
     if (mine) {
-      v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      for (int i = 0; i < splits; ++i) v += get_part(rs, at + i * step);
+      y = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < splits; ++i) y += get_part(rs, part + i * step);
     }
   }
-  if (mine) store_four(a, m0 + j, (int)(nb0 + wave) * 16 + 4 * g4, v, wide_rows(a));
+  if (mine) store_four(a, j, (int)block * 16 + 4 * g4, y, wide_rows(a));
 }
 
-// ---- 17 to 64 rows: a workgroup of four wavefronts takes 16 * MB rows and 64 * NB outputs, NB blocks each wavefront ----
+// ---- up to 64 rows: a workgroup of four wavefronts takes 16 * MB rows and 128 outputs, two blocks of 16 each wavefront ----
 // x travels to LDS as matrix operands (a wavefront's load of 1 KB is one operand of 16 rows by 32 inputs), in a ring of RING
-// blocks of 128 inputs that all four wavefronts read; weights go straight to registers, AHEAD blocks before they are used.
-constexpr int W4_RING = 4;
+// blocks of 128 inputs that all four wavefronts read; weights go straight to registers, two blocks before they are used.
+constexpr int TILE_RING = 4, TILE_NB = 2;
 
 __device__ __forceinline__ void x_to_lds(const void *src, unsigned char *lds) {
   __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
 }
 
-template <int GROUP, bool ZEROS, int MB, int NB>
-__global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4Layout l, int splits) {
-  constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32, BLK = 4 * MB * 1024;
+template <int GROUP, bool ZEROS, int MB>
+__global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W4Layout l, int splits, int tiles) {
+  constexpr int NB = TILE_NB, GPB = 128 / GROUP, STEPS = GROUP / 32, BLK = 4 * MB * 1024;
   // (dynamic: the compiler would let every read of a ring that it knows wait for all that is on the way to it)
   extern __shared__ __align__(16) unsigned char ring[];
   unsigned *flag = reinterpret_cast<unsigned *>(ring);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
-  const int tile = blockIdx.x, split = blockIdx.y, m0 = blockIdx.z * 64;
+  const Place at = place(splits, tiles);
+  const int tile = at.tile, split = at.split, m0 = at.z * 64;
   const int64_t nb0 = ((int64_t)tile * 4 + wave) * NB;
   const int n_kb = (int)l.k_blocks, kb0 = (int)((int64_t)n_kb * split / splits), kb1 = (int)((int64_t)n_kb * (split + 1) / splits);
   const uint16_t *x[MB];
@@ -192,7 +235,7 @@ __global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4La
   auto request = [&](int kb) __attribute__((always_inline)) {
     const int k0 = min(min(kb, kb1 - 1) * 128 + 32 * wave, a.k - 32);
 #pragma unroll
-    for (int i = 0; i < MB; ++i) x_to_lds(x[i] + k0, ring + (kb % W4_RING) * BLK + (wave * MB + i) * 1024);
+    for (int i = 0; i < MB; ++i) x_to_lds(x[i] + k0, ring + (kb % TILE_RING) * BLK + (wave * MB + i) * 1024);
   };
   const unsigned char *wp[NB];
   int64_t gp[NB];
@@ -220,13 +263,15 @@ __global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4La
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int i = 0; i < MB; ++i) y[b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const Unpack unpack;
+  const bf16x8_t summing = sum_operand<ZEROS>();
   auto compute = [&](int kb, Block &f) __attribute__((always_inline)) {
     // scales are unpacked here, and not where they are loaded (which would wait for them there)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int g = 0; g < GPB; ++g) f.g[b][g].here();
-    const unsigned char *blk = ring + (kb % W4_RING) * BLK + lane * 16;
+    const unsigned char *blk = ring + (kb % TILE_RING) * BLK + lane * 16;
 #pragma unroll
     for (int g = 0; g < GPB; ++g) {
       bf16x8_t xv[STEPS][MB];
@@ -236,19 +281,19 @@ __global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4La
         for (int i = 0; i < MB; ++i) xv[s][i] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(blk + ((g * STEPS + s) * MB + i) * 1024));
       f32x4_t sum[MB];
 #pragma unroll
-      for (int i = 0; i < MB; ++i) {
-        sum[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < MB; ++i) sum[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(ONES), xv[s][i], sum[i], 0, 0, 0);
-      }
+      for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(summing, xv[s][i], sum[i], 0, 0, 0);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         f32x4_t d[MB];
 #pragma unroll
-        for (int i = 0; i < MB; ++i) d[i] = f.g[b][g].offset(sum[i][0]);
+        for (int i = 0; i < MB; ++i) d[i] = f.g[b][g].first(sum[i]);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-          const bf16x8_t w = as_operand(f.w[b][g * STEPS + s]);
+          const bf16x8_t w = unpack(f.w[b][g * STEPS + s]);
 #pragma unroll
           for (int i = 0; i < MB; ++i) d[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xv[s][i], d[i], 0, 0, 0);
         }
@@ -268,16 +313,23 @@ __global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4La
     __builtin_amdgcn_s_waitcnt((IN_FLIGHT & 0xF) | ((IN_FLIGHT >> 4) << 14) | 0xF70);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    request(kb + W4_RING - 1);
+    request(kb + TILE_RING - 1);
     compute(kb, f);
     __builtin_amdgcn_sched_barrier(0);
     load(kb + 2, f);
     __builtin_amdgcn_sched_barrier(0);
   };
-  for (int i = 0; i < W4_RING - 1; ++i) request(kb0 + i);
   Block fa, fb;
+  static_assert(TILE_RING == 4, "three blocks of x on the way, in the order that the steps leave them");
+  request(kb0);
+  request(kb0 + 1);
+  __builtin_amdgcn_sched_barrier(0);
   load(kb0, fa);
+  __builtin_amdgcn_sched_barrier(0);
+  request(kb0 + 2);
+  __builtin_amdgcn_sched_barrier(0);
   load(kb0 + 1, fb);
+  __builtin_amdgcn_sched_barrier(0);
   int kb = kb0;
   for (; kb + 1 < kb1; kb += 2) {
     step(kb, fa);
@@ -287,13 +339,12 @@ __global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4La
   __builtin_amdgcn_s_waitcnt(0x0F70);  // the look-ahead has landed before the LDS is released
   if (splits > 1) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(a.ws, 0, 0x7fffffff, 0x00020000);
-    const int cell = blockIdx.z * gridDim.x + tile;
-    const unsigned step_bytes = NB * MB * 256 * 16u, at = (unsigned)(cell * splits) * step_bytes + threadIdx.x * 16u;
+    const unsigned step_bytes = NB * MB * 256 * 16u, part = (unsigned)(at.cell * splits) * step_bytes + threadIdx.x * 16u;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < MB; ++i) put_part(rs, at + split * step_bytes + (b * MB + i) * 4096u, y[b][i]);
-    if (!last_of(a.counters + cell, splits, flag)) return;
+      for (int i = 0; i < MB; ++i) put_part(rs, part + split * step_bytes + (b * MB + i) * 4096u, y[b][i]);
+    if (!last_of(a.counters + at.cell, splits, flag)) return;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -303,7 +354,7 @@ __global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4La
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int i = 0; i < MB; ++i) v[b][i] = get_part(rs, at + p * step_bytes + (b * MB + i) * 4096u);
+        for (int i = 0; i < MB; ++i) v[b][i] = get_part(rs, part + p * step_bytes + (b * MB + i) * 4096u);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -315,6 +366,12 @@ __global__ __launch_bounds__(256) void w4_tile_kernel(const W4Args a, const W4La
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int i = 0; i < MB; ++i) store_four(a, m0 + 16 * i + j, (int)(nb0 + b) * 16 + 4 * g4, y[b][i], wide);
+}
+
+// products over no inputs
+__global__ __launch_bounds__(256) void w4_zero_kernel(const W4Args a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < (int64_t)a.m * a.n) a.y[i / a.n * a.y_stride + i % a.n] = 0;
 }
 
 // One 32-bit word of a block per thread, then a scale (and zero point) per thread.
@@ -345,37 +402,68 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *packed, con
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // splits of the inputs, within the workspace and the counters
-int within(const W4Args &a, int want, int cells, int floats_per_part) {
+int within(const W4Args &a, int want, int64_t cells, int floats_per_part) {
   if (cells > a.n_counters) return 1;
-  return std::max(1, (int)std::min<int64_t>(want, (int64_t)(a.ws_floats / ((size_t)cells * floats_per_part))));
+  return std::max(1, (int)std::min<int64_t>(want, (int64_t)a.ws_floats / (cells * floats_per_part)));
 }
 
-template <int GROUP, bool ZEROS, int NB, int U>
-hipError_t launch_few(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  const int tiles = ceil_div(l.n_blocks, NB), z = ceil_div(a.m, 16);
-  const int splits = within(a, std::min<int>(ceil_div(a.n_cu, tiles), (int)l.k_blocks / 16), tiles * z, NB * 256);
-  hipLaunchKernelGGL((w4_few_kernel<GROUP, ZEROS, NB, U>), dim3(tiles, splits, z), dim3(512), 0, stream, a, l, splits);
+constexpr int FEW_LDS = 128 * 1024;  // for x
+
+template <int GROUP, bool ZEROS, int KW, int U>
+hipError_t run_few(const W4Args &a, const W4Layout &l, int splits, hipStream_t stream) {
+  const int tiles = ceil_div(l.n_blocks, 8 / KW), rows = a.m;
+  const int x_row = ceil_div(l.k_blocks, splits) * 128 + 8, lds = std::max(rows * x_row * 2, 512 * 16 + 16);
+  static OncePerDevice once;
+  if (const hipError_t e = allow_lds(once, reinterpret_cast<const void *>(&w4_few_kernel<GROUP, ZEROS, KW, U>), 160 * 1024)) return e;
+  if (lds > 160 * 1024) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((w4_few_kernel<GROUP, ZEROS, KW, U>), dim3((unsigned)(tiles * splits)), dim3(512), lds, stream, a, l, splits, tiles, x_row);
   return hipGetLastError();
 }
 
-template <int GROUP, bool ZEROS, int MB, int NB>
+template <int GROUP, bool ZEROS, int MB>
+hipError_t run_tile(const W4Args &a, const W4Layout &l, int splits, hipStream_t stream) {
+  const int tiles = ceil_div(l.n_blocks, 4 * TILE_NB), z = ceil_div(a.m, 64);
+  hipLaunchKernelGGL((w4_tile_kernel<GROUP, ZEROS, MB>), dim3((unsigned)(tiles * splits * z)), dim3(256), TILE_RING * 4 * MB * 1024, stream, a, l, splits,
+                     tiles);
+  return hipGetLastError();
+}
+
+template <int GROUP, bool ZEROS, int MB>
 hipError_t launch_tile(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  const int tiles = ceil_div(l.n_blocks, 4 * NB), z = ceil_div(a.m, 64);
-  const int splits = within(a, std::min<int>(ceil_div(a.n_cu, tiles), (int)l.k_blocks / 4), tiles * z, NB * MB * 1024);
-  hipLaunchKernelGGL((w4_tile_kernel<GROUP, ZEROS, MB, NB>), dim3(tiles, splits, z), dim3(256), W4_RING * 4 * MB * 1024, stream, a, l, splits);
-  return hipGetLastError();
+  const int64_t cells = (int64_t)ceil_div(l.n_blocks, 4 * TILE_NB) * ceil_div(a.m, 64);
+  const int want = std::min(std::min(ceil_div(2 * a.n_cu, cells), 8), (int)l.k_blocks / 4);
+  return run_tile<GROUP, ZEROS, MB>(a, l, within(a, want, cells, TILE_NB * MB * 1024), stream);
+}
+
+// Few rows: how many wavefronts share the inputs of a block of outputs, and how many workgroups.  Timed on 9 shapes from 1536 x 2048 to
+// 57344 x 8192 with 1 to 16 rows, each with 1 to 8 wavefronts and 1 to 16 workgroups: one workgroup of eight where there are
+// few blocks (4096 x 4096, one row 5.0 us; two wavefronts and four workgroups 6.5), else two wavefronts, and workgroups for about 3840 wavefronts
+// in all (28672 x 4096, 4 rows 15.3 us, one wavefront 17.1, four 16.4; 10240 x 8192 on three workgroups 14.2, eight wavefronts 15.4).
+template <int GROUP, bool ZEROS>
+hipError_t launch_few(const W4Args &a, const W4Layout &l, hipStream_t stream) {
+  const int nb = (int)l.n_blocks, kb = (int)l.k_blocks;
+  const int kw = nb <= 256 || (a.m == 1 && nb < 1024) ? 8 : nb <= 448 ? 4 : 2;
+  const int want = std::min(((kw == 8 ? 2048 : 3840) + nb * kw / 2) / (nb * kw), kb / (kw == 8 ? 8 : 20));
+  const int most_kb = std::max(1, (FEW_LDS / a.m / 2 - 8) / 128), fit = ceil_div(kb, most_kb);  // so many that x fits
+  const int splits = within(a, std::max(std::max(want, fit), 1), ceil_div(nb, 8 / kw), 8 / kw * 256);
+  if (splits < fit) return launch_tile<GROUP, ZEROS, 1>(a, l, stream);
+  if (kw == 2) return run_few<GROUP, ZEROS, 2, 2>(a, l, splits, stream);
+  if (kw == 4) return run_few<GROUP, ZEROS, 4, 2>(a, l, splits, stream);
+  // (a block at a time where a wavefront has four at most: 6144 x 4096 6.0 us, two at a time 6.4)
+  if (kb <= 32 * splits) return run_few<GROUP, ZEROS, 8, 1>(a, l, splits, stream);
+  return run_few<GROUP, ZEROS, 8, 2>(a, l, splits, stream);
 }
 
 template <int GROUP, bool ZEROS>
 hipError_t launch_group(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  if (a.m <= 16 || a.k < 32) {
-    if (l.n_blocks >= 4 * a.n_cu) return launch_few<GROUP, ZEROS, 4, 2>(a, l, stream);
-    if (l.n_blocks >= 2 * a.n_cu) return launch_few<GROUP, ZEROS, 2, 2>(a, l, stream);
-    return launch_few<GROUP, ZEROS, 1, 4>(a, l, stream);
-  }
-  if (a.m <= 32) return launch_tile<GROUP, ZEROS, 2, 4>(a, l, stream);
-  if (a.m <= 48) return launch_tile<GROUP, ZEROS, 3, 4>(a, l, stream);
-  return launch_tile<GROUP, ZEROS, 4, 4>(a, l, stream);
+  // Beyond eight rows, three of large weights, a copy of x in every workgroup costs more than the tiles' ring: 8192 x 28672, 8 rows
+  // 28.9 us against 26.9, 57344 x 8192 64 against 49; 4096 x 4096 6.6 against 8.7.
+  const bool large = l.n_blocks * l.k_blocks >= 96 << 10;
+  if (a.m <= (large ? 3 : 8)) return launch_few<GROUP, ZEROS>(a, l, stream);
+  if (a.m <= 16) return launch_tile<GROUP, ZEROS, 1>(a, l, stream);
+  if (a.m <= 32) return launch_tile<GROUP, ZEROS, 2>(a, l, stream);
+  if (a.m <= 48) return launch_tile<GROUP, ZEROS, 3>(a, l, stream);
+  return launch_tile<GROUP, ZEROS, 4>(a, l, stream);
 }
 
 template <int GROUP>
@@ -388,6 +476,10 @@ hipError_t launch_zeros(const W4Args &a, const W4Layout &l, hipStream_t stream) 
 hipError_t launch_w4_linear(const W4Args &a, hipStream_t stream) {
   if (a.m <= 0 || a.n <= 0) return hipSuccess;
   const W4Layout l = w4_layout(a.n, a.k, a.group, a.with_zeros);
+  if (a.k == 0) {
+    hipLaunchKernelGGL(w4_zero_kernel, dim3((unsigned)(((int64_t)a.m * a.n + 255) / 256)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+  }
   if (a.group == 32) return launch_zeros<32>(a, l, stream);
   if (a.group == 64) return launch_zeros<64>(a, l, stream);
   if (a.group == 128) return launch_zeros<128>(a, l, stream);
