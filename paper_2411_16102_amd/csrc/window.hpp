@@ -32,12 +32,18 @@ struct WindowArgs {
 hipError_t launch_window_units(const WindowArgs &a, hipStream_t stream);
 hipError_t launch_window_join(const WindowArgs &a, hipStream_t stream);
 
+// Rows of one sequence whose keys and values go to one page, at most 16, or rows that append nothing (page -1).
+struct RopeItem {
+  int32_t row0, n_rows, page, slot0;
+};
+
 struct RopeArgs {
-  int n_rows, n_q_heads, n_kv_heads, head_dim;
+  int n_rows, n_items, n_q_heads, n_kv_heads, head_dim;
+  bool whole;                      // eight pairs from a multiple of eight on share an axis
+  const RopeItem *items;
   const float *cos, *sin;          // [max_positions][head_dim / 2]
   const int32_t *positions;        // [n_axes][n_rows]
   const int32_t *axis_of_pair;     // [head_dim / 2]
-  const int32_t *row_page, *row_slot;  // [n_rows]; page -1: the row appends nothing
   const uint16_t *qkv;
   uint16_t *q, *kv_pool;
   int64_t qkv_stride, q_stride;

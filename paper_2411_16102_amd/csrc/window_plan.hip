@@ -23,12 +23,12 @@ constexpr long STAGE_WORDS = 1 << 16;   // of the plan's pinned memory at first 
 
 // What the kernels of a planned step need to know beside the arrays on the device.
 struct Planned {
-  bool made = false, has_angles = false;
-  int n_rows = 0, n_items = 0, n_joins = 0, window = 1, sinks = 0;
+  bool made = false, has_angles = false, whole_axes = true;
+  int n_rows = 0, n_rope = 0, n_items = 0, n_joins = 0, window = 1, sinks = 0;
   int n_work = 0, n_cut = 0, wide_blocks = 0;   // wide work: workgroups per group of heads, blocks of rows that several share, all blocks
   int32_t longest = 0, split_rows = 0;
   long states = 0, cut_states = 0, pages = 0;
-  long off_items = 0, off_pages = 0, off_joins = 0, off_row_page = 0, off_row_slot = 0, off_positions = 0, off_axis = 0, words = 0;
+  long off_items = 0, off_pages = 0, off_joins = 0, off_rope = 0, off_positions = 0, off_axis = 0, words = 0;
   long off_work = 0, off_cut = 0, off_row_start = 0, off_kv_len = 0, off_page_start = 0, off_page_ids = 0;
   // partial states, in floats
   long at_m = 0, at_l = 0, at_cut_acc = 0, at_cut_m = 0, at_cut_l = 0, state_floats = 0;
@@ -47,6 +47,7 @@ struct bs_window {
   // host scratch reused across plans
   std::vector<int32_t> words, refs, item_pages, joins, cut, wide_start, wide_pages;
   std::vector<WindowItem> items;
+  std::vector<RopeItem> rope;
   struct Work { int blocks, seq, block, t0, t1, state; };
   std::vector<Work> work;
 };
@@ -212,6 +213,20 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r) {
   return BS_OK;
 }
 
+// Runs of rows whose keys and values go to one page.
+void plan_appends(bs_window *w, const bs_batch *b) {
+  w->rope.clear();
+  for (int s = 0; s < b->n_seq; ++s) {
+    const int r0 = b->row_start[s], rows = b->row_start[s + 1] - r0, first = b->kv_len[s] - rows;
+    for (int j = 0; j < rows;) {
+      const int at = first + j, n = std::min(rows - j, at < 0 ? std::min(PAGE, -at) : PAGE - at % PAGE);
+      w->rope.push_back({r0 + j, n, at < 0 ? -1 : b->page_ids[b->page_start[s] + at / PAGE], at < 0 ? 0 : at % PAGE});
+      j += n;
+    }
+  }
+  w->p.n_rope = (int)w->rope.size();
+}
+
 template <class T>
 int grow(bs_ctx *c, T **at, long *cap, long want, size_t each) {
   if (want <= *cap) return BS_OK;
@@ -317,8 +332,13 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     const auto fail_with = [&](int rc) { w->p = Planned(); return rc; };
     const Route route = route_of(g);
     if (const int rc = plan_work(w, b, route)) return fail_with(rc);
-    if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff) return fail_with(too_large(w));
+    plan_appends(w, b);
+    // (grids count units of a KV head, workgroups of some heads, and shares of the heads of a run)
+    if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff ||
+        (int64_t)p.n_rope * (g.n_kv_heads + 1) + 4096 > 0x7fffffff)
+      return fail_with(too_large(w));
 
+    for (int i = 0; n_axes > 0 && i < half; ++i) p.whole_axes = p.whole_axes && axis_of_pair[i] == axis_of_pair[i & ~7];
     const int axes = std::max(1, n_axes);
     const long n_item_pages = (long)w->item_pages.size(), n_wide_pages = (long)w->wide_pages.size();
     p.off_pages = 8L * p.n_items;
@@ -330,9 +350,8 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     p.off_kv_len = p.off_row_start + n_tab;
     p.off_page_start = p.off_kv_len + n_tab;
     p.off_page_ids = p.off_page_start + n_tab;
-    p.off_row_page = p.off_page_ids + n_wide_pages;
-    p.off_row_slot = p.off_row_page + rows;
-    p.off_axis = p.off_row_slot + rows;
+    p.off_rope = whole_units(p.off_page_ids + n_wide_pages);
+    p.off_axis = p.off_rope + 4L * p.n_rope;
     p.off_positions = p.off_axis + half;
     p.words = whole_units(p.off_positions + (long)axes * rows);
     std::vector<int32_t> &words = w->words;
@@ -355,20 +374,13 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
       if (n_wide_pages) std::memcpy(&words[p.off_page_ids], w->wide_pages.data(), sizeof(int32_t) * n_wide_pages);
     }
     if (p.n_joins) std::memcpy(&words[p.off_joins], w->joins.data(), sizeof(int32_t) * w->joins.size());
-    bool turned = true;
-    for (int s = 0; s < b->n_seq; ++s) {
+    if (p.n_rope) std::memcpy(&words[p.off_rope], w->rope.data(), sizeof(RopeItem) * p.n_rope);
+    p.has_angles = true;
+    for (int s = 0; n_axes == 0 && s < b->n_seq; ++s) {
       const int r0 = b->row_start[s], n = b->row_start[s + 1] - r0;
-      for (int j = 0; j < n; ++j) {
-        const int at = b->kv_len[s] - n + j;
-        words[p.off_row_page + r0 + j] = at < 0 ? -1 : b->page_ids[b->page_start[s] + at / PAGE];
-        words[p.off_row_slot + r0 + j] = at < 0 ? 0 : at % PAGE;
-        if (n_axes == 0) {
-          words[p.off_positions + r0 + j] = std::max(0, at);
-          turned = turned && at < g.max_positions;
-        }
-      }
+      if (n > 0 && b->kv_len[s] > g.max_positions) p.has_angles = false;
+      for (int j = 0; j < n; ++j) words[p.off_positions + r0 + j] = std::max(0, b->kv_len[s] - n + j);
     }
-    p.has_angles = turned;
     if (n_axes > 0) {
       std::memcpy(&words[p.off_positions], positions, sizeof(int32_t) * (size_t)n_axes * rows);
       std::memcpy(&words[p.off_axis], axis_of_pair, sizeof(int32_t) * half);
@@ -421,12 +433,12 @@ int bs_rope_append(bs_window *w, const void *qkv, int64_t qkv_stride, void *q, i
     if (q == qkv && q_stride != qkv_stride) return ctx_fail(c, BS_EINVAL, "bs_rope_append: in place, but with another stride");
     CTX_HIP_TRY(c, hipSetDevice(v.device));
     RopeArgs a{};
-    a.n_rows = p.n_rows; a.n_q_heads = g.n_q_heads; a.n_kv_heads = g.n_kv_heads; a.head_dim = g.head_dim;
+    a.n_rows = p.n_rows; a.n_items = p.n_rope; a.n_q_heads = g.n_q_heads; a.n_kv_heads = g.n_kv_heads; a.head_dim = g.head_dim;
     a.cos = v.rope_cos; a.sin = v.rope_sin;
     a.positions = w->d_words + p.off_positions;
     a.axis_of_pair = w->d_words + p.off_axis;
-    a.row_page = w->d_words + p.off_row_page;
-    a.row_slot = w->d_words + p.off_row_slot;
+    a.whole = p.whole_axes;
+    a.items = reinterpret_cast<const RopeItem *>(w->d_words + p.off_rope);
     a.qkv = (const uint16_t *)qkv; a.q = (uint16_t *)q; a.kv_pool = (uint16_t *)kv_pool;
     a.qkv_stride = qkv_stride; a.q_stride = q_stride;
     CTX_HIP_TRY(c, launch_rope_append(a, (hipStream_t)stream));
