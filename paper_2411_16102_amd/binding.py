@@ -191,16 +191,17 @@ def raw():
         lib.bs_pages_destroy.restype = None
         lib.bs_pages_last_error.argtypes = [_p]
         lib.bs_pages_last_error.restype = C.c_char_p
-        lib.bs_pages_open.argtypes = [_p, _i32, _i32p]
-        lib.bs_pages_fork.argtypes = [_p, _i32p, _i32, _i32, _i32p]
-        lib.bs_pages_extend.argtypes = [_p, _i32p, _i32p, _i32, _i32p, _i32p, _i32p]
-        lib.bs_pages_trim.argtypes = [_p, _i32p, _i32, _i32, _i32]
-        lib.bs_pages_free.argtypes = [_p, _i32p, _i32]
-        lib.bs_pages_compact.argtypes = [_p, _i32p, _i32p, _i32p, _i32p]
-        lib.bs_pages_tables.argtypes = [_p, _i32p, _i32, _i32p, _i32p, _i32p]
-        lib.bs_pages_stats.argtypes = [_p, _i32p, _i32p]
-        lib.bs_kv_copy_pages.argtypes = [_p, C.POINTER(_p), _i32, _i64, _i32p, _i32p, _i32, _p]
-        lib.bs_kv_compact.argtypes = [_p, C.POINTER(_p), _i32, _i64, _i32p, _i64, _i32p, _i32p, _p]
+        # (int32 arrays by address, see _Words)
+        lib.bs_pages_open.argtypes = [_p, _i32, _p]
+        lib.bs_pages_fork.argtypes = [_p, _p, _i32, _i32, _p]
+        lib.bs_pages_extend.argtypes = [_p, _p, _p, _i32, _p, _p, _p]
+        lib.bs_pages_trim.argtypes = [_p, _p, _i32, _i32, _i32]
+        lib.bs_pages_free.argtypes = [_p, _p, _i32]
+        lib.bs_pages_compact.argtypes = [_p, _p, _p, _p, _p]
+        lib.bs_pages_tables.argtypes = [_p, _p, _i32, _p, _p, _p]
+        lib.bs_pages_stats.argtypes = [_p, _p, _p]
+        lib.bs_kv_copy_pages.argtypes = [_p, _p, _i32, _i64, _p, _p, _i32, _p]
+        lib.bs_kv_compact.argtypes = [_p, _p, _i32, _i64, _p, _i64, _p, _p, _p]
         lib.bs_batch_free.argtypes = [C.POINTER(BatchOwned)]
         lib.bs_batch_free.restype = None
         _lib = lib
@@ -259,6 +260,10 @@ class Layer:
         if rc != 0:
             raise BlendStepError(rc, (self.lib.bs_last_error(None) or b"").decode())
         self.h = h
+        # of every call on streams
+        self._bf16_type = torch.bfloat16
+        self._q_width = shape.n_q_heads * shape.head_dim
+        self._page_elems = self.page_bytes() // 2
 
     def close(self):
         if getattr(self, "h", None):
@@ -463,9 +468,12 @@ class Layer:
 
     def window_attention(self, plan: "WindowPlan", q, kv_pool, out=None, stream=None):
         """Sliding-window attention with sinks of the plan's rows; q and out: [n_rows, Hq * dh] bf16, rows at any stride."""
+        width = self._q_width
+        self._check_rows(plan, q, width)
         if out is None:
-            out = self.torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        self._check_rows(plan, (q, out))
+            out = q.new_empty((plan.n_rows, width))
+        else:
+            self._check_rows(plan, out, width)
         self._check_pool(plan, kv_pool)
         self._check(self.lib.bs_window_attention(plan.h, q.data_ptr(), q.stride(0), out.data_ptr(), out.stride(0), kv_pool.data_ptr(),
                                                  self._raw_stream(stream)))
@@ -474,27 +482,25 @@ class Layer:
     def rope_append(self, plan: "WindowPlan", qkv, kv_pool, q=None, stream=None):
         """Turns queries and keys of fused rows [n_rows, (Hq + 2 Hkv) * dh] and appends keys and values to kv_pool; the
         turned queries [n_rows, Hq * dh] (q: where they go; qkv[:, :Hq * dh] for in place)."""
-        width = self.shape.n_q_heads * self.shape.head_dim
+        self._check_rows(plan, qkv, self.shape.n_qkv)
         if q is None:
-            q = self.torch.empty((plan.n_rows, width), dtype=qkv.dtype, device=qkv.device)
-        self._check_rows(plan, (q,))
-        self._check_rows(plan, (qkv,), width + 2 * self.shape.n_kv_heads * self.shape.head_dim)
+            q = qkv.new_empty((plan.n_rows, self._q_width))
+        else:
+            self._check_rows(plan, q, self._q_width)
         self._check_pool(plan, kv_pool)
         self._check(self.lib.bs_rope_append(plan.h, qkv.data_ptr(), qkv.stride(0), q.data_ptr(), q.stride(0), kv_pool.data_ptr(),
                                             self._raw_stream(stream)))
         return q
 
     def _raw_stream(self, stream):
-        return (stream if stream is not None else self.torch.cuda.current_stream(self.device)).cuda_stream
+        return _current_stream(self.device) if stream is None else stream.cuda_stream
 
-    def _check_rows(self, plan, tensors, width=None):
-        width = width if width is not None else self.shape.n_q_heads * self.shape.head_dim
-        for t in tensors:
-            if t.dtype != self.torch.bfloat16 or t.dim() != 2 or t.shape[0] != plan.n_rows or t.shape[1] != width or t.stride(1) != 1:
-                raise ValueError("expected bf16 rows [%d, %d], got %s %s" % (plan.n_rows, width, t.dtype, tuple(t.shape)))
+    def _check_rows(self, plan, t, width):
+        if t.dtype is not self._bf16_type or tuple(t.shape) != (plan.n_rows, width) or t.stride(1) != 1:
+            raise ValueError("expected bf16 rows [%d, %d], got %s %s" % (plan.n_rows, width, t.dtype, tuple(t.shape)))
 
     def _check_pool(self, plan, kv_pool):
-        if kv_pool.dtype != self.torch.bfloat16 or not kv_pool.is_contiguous() or kv_pool.numel() * 2 < plan.n_pages * self.page_bytes():
+        if kv_pool.dtype is not self._bf16_type or not kv_pool.is_contiguous() or kv_pool.numel() < plan.n_pages * self._page_elems:
             raise ValueError("the pool is smaller than the %d pages of the plan, or not contiguous bf16" % plan.n_pages)
 
     def w4_pack(self, packed, scales, zeros=None, stream=None):
@@ -517,11 +523,11 @@ class Layer:
 
     def w4_linear(self, x, weight: "W4Weight", out=None, stream=None):
         """x [m, k] bf16 times a laid-out 4-bit weight: [m, n] bf16."""
-        if x.dtype != self.torch.bfloat16 or x.dim() != 2 or x.shape[1] != weight.k or (x.stride(1) != 1 and x.numel()):
+        if x.dtype is not self._bf16_type or x.dim() != 2 or x.shape[1] != weight.k or (x.stride(1) != 1 and x.numel()):
             raise ValueError("w4_linear: bf16 rows of %d inputs, got %s %s" % (weight.k, x.dtype, tuple(x.shape)))
         m = x.shape[0]
         if out is None:
-            out = self.torch.empty((m, weight.n), dtype=x.dtype, device=x.device)
+            out = x.new_empty((m, weight.n))
         elif out.dtype != x.dtype or tuple(out.shape) != (m, weight.n) or out.stride(1) != 1:
             raise ValueError("w4_linear: out is not bf16 [%d, %d]" % (m, weight.n))
         self._check(self.lib.bs_w4_linear(self.h, x.data_ptr(), x.stride(0) if x.numel() else 0, weight.data.data_ptr(), m, weight.n, weight.k, weight.group,
@@ -529,33 +535,72 @@ class Layer:
         return out
 
     def _pools(self, pools):
-        """(addresses, how many, pages of each) of a tensor [n_pools, elements] or a list of flat pools."""
-        pools = [pools[i] for i in range(pools.shape[0])] if hasattr(pools, "shape") else list(pools)
-        size = self.page_bytes() // 2
+        """(array of addresses, pages of each) of a tensor [n_pools, elements] or a list of flat pools."""
+        size = self._page_elems
+        if hasattr(pools, "shape"):
+            if pools.dtype is not self._bf16_type or pools.dim() != 2 or not pools.is_contiguous() or pools.shape[1] % size:
+                raise ValueError("pools are contiguous bf16 [n_pools, elements], whole pages each")
+            n, elems = pools.shape
+            first = pools.data_ptr()
+            return np.arange(first, first + 2 * elems * n, 2 * elems, dtype=np.uint64)[:n] if elems else np.zeros(n, dtype=np.uint64), elems // size
+        pools = list(pools)
         for p in pools:
-            if p.dtype != self.torch.bfloat16 or not p.is_contiguous() or p.numel() != pools[0].numel() or p.numel() % size:
+            if p.dtype is not self._bf16_type or not p.is_contiguous() or p.numel() != pools[0].numel() or p.numel() % size:
                 raise ValueError("pools are contiguous bf16 tensors of one size, whole pages each")
-        return (C.c_void_p * len(pools))(*[p.data_ptr() for p in pools]), len(pools), pools[0].numel() // size if pools else 0
+        return np.array([p.data_ptr() for p in pools], dtype=np.uint64), pools[0].numel() // size if pools else 0
 
     def copy_pages(self, pools, src, dst, stream=None):
         """Page src[i] to page dst[i] in every pool (one per layer: a list, or a tensor [n_layers, elements])."""
-        at, n, n_pages = self._pools(pools)
+        at, n_pages = self._pools(pools)
         src, dst = _i32(src), _i32(dst)
         if src.shape != dst.shape:
             raise ValueError("copy_pages: %d sources, %d destinations" % (src.size, dst.size))
-        self._check(self.lib.bs_kv_copy_pages(self.h, at, n, n_pages, _ptr(src), _ptr(dst), src.size, self._raw_stream(stream)))
+        self._check(self.lib.bs_kv_copy_pages(self.h, _address(at), at.size, n_pages, _address(src), _address(dst), src.size, self._raw_stream(stream)))
 
     def compact_pages(self, pools, tables, stream=None):
         """Moves the pages that `tables` names to the front of every pool: (the tables with the new numbers, pages named)."""
-        at, n, n_pages = self._pools(pools)
+        at, n_pages = self._pools(pools)
         tables = _i32(tables)
-        out, live = np.empty_like(tables), C.c_int32()
-        self._check(self.lib.bs_kv_compact(self.h, at, n, n_pages, _ptr(tables), tables.size, _ptr(out), C.byref(live), self._raw_stream(stream)))
-        return out, live.value
+        out, live = np.empty_like(tables), np.zeros(1, dtype=np.int32)
+        self._check(self.lib.bs_kv_compact(self.h, _address(at), at.size, n_pages, _address(tables), tables.size, _address(out), _address(live),
+                                           self._raw_stream(stream)))
+        return out, int(live[0])
+
+
+def _address(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]
+
+
+class _Words:
+    """An int32 array that is kept for the arguments of calls, with its address at hand (taking an array's costs as much as a call)."""
+
+    def __init__(self):
+        self.a = np.zeros(64, dtype=np.int32)
+        self.at = _address(self.a)
+
+    def room(self, n: int) -> int:
+        if n > self.a.size:
+            self.a = np.zeros(2 * n, dtype=np.int32)
+            self.at = _address(self.a)
+        return self.at
+
+    def put(self, values):
+        """(address, how many) of a copy."""
+        v = np.asarray(values, dtype=np.int32)
+        at = self.room(v.size)
+        self.a[:v.size] = v.reshape(-1)
+        return at, v.size
 
 
 def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def _current_stream(device: int) -> int:
+    """The handle of PyTorch's current stream (without the Stream object where PyTorch hands it out so: a microsecond a call)."""
+    import torch
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(device) if get is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 @dataclass
@@ -626,6 +671,7 @@ class Pages:
         if rc != 0:
             raise BlendStepError(rc, (self.lib.bs_pages_last_error(None) or b"").decode())
         self.h = h
+        self._ids, self._out, self._src, self._dst, self._count = (_Words() for _ in range(5))
 
     def close(self):
         if getattr(self, "h", None):
@@ -644,39 +690,42 @@ class Pages:
 
     def open(self, n: int = 1) -> np.ndarray:
         """Ids of n new, empty sequences."""
-        ids = np.zeros(max(1, n), dtype=np.int32)
-        self._check(self.lib.bs_pages_open(self.h, n, _ptr(ids)))
-        return ids[:n]
+        out = self._out.room(n)
+        self._check(self.lib.bs_pages_open(self.h, n, out))
+        return self._out.a[:n].copy()
 
     def fork(self, parents, children: int = 1) -> np.ndarray:
         """Ids of `children` new sequences for each parent, which share its pages."""
-        parents = _i32(parents).reshape(-1)
-        out = np.zeros(max(1, parents.size * max(0, children)), dtype=np.int32)
-        self._check(self.lib.bs_pages_fork(self.h, _ptr(parents), parents.size, children, _ptr(out)))
-        return out[:parents.size * children]
+        at, n = self._ids.put(parents)
+        out = self._out.room(n * max(0, children))
+        self._check(self.lib.bs_pages_fork(self.h, at, n, children, out))
+        return self._out.a[:n * children].copy()
 
     def extend(self, ids, tokens):
         """Room for further tokens; (src, dst) of the pages to copy in every pool before they are written to."""
-        ids = _i32(ids).reshape(-1)
-        tokens = np.ascontiguousarray(np.broadcast_to(_i32(tokens), ids.shape))
-        src, dst, n = np.zeros(max(1, ids.size), dtype=np.int32), np.zeros(max(1, ids.size), dtype=np.int32), C.c_int32()
-        self._check(self.lib.bs_pages_extend(self.h, _ptr(ids), _ptr(tokens), ids.size, _ptr(src), _ptr(dst), C.byref(n)))
-        return src[:n.value], dst[:n.value]
+        at, n = self._ids.put(ids)
+        more = self._out.room(n)
+        self._out.a[:n] = tokens
+        src, dst = self._src.room(n), self._dst.room(n)
+        self._check(self.lib.bs_pages_extend(self.h, at, more, n, src, dst, self._count.at))
+        n = int(self._count.a[0])
+        return self._src.a[:n].copy(), self._dst.a[:n].copy()
 
     def trim(self, ids, window: int, sinks: int = 0):
-        ids = _i32(ids).reshape(-1)
-        self._check(self.lib.bs_pages_trim(self.h, _ptr(ids), ids.size, window, sinks))
+        """Gives up the pages that no later row sees; their entries in the tables become -1."""
+        at, n = self._ids.put(ids)
+        self._check(self.lib.bs_pages_trim(self.h, at, n, window, sinks))
 
     def free(self, ids):
-        ids = _i32(ids).reshape(-1)
-        self._check(self.lib.bs_pages_free(self.h, _ptr(ids), ids.size))
+        at, n = self._ids.put(ids)
+        self._check(self.lib.bs_pages_free(self.h, at, n))
 
     def compact(self):
         """(src, dst) of the moves, and the number of live pages."""
-        src, dst = np.zeros(max(1, self.n_pages), dtype=np.int32), np.zeros(max(1, self.n_pages), dtype=np.int32)
-        moves, live = C.c_int32(), C.c_int32()
-        self._check(self.lib.bs_pages_compact(self.h, _ptr(src), _ptr(dst), C.byref(moves), C.byref(live)))
-        return src[:moves.value], dst[:moves.value], live.value
+        src, dst = self._src.room(self.n_pages), self._dst.room(self.n_pages)
+        self._check(self.lib.bs_pages_compact(self.h, src, dst, self._count.at, self._count.at + 4))
+        n, live = int(self._count.a[0]), int(self._count.a[1])
+        return self._src.a[:n].copy(), self._dst.a[:n].copy(), live
 
     def lengths(self, ids) -> np.ndarray:
         return self._tables(ids, False)[0]
@@ -686,18 +735,18 @@ class Pages:
         return self._tables(ids, True)[1:]
 
     def _tables(self, ids, whole):
-        ids = _i32(ids).reshape(-1)
-        tokens, start = np.zeros(max(1, ids.size), dtype=np.int32), np.zeros(ids.size + 1, dtype=np.int32)
-        self._check(self.lib.bs_pages_tables(self.h, _ptr(ids), ids.size, _ptr(tokens), _ptr(start), None))
-        pages = np.zeros(max(1, int(start[-1])), dtype=np.int32)
+        at, n = self._ids.put(ids)
+        tokens, start = self._out.room(n), np.empty(n + 1, dtype=np.int32)
+        first = _address(start)
+        self._check(self.lib.bs_pages_tables(self.h, at, n, tokens, first, None))
+        pages = np.empty(int(start[-1]) if whole else 0, dtype=np.int32)
         if whole:
-            self._check(self.lib.bs_pages_tables(self.h, _ptr(ids), ids.size, _ptr(tokens), _ptr(start), _ptr(pages)))
-        return tokens[:ids.size], start, pages[:int(start[-1])]
+            self._check(self.lib.bs_pages_tables(self.h, at, n, tokens, first, _address(pages)))
+        return self._out.a[:n].copy(), start, pages
 
     def stats(self) -> dict:
-        free, live = C.c_int32(), C.c_int32()
-        self._check(self.lib.bs_pages_stats(self.h, C.byref(free), C.byref(live)))
-        return {"free": free.value, "sequences": live.value}
+        self._check(self.lib.bs_pages_stats(self.h, self._count.at, self._count.at + 4))
+        return {"free": int(self._count.a[0]), "sequences": int(self._count.a[1])}
 
 
 class Builder:

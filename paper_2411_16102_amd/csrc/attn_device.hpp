@@ -50,7 +50,7 @@ __device__ __forceinline__ u32x4_t mask_tokens8(u32x4_t v, int t0, int limit) {
 __device__ __forceinline__ u32x4_t mask_between8(u32x4_t v, int t0, int lo, int hi) {
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (t0 + i >= lo && t0 + i < hi) v[i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+    v[i >> 1] &= (t0 + i >= lo) & (t0 + i < hi) ? (i & 1 ? 0x0000FFFFu : 0xFFFF0000u) : 0xFFFFFFFFu;
   return v;
 }
 

@@ -58,6 +58,7 @@ struct Sequence {
 
 struct bs_pages {
   std::vector<int32_t> refs;   // references to each page
+  int64_t most_refs = 1;       // no page has more
   Numbers free;                // pages without one
   std::vector<Sequence> seqs;
   Numbers free_ids;            // of seqs
@@ -186,11 +187,14 @@ int bs_pages_fork(bs_pages *p, const int32_t *parents, int32_t n, int32_t childr
     if (children < 0 || (int64_t)n * children > 0x7fffffff || (int64_t)p->seqs.size() + (int64_t)n * children > 0x7fffffff)
       return fail(p, BS_EINVAL, "bs_pages_fork: %d children of %d parents", children, n);
     if (n > 0 && children > 0 && !out) return fail(p, BS_EINVAL, "bs_pages_fork: out is NULL");
-    int64_t most = 0;
-    for (const int32_t r : p->refs) most = std::max<int64_t>(most, r);
-    if (most + (int64_t)n * children > std::numeric_limits<int32_t>::max()) return fail(p, BS_EINVAL, "too many references to a page");
     const int64_t more = (int64_t)n * children;
+    if (p->most_refs + more > std::numeric_limits<int32_t>::max()) {
+      p->most_refs = 0;
+      for (const int32_t r : p->refs) p->most_refs = std::max<int64_t>(p->most_refs, r);
+      if (p->most_refs + more > std::numeric_limits<int32_t>::max()) return fail(p, BS_EINVAL, "too many references to a page");
+    }
     reserve_ids(p, more);
+    p->most_refs += more;
     std::vector<std::vector<int32_t>> tables((size_t)more);  // every allocation comes before the first change
     for (size_t i = 0; i < tables.size(); ++i) tables[i] = p->seqs[parents[i / (size_t)children]].table;
     for (size_t i = 0; i < tables.size(); ++i) {

@@ -12,12 +12,14 @@
 #include "../../include/blendstep_stream.h"
 #include "common.hpp"
 #include "context.hpp"
+#include "join.hpp"
 #include "w4.hpp"
 
 using namespace bs;
 
 namespace bs {
 namespace {
+using namespace join_dev;
 
 // The constants live in registers: as literals they would keep the and and the or apart.
 struct Unpack {
@@ -35,28 +37,6 @@ template <bool ZEROS>
 __device__ __forceinline__ bf16x8_t sum_operand() {
   constexpr uint32_t V = ZEROS ? 0x3F803F80u : 0xC308C308u;
   return as_bf16x8(u32x4_t{V, V, V, V});
-}
-
-// 16-byte accesses that all XCDs agree on (their L2 caches are their own): partial sums travel past those
-constexpr int SC1 = 16;
-__device__ __forceinline__ void put_part(const __amdgpu_buffer_rsrc_t &rs, unsigned at, f32x4_t v) {
-  const u32x4_t w = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-  __builtin_amdgcn_raw_buffer_store_b128(w, rs, at, 0, SC1);
-}
-__device__ __forceinline__ f32x4_t get_part(const __amdgpu_buffer_rsrc_t &rs, unsigned at) {
-  const u32x4_t w = __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, SC1);
-  return f32x4_t{__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
-}
-
-// Whether this workgroup is the last of `parts` to arrive at a counter (which it clears for the next launch).
-__device__ __forceinline__ bool last_of(unsigned *counter, unsigned parts, unsigned *flag) {
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wavefront's part has arrived where all XCDs see it
-  __syncthreads();
-  if (threadIdx.x == 0) *flag = atomicAdd(counter, 1u);
-  __syncthreads();
-  if (*flag + 1u != parts) return false;
-  if (threadIdx.x == 0) atomicExch(counter, 0u);
-  return true;
 }
 
 // Which outputs, inputs and rows a workgroup takes.
@@ -81,6 +61,18 @@ __device__ __forceinline__ void store_four(const W4Args &a, int m, int n0, f32x4
     if (n0 + r < a.n) y[r] = (uint16_t)pack_bf16x2(v[r], 0.f);
 }
 __device__ __forceinline__ bool wide_rows(const W4Args &a) { return (a.y_stride & 3) == 0 && (reinterpret_cast<uintptr_t>(a.y) & 7) == 0; }
+
+// d += a b.  The compiler may give the sum other registers than d's, and a following product that adds to it then waits for it as for
+// any other result: where less than two independent products come between (NEAR), the wait is written out.
+template <bool NEAR>
+__device__ __forceinline__ f32x4_t mfma(f32x4_t d, bf16x8_t a, bf16x8_t b) {
+  d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, d, 0, 0, 0);
+  if constexpr (NEAR) asm volatile("s_nop 7" : "+v"(d));
+  return d;
+}
+
+// Matrix instructions behind this stay behind it; others may move across.
+__device__ __forceinline__ void products_in_order() { __builtin_amdgcn_sched_barrier(0x3F6); }
 
 // Scales (and zero points) of four outputs in one group, as 32-bit numbers.
 template <bool ZEROS>
@@ -165,10 +157,10 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
       for (int g = 0; g < GPB; ++g) {
         f32x4_t d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(summing, xv[g * STEPS + s], d, 0, 0, 0);
+        for (int s = 0; s < STEPS; ++s) d = mfma<true>(d, summing, xv[g * STEPS + s]);
         d = f.g[u][g].first(d);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack(f.w[u][g * STEPS + s]), xv[g * STEPS + s], d, 0, 0, 0);
+        for (int s = 0; s < STEPS; ++s) d = mfma<true>(d, unpack(f.w[u][g * STEPS + s]), xv[g * STEPS + s]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[r] = __builtin_fmaf(f.g[u][g].scale(r), d[r], y[r]);
       }
@@ -196,7 +188,7 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
       for (int i = 1; i < KW; ++i) y += sums[threadIdx.x + 64 * i];
   }
   if (splits > 1) {
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(a.ws, 0, 0x7fffffff, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rs = parts_of(a.ws);
     const unsigned part = (unsigned)((at.cell * splits * NW + wave / KW) * 64 + lane) * 16u, step = NW * 64 * 16u;
     if (mine) put_part(rs, part + split * step, y);
     if (!last_of(a.counters + at.cell, splits, reinterpret_cast<unsigned *>(lds + 512 * 16))) return;
@@ -285,7 +277,10 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
 #pragma unroll
       for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-        for (int i = 0; i < MB; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(summing, xv[s][i], sum[i], 0, 0, 0);
+        for (int i = 0; i < MB; ++i) {
+          sum[i] = mfma<(MB < 3)>(sum[i], summing, xv[s][i]);
+          if (i == MB - 1) products_in_order();
+        }
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         f32x4_t d[MB];
@@ -295,7 +290,10 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
         for (int s = 0; s < STEPS; ++s) {
           const bf16x8_t w = unpack(f.w[b][g * STEPS + s]);
 #pragma unroll
-          for (int i = 0; i < MB; ++i) d[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xv[s][i], d[i], 0, 0, 0);
+          for (int i = 0; i < MB; ++i) {
+            d[i] = mfma<(MB < 3)>(d[i], w, xv[s][i]);
+            if (i == MB - 1) products_in_order();
+          }
         }
 #pragma unroll
         for (int i = 0; i < MB; ++i)
@@ -338,7 +336,7 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
   if (kb < kb1) step(kb, fa);
   __builtin_amdgcn_s_waitcnt(0x0F70);  // the look-ahead has landed before the LDS is released
   if (splits > 1) {
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(a.ws, 0, 0x7fffffff, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rs = parts_of(a.ws);
     const unsigned step_bytes = NB * MB * 256 * 16u, part = (unsigned)(at.cell * splits) * step_bytes + threadIdx.x * 16u;
 #pragma unroll
     for (int b = 0; b < NB; ++b)

@@ -16,7 +16,7 @@ using namespace bs;
 namespace {
 
 constexpr int PAGE = 16;
-constexpr int MOST_UNIT_PAGES = 64;     // a lane of a wavefront holds one page of its unit
+constexpr int MOST_STATES = 4095;        // of rows whose pages are split (see WindowItem::group)
 constexpr int MAX_AXES = 8;
 constexpr int32_t MAX_LEN = 1 << 30;    // of lengths and rows, so that sums of two stay in 32 bits
 constexpr long STAGE_WORDS = 1 << 16;   // of the plan's pinned memory at first (it grows with the plans)
@@ -24,14 +24,13 @@ constexpr long STAGE_WORDS = 1 << 16;   // of the plan's pinned memory at first 
 // What the kernels of a planned step need to know beside the arrays on the device.
 struct Planned {
   bool made = false, has_angles = false, whole_axes = true;
-  int n_rows = 0, n_rope = 0, n_items = 0, n_joins = 0, window = 1, sinks = 0;
+  int n_rows = 0, n_rope = 0, n_items = 0, waves = 1, window = 1, sinks = 0;
   int n_work = 0, n_cut = 0, wide_blocks = 0;   // wide work: workgroups per group of heads, blocks of rows that several share, all blocks
   int32_t longest = 0, split_rows = 0;
   long states = 0, cut_states = 0, pages = 0;
-  long off_items = 0, off_pages = 0, off_joins = 0, off_rope = 0, off_positions = 0, off_axis = 0, words = 0;
+  long off_items = 0, off_pages = 0, off_rope = 0, off_positions = 0, off_axis = 0, words = 0;
   long off_work = 0, off_cut = 0, off_row_start = 0, off_kv_len = 0, off_page_start = 0, off_page_ids = 0;
-  // partial states, in floats
-  long at_m = 0, at_l = 0, at_cut_acc = 0, at_cut_m = 0, at_cut_l = 0, state_floats = 0;
+  long at_cut_acc = 0, at_cut_m = 0, at_cut_l = 0, state_floats = 0;  // partial states, in floats
 };
 
 }  // namespace
@@ -44,10 +43,14 @@ struct bs_window {
   long cap_words = 0;
   float *d_states = nullptr;
   long cap_states = 0;
+  unsigned *d_counters = nullptr;
+  long cap_counters = 0;
   // host scratch reused across plans
-  std::vector<int32_t> words, refs, item_pages, joins, cut, wide_start, wide_pages;
+  std::vector<int32_t> words, refs, item_pages, cut, wide_start, wide_pages;
   std::vector<WindowItem> items;
   std::vector<RopeItem> rope;
+  struct Rows { int seq, first, n, pages; };  // rows of narrow work that share their units
+  std::vector<Rows> rows;
   struct Work { int blocks, seq, block, t0, t1, state; };
   std::vector<Work> work;
 };
@@ -116,38 +119,74 @@ int check_seen(bs_window *w, int seq, const int32_t *table, const Seen &seen) {
 
 int too_large(bs_window *w) { return ctx_fail(w->ctx, BS_EUNSUPPORTED, "the step is too large for one plan"); }
 
-// Cuts rows [j, end) of a sequence into narrow units of at most `per_unit` rows and `chunk` pages.
-int add_units(bs_window *w, const bs_batch *b, int s, int j, int end, int per_unit, int chunk) {
-  Planned &p = w->p;
-  const int r0 = b->row_start[s], rows = b->row_start[s + 1] - r0;
-  const int32_t *table = b->page_ids + b->page_start[s];
+// Rows [j, end) of a sequence as narrow work, at most `per_unit` in a unit.
+int add_rows(bs_window *w, const bs_batch *b, int s, int j, int end, int per_unit) {
+  const int rows = b->row_start[s + 1] - b->row_start[s];
   for (; j < end; j += per_unit) {
     const int n = std::min(per_unit, end - j), p0 = b->kv_len[s] - rows + j;
-    const Seen seen = seen_by(p0, p0 + n - 1, p.window, p.sinks);
-    if (const int rc = check_seen(w, s, table, seen)) return rc;
-    const int n_pages = seen.pages(), n_chunks = std::max(1, (n_pages + chunk - 1) / chunk);
-    for (int k = 0; k < n_chunks; ++k) {
-      // chunks of nearly equal lengths
-      const int lo = (int)((int64_t)n_pages * k / n_chunks), hi = (int)((int64_t)n_pages * (k + 1) / n_chunks);
+    const Seen seen = seen_by(p0, p0 + n - 1, w->p.window, w->p.sinks);
+    if (const int rc = check_seen(w, s, b->page_ids + b->page_start[s], seen)) return rc;
+    w->rows.push_back({s, j, n, seen.pages()});
+  }
+  return BS_OK;
+}
+
+// How narrow work is cut: wavefronts of a workgroup, pages of a unit.
+struct Division {
+  int waves, pages;
+};
+Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int n_cu) {
+  int64_t all = 0;
+  int longest = 0;
+  for (const bs_window::Rows &r : rows) {
+    all += r.pages;
+    longest = std::max(longest, r.pages);
+  }
+  const int64_t units = (int64_t)rows.size() * hkv, slots = 8 * (int64_t)n_cu;
+  if (units >= slots || longest <= 2) return {1, std::max(2, longest)};
+  const int per_wave = (int)std::max<int64_t>(2, (all * hkv / slots + 1) / 2 * 2);  // pages of a wavefront where all are busy
+  const int shares = (longest + per_wave - 1) / per_wave;
+  int waves = 1;
+  while (waves < 8 && 2 * waves <= shares && units * ((shares + 2 * waves - 1) / (2 * waves)) >= n_cu / 2) waves *= 2;
+  return {waves, per_wave * waves};
+}
+
+// The units of the rows of narrow work.
+int add_units(bs_window *w, const bs_batch *b, const Division &div) {
+  Planned &p = w->p;
+  p.waves = div.waves;
+  for (const bs_window::Rows &r : w->rows) {
+    const int r0 = b->row_start[r.seq], p0 = b->kv_len[r.seq] - (b->row_start[r.seq + 1] - r0) + r.first;
+    const int32_t *table = b->page_ids + b->page_start[r.seq];
+    const Seen seen = seen_by(p0, p0 + r.n - 1, p.window, p.sinks);
+    int n_units = std::max(1, (r.pages + div.pages - 1) / div.pages);
+    n_units = std::min(n_units, MOST_STATES);
+    if (n_units > 1 && p.states + n_units >= 1L << WINDOW_STATE_BITS) n_units = 1;
+    for (int k = 0; k < n_units; ++k) {
+      // whole pairs of pages, in nearly equal shares
+      const int64_t pairs = (r.pages + 1) / 2;
+      const int lo = (int)(2 * (pairs * k / n_units)), hi = std::min(r.pages, (int)(2 * (pairs * (k + 1) / n_units)));
       WindowItem it{};
-      it.row0 = r0 + j;
-      it.n_rows = n;
+      it.row0 = r0 + r.first;
+      it.n_rows = r.n;
       it.page_off = (int32_t)w->item_pages.size();
       it.n_pages = hi - lo;
       it.at = p0 - seen.left_out() - PAGE * lo;
       it.sinks = std::max(0, std::min(p.sinks - PAGE * lo, PAGE * (hi - lo)));
-      it.state = n_chunks > 1 ? (int32_t)(p.states + (long)k * n) : -1;
+      it.state = n_units > 1 ? (int32_t)(p.states + k) : -1;
+      it.group = n_units > 1 ? (int32_t)((uint32_t)p.states | (uint32_t)n_units << WINDOW_STATE_BITS) : 0;
       w->items.push_back(it);
       for (int i = lo; i < hi; ++i) w->item_pages.push_back(table[seen.page(i)]);
       p.longest = std::max(p.longest, it.n_pages);
     }
-    if (n_chunks > 1) {
-      for (int i = 0; i < n; ++i) w->joins.insert(w->joins.end(), {r0 + j + i, (int32_t)(p.states + i), n, n_chunks});
-      p.states += (long)n_chunks * n;
-      p.split_rows += n;
+    if (n_units > 1) {
+      p.states += n_units;
+      p.split_rows += r.n;
     }
-    if (p.states > MAX_LEN || w->item_pages.size() > (size_t)MAX_LEN) return too_large(w);
+    if (w->item_pages.size() > (size_t)MAX_LEN || w->items.size() > (size_t)MAX_LEN) return too_large(w);
   }
+  // longest first: the short ones then fill the end of the launch
+  std::stable_sort(w->items.begin(), w->items.end(), [](const auto &x, const auto &y) { return x.n_pages > y.n_pages; });
   return BS_OK;
 }
 
@@ -171,7 +210,7 @@ int add_blocks(bs_window *w, const bs_batch *b, int s, const Route &r) {
   for (int k = 0; k * r.rows < rows; ++k) {
     const int j = k * r.rows, end = std::min(rows, j + r.rows), p0 = b->kv_len[s] - rows + j, p1 = b->kv_len[s] - rows + end - 1;
     if (p1 < 0) {
-      if (const int rc = add_units(w, b, s, j, end, r.per_unit, MOST_UNIT_PAGES)) return rc;
+      if (const int rc = add_rows(w, b, s, j, end, r.per_unit)) return rc;
       continue;
     }
     const Seen seen = seen_by(p0, p1, p.window, p.sinks);
@@ -183,11 +222,11 @@ int add_blocks(bs_window *w, const bs_batch *b, int s, const Route &r) {
   return BS_OK;
 }
 
-int plan_work(bs_window *w, const bs_batch *b, const Route &r) {
+int plan_work(bs_window *w, const bs_batch *b, const Route &r, int hkv, int n_cu) {
   Planned &p = w->p;
   w->items.clear();
   w->item_pages.clear();
-  w->joins.clear();
+  w->rows.clear();
   w->work.clear();
   w->cut.clear();
   w->wide_start.assign((size_t)b->n_seq + 1, 0);
@@ -198,13 +237,13 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r) {
     if (is_wide(r, rows)) {
       if (const int rc = add_blocks(w, b, s, r)) return rc;
       w->wide_pages.insert(w->wide_pages.end(), b->page_ids + b->page_start[s], b->page_ids + b->page_start[s + 1]);
-    } else if (const int rc = add_units(w, b, s, 0, rows, r.per_unit, MOST_UNIT_PAGES)) {
+    } else if (const int rc = add_rows(w, b, s, 0, rows, r.per_unit)) {
       return rc;
     }
   }
   w->wide_start[b->n_seq] = (int32_t)w->wide_pages.size();
+  if (const int rc = add_units(w, b, divide(w->rows, hkv, n_cu))) return rc;
   p.n_items = (int)w->items.size();
-  p.n_joins = (int)w->joins.size() / 4;
   p.pages += (long)w->item_pages.size();
   // longest first: the short ones then fill the end of the launch
   std::stable_sort(w->work.begin(), w->work.end(), [](const auto &x, const auto &y) { return x.blocks > y.blocks; });
@@ -298,6 +337,7 @@ void bs_window_destroy(bs_window *w) {
     (void)hipDeviceSynchronize();
     if (w->d_words) (void)hipFree(w->d_words);
     if (w->d_states) (void)hipFree(w->d_states);
+    if (w->d_counters) (void)hipFree(w->d_counters);
     w->stage.close();
   }
   delete w;
@@ -331,7 +371,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     p.sinks = std::min(sinks, MAX_LEN);
     const auto fail_with = [&](int rc) { w->p = Planned(); return rc; };
     const Route route = route_of(g);
-    if (const int rc = plan_work(w, b, route)) return fail_with(rc);
+    if (const int rc = plan_work(w, b, route, g.n_kv_heads, v.n_cu > 0 ? v.n_cu : 256)) return fail_with(rc);
     plan_appends(w, b);
     // (grids count units of a KV head, workgroups of some heads, and shares of the heads of a run)
     if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff ||
@@ -342,8 +382,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     const int axes = std::max(1, n_axes);
     const long n_item_pages = (long)w->item_pages.size(), n_wide_pages = (long)w->wide_pages.size();
     p.off_pages = 8L * p.n_items;
-    p.off_joins = p.off_pages + whole_units(n_item_pages);
-    p.off_work = p.off_joins + 4L * p.n_joins;
+    p.off_work = p.off_pages + whole_units(n_item_pages);
     p.off_cut = p.off_work + 4L * p.n_work;
     p.off_row_start = p.off_cut + 4L * p.n_cut;
     const long n_tab = p.n_work ? b->n_seq + 1 : 0;
@@ -373,7 +412,6 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
       std::memcpy(&words[p.off_page_start], w->wide_start.data(), sizeof(int32_t) * n_tab);
       if (n_wide_pages) std::memcpy(&words[p.off_page_ids], w->wide_pages.data(), sizeof(int32_t) * n_wide_pages);
     }
-    if (p.n_joins) std::memcpy(&words[p.off_joins], w->joins.data(), sizeof(int32_t) * w->joins.size());
     if (p.n_rope) std::memcpy(&words[p.off_rope], w->rope.data(), sizeof(RopeItem) * p.n_rope);
     p.has_angles = true;
     for (int s = 0; n_axes == 0 && s < b->n_seq; ++s) {
@@ -392,14 +430,20 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     if (const int rc = stream_is_capturing(c, st, &capturing)) return fail_with(rc);
     if (capturing) return fail_with(ctx_fail(c, BS_EINVAL, "bs_window_plan cannot be captured: plan first, then capture the calls that use the plan"));
     if (const int rc = grow(c, &w->d_words, &w->cap_words, p.words, sizeof(int32_t))) return fail_with(rc);
-    const long n = p.states * g.n_q_heads, n_cut = p.cut_states * route.rows * g.n_q_heads;  // state rows of a head
-    p.at_m = n * g.head_dim;
-    p.at_l = p.at_m + whole_units(n);
-    p.at_cut_acc = p.at_l + whole_units(n);
+    const long n_cut = p.cut_states * route.rows * g.n_q_heads;  // state rows of a head of wide work
+    p.at_cut_acc = p.states * g.n_kv_heads * (g.head_dim / 16 + 1) * 256;
     p.at_cut_m = p.at_cut_acc + n_cut * g.head_dim;
     p.at_cut_l = p.at_cut_m + n_cut;
     p.state_floats = p.at_cut_l + n_cut;
+    if (p.at_cut_acc > (1L << 29)) return fail_with(too_large(w));  // (offsets of the joins: 32 bits of bytes)
     if (const int rc = grow(c, &w->d_states, &w->cap_states, p.state_floats, sizeof(float))) return fail_with(rc);
+    if (p.states * g.n_kv_heads > w->cap_counters) {
+      if (const int rc = grow(c, &w->d_counters, &w->cap_counters, p.states * g.n_kv_heads, sizeof(unsigned))) return fail_with(rc);
+      if (hipError_t e = hipMemset(w->d_counters, 0, sizeof(unsigned) * (size_t)w->cap_counters)) {
+        w->cap_counters = 0;
+        return fail_with(ctx_fail(c, BS_EHIP, "hipMemset: %s", hipGetErrorString(e)));
+      }
+    }
     int32_t *pinned = nullptr;
     if (const int e = w->stage.place(p.words, st, &pinned))
       return fail_with(ctx_fail(c, e == hipErrorOutOfMemory ? BS_ENOMEM : BS_EHIP, "pinned memory of a plan: %s", hipGetErrorString((hipError_t)e)));
@@ -470,11 +514,9 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
     a.n_items = p.n_items; a.window = p.window;
     a.q = (const uint16_t *)q; a.kv_pool = (const uint16_t *)kv_pool; a.out = (uint16_t *)out;
     a.q_stride = q_stride; a.out_stride = out_stride;
-    a.joins = w->d_words + p.off_joins;
-    a.n_joins = p.n_joins;
-    a.part_acc = w->d_states;
-    a.part_m = w->d_states + p.at_m;
-    a.part_l = w->d_states + p.at_l;
+    a.waves = p.waves;
+    a.parts = w->d_states;
+    a.counters = w->d_counters;
     if (p.n_work) {
       const Route route = route_of(g);
       WindowPrefillArgs f{};
@@ -490,7 +532,6 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
       CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
     }
     CTX_HIP_TRY(c, launch_window_units(a, st));
-    CTX_HIP_TRY(c, launch_window_join(a, st));
     return BS_OK;
   });
 }
