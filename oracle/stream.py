@@ -25,15 +25,16 @@ def window_attention(q, K, V, first: int, window: int, sinks: int):
     n, hq, dh = q.shape
     grp = hq // K.shape[1]
     out, weight = np.zeros((n, hq, dh)), np.zeros((n, hq, dh))
-    for j in range(n):
-        see = [t for t in range(len(K)) if visible(first + j, t, window, sinks)]
-        if not see:
-            continue
-        for h in range(hq):
-            s = K[see, h // grp].astype(np.float64) @ q[j, h] / np.sqrt(dh)
-            e = np.exp(s - s.max())
-            out[j, h] = e @ V[see, h // grp] / e.sum()
-            weight[j, h] = e @ np.abs(V[see, h // grp]) / e.sum()
+    p, t = first + np.arange(n)[:, None], np.arange(len(K))[None, :]
+    see = (t <= p) & ((t > p - window) | (t < sinks))
+    some, rows = see.any(axis=0), see.any(axis=1)
+    K, V, see = K[some].astype(np.float64), V[some].astype(np.float64), see[:, some]
+    for h in range(hq if rows.any() else 0):
+        s = np.where(see, q[:, h] @ K[:, h // grp].T / np.sqrt(dh), -np.inf)[rows]
+        e = np.exp(s - s.max(axis=1, keepdims=True))
+        e /= e.sum(axis=1, keepdims=True)
+        out[rows, h] = e @ V[:, h // grp]
+        weight[rows, h] = e @ np.abs(V[:, h // grp])
     return out, weight
 
 

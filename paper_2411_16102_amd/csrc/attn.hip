@@ -24,6 +24,7 @@
 #include "attn.hpp"
 #include "attn_device.hpp"
 #include "common.hpp"
+#include "window_device.hpp"
 
 namespace bs {
 namespace {
@@ -405,7 +406,8 @@ __device__ __forceinline__ void prefill_workgroup(const Args &a, int heads_per_w
     const int row0 = row_w + qb * 32;
     n_q[qb] = min(32, q_len - row0);                       // <= 0: the block does not exist
     first_pos[qb] = before + row0;
-    my_pos[qb] = min(first_pos[qb] + lr, kv_len - 1);
+    // (a range may end before the row; the row's window goes by where it stands)
+    my_pos[qb] = WINDOW ? first_pos[qb] + lr : min(first_pos[qb] + lr, kv_len - 1);
     const bool ok = lr < n_q[qb];
     const uint16_t *p = a.q + (size_t)(r0 + (ok ? row0 + lr : 0)) * q_row<DH>(a) + head * DH + 8 * g2;
 #pragma unroll
@@ -646,6 +648,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, DH == 64
   extern __shared__ __align__(256) unsigned char attn_smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   prefill_workgroup<DH>(a, heads_per_wg, blockIdx.x, wave, threadIdx.x & 63, attn_smem);
+}
+
+// Both kinds of work of a step in one launch: the blocks of rows, longest first, then the units, which stream pages on the CUs that
+// blocks leave and while these wait for their pipes.
+template <int DH>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, DH == 64 ? 2 : 1))) void window_step_kernel(const WindowArgs u, const WindowPrefillArgs a, int heads_per_wg, int n_blocks) {
+  extern __shared__ __align__(256) unsigned char attn_smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int)blockIdx.x < n_blocks) prefill_workgroup<DH>(a, heads_per_wg, blockIdx.x, wave, threadIdx.x & 63, attn_smem);
+  else window_dev::window_unit<DH, 4>(u, (int)blockIdx.x - n_blocks, attn_smem);
 }
 
 // The same without the ring, for groups of heads that are not a multiple of four: a wavefront takes 64 query
@@ -977,6 +989,16 @@ hipError_t launch_window_prefill(const WindowPrefillArgs &a, int heads, hipStrea
   static OncePerDevice once[2];
   if (a.s.head_dim == 128) return launch_with_lds(window_prefill_kernel<128>, once[0], grid, PF_LDS(128), stream, a, heads);
   if (a.s.head_dim == 64) return launch_with_lds(window_prefill_kernel<64>, once[1], grid, PF_LDS(64), stream, a, heads);
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_window_step(const WindowArgs &u, const WindowPrefillArgs &a, int heads, hipStream_t stream) {
+  if (u.waves != 4 || u.n_items <= 0 || a.n_work <= 0) return hipErrorInvalidValue;
+  const int n_blocks = a.n_work * (a.s.n_q_heads / heads), grid = n_blocks + u.n_items * u.s.n_kv_heads;
+  static OncePerDevice once[2];
+  static_assert(window_dev::WINDOW_UNIT_LDS(128, 4) <= PF_LDS(128) && window_dev::WINDOW_UNIT_LDS(64, 4) <= PF_LDS(64), "a unit's LDS fits a ring's");
+  if (a.s.head_dim == 128) return launch_with_lds(window_step_kernel<128>, once[0], grid, PF_LDS(128), stream, u, a, heads, n_blocks);
+  if (a.s.head_dim == 64) return launch_with_lds(window_step_kernel<64>, once[1], grid, PF_LDS(64), stream, u, a, heads, n_blocks);
   return hipErrorInvalidValue;
 }
 

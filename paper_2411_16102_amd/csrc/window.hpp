@@ -31,6 +31,8 @@ struct WindowArgs {
   unsigned *counters;            // [states][Hkv], zero between launches
 };
 hipError_t launch_window_units(const WindowArgs &a, hipStream_t stream);
+// Narrow and wide work of a step in one launch (a.waves is 4).
+hipError_t launch_window_step(const WindowArgs &a, const WindowPrefillArgs &f, int heads, hipStream_t stream);
 
 // Rows of one sequence whose keys and values go to one page, at most 16, or rows that append nothing (page -1).
 struct RopeItem {

@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <limits>
 #include <vector>
 
 #include "../../include/blendstep_stream.h"
@@ -131,24 +132,48 @@ int add_rows(bs_window *w, const bs_batch *b, int s, int j, int end, int per_uni
   return BS_OK;
 }
 
-// How narrow work is cut: wavefronts of a workgroup, pages of a unit.
+// How narrow work is cut: wavefronts of a workgroup, pages of a unit, and the microseconds that are expected of it.  Timed for 1 to 256 streams
+// of four head layouts, windows of 64 to 4096, each with 1 to 8 wavefronts and 4 to 256 pages: within 2 % of the best of them on
+// average, 11 % at worst (one stream, window 1024, 8 KV heads: 6 units of 12 pages 9.2 us, one of 66 on eight wavefronts 18; 64 of window 4096: whole
+// on eight 169, halves 187).
 struct Division {
   int waves, pages;
+  double us;
 };
-Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int n_cu) {
-  int64_t all = 0;
-  int longest = 0;
+Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int dh, int n_cu) {
+  int64_t all = 0, once = 0;  // pages of all units; without those that rows of the same sequence have seen before
+  int longest = 0, last = -1;
   for (const bs_window::Rows &r : rows) {
     all += r.pages;
+    once += r.seq == last ? std::min(r.pages, 1) : r.pages;
+    last = r.seq;
     longest = std::max(longest, r.pages);
   }
-  const int64_t units = (int64_t)rows.size() * hkv, slots = 8 * (int64_t)n_cu;
-  if (units >= slots || longest <= 2) return {1, std::max(2, longest)};
-  const int per_wave = (int)std::max<int64_t>(2, (all * hkv / slots + 1) / 2 * 2);  // pages of a wavefront where all are busy
-  const int shares = (longest + per_wave - 1) / per_wave;
-  int waves = 1;
-  while (waves < 8 && 2 * waves <= shares && units * ((shares + 2 * waves - 1) / (2 * waves)) >= n_cu / 2) waves *= 2;
-  return {waves, per_wave * waves};
+  // A CU streams 36 GB/s of pages however many ask, a unit's pages go through one; a join waits for a round trip and one more for every
+  // eight units or so.
+  const double us_per_page = dh == 128 ? 0.23 : 0.13, all_us = (double)once * hkv * dh * (4.0 * PAGE / 5.9e6);
+  double best = 0;
+  Division div = {1, std::max(2, longest), 0.0};
+  int64_t n_units = (int64_t)rows.size() * hkv;
+  for (int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+    const int pages = std::max(2, 2 * ((longest + 2 * n - 1) / (2 * n)));
+    if (n > 1 && pages < 4) break;
+    int64_t units = 0;
+    for (const bs_window::Rows &r : rows) units += std::max(1, (r.pages + pages - 1) / pages);
+    units *= hkv;
+    const double rounds = units <= 4 * (int64_t)n_cu ? (double)((units + n_cu - 1) / n_cu) : 0.5 + (double)all * hkv / pages / n_cu;
+    const double cost = std::max(all_us, us_per_page * pages * rounds) + (n > 1 ? 2.0 + 0.25 * n + 0.004 * (double)units : 0.0);
+    if (n == 1 || cost < best) {
+      best = cost;
+      div.pages = std::max(2, pages);
+      n_units = units;
+    }
+  }
+  // Wavefronts of a workgroup: about 16 to 32 pages each, and no more than two for a SIMD.
+  div.waves = div.pages <= 2 ? 1 : div.pages <= 64 ? 2 : div.pages <= 128 ? 4 : 8;
+  while (div.waves > 1 && n_units * div.waves > 12 * (int64_t)n_cu) div.waves /= 2;
+  div.us = best;
+  return div;
 }
 
 // The units of the rows of narrow work.
@@ -199,7 +224,6 @@ Route route_of(const bs_layer_cfg &g) {
   const int grp = g.n_q_heads / g.n_kv_heads, heads = grp % 4 == 0 ? 4 : grp % 2 == 0 ? 2 : 1;
   return {std::max(1, 16 / grp), heads, 64 * (4 / heads)};
 }
-bool is_wide(const Route &r, int rows) { return rows > 4 * r.per_unit; }
 
 // The rows of a longer segment as blocks for wide workgroups; rows of blocks that stand wholly in front of their sequence see nothing:
 // units without pages.
@@ -222,19 +246,73 @@ int add_blocks(bs_window *w, const bs_batch *b, int s, const Route &r) {
   return BS_OK;
 }
 
-int plan_work(bs_window *w, const bs_batch *b, const Route &r, int hkv, int n_cu) {
+// How the blocks of wide work are cut into ranges of their pages, workgroups of their own: 32-token blocks of a range (0: not cut), and the
+// microseconds that are expected.  A workgroup takes 1.25 us per 32 tokens (64-wide heads: 1.15, two to a CU) and two such
+// to begin; states and their merge cost 10 us and 0.02 for every workgroup.  Timed for segments of 6 to 300 rows, 1 to 16 of them, windows of
+// 1024 to 4096: 64 rows behind 4096 tokens, 8 KV heads, 165 us whole, 28 in ranges of 8; four segments of 300 rows 149 whole, 168 in halves.
+struct Cut {
+  int blocks;
+  double us;
+};
+Cut cut_choice(const std::vector<bs_window::Work> &work, int wg_per_work, int dh, int rows, int n_cu) {
+  const double us = dh == 64 ? 1.15 : 1.25;
+  const int64_t slots = dh == 64 ? 2 * n_cu : n_cu;
+  int64_t all = 0;
+  int longest = 0;
+  for (const bs_window::Work &k : work) {
+    all += k.blocks + 2;
+    longest = std::max(longest, k.blocks);
+  }
+  Cut best = {0, us * std::max((double)(longest + 2), (double)(all * wg_per_work) / slots)};
+  for (int t : {4, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96}) {
+    if (t >= longest || longest >= 65536) break;
+    int64_t ranges = 0, states = 0;
+    for (const bs_window::Work &k : work) {
+      const int n = (k.blocks + t - 1) / t;
+      ranges += n;
+      states += n > 1 ? n : 0;
+    }
+    if (states * rows > MAX_LEN / 64) continue;
+    const int64_t wgs = ranges * wg_per_work;
+    const double cost = us * (t + 2) * (double)((wgs + slots - 1) / slots) + 10.0 + 0.02 * (double)wgs;
+    if (cost < best.us) best = {t, cost};
+  }
+  return best;
+}
+
+void cut_blocks(bs_window *w, int most) {
   Planned &p = w->p;
-  w->items.clear();
-  w->item_pages.clear();
+  if (most == 0) return;
+  std::vector<bs_window::Work> whole;
+  whole.swap(w->work);
+  for (const bs_window::Work &k : whole) {
+    const int n = (k.blocks + most - 1) / most;
+    if (n == 1) {
+      w->work.push_back(k);
+      continue;
+    }
+    w->cut.insert(w->cut.end(), {k.seq, k.block, (int32_t)p.cut_states, n});
+    for (int i = 0; i < n; ++i) {
+      const int t0 = (int)((int64_t)k.blocks * i / n), t1 = (int)((int64_t)k.blocks * (i + 1) / n);
+      w->work.push_back({t1 - t0, k.seq, k.block, t0, i + 1 < n ? t1 : 0, (int)p.cut_states + i});
+    }
+    p.cut_states += n;
+  }
+}
+
+// Sorts the rows of every sequence into the two kinds of work: wide that of sequences with more than most_narrow rows.
+int sort_rows(bs_window *w, const bs_batch *b, const Route &r, int most_narrow) {
+  Planned &p = w->p;
   w->rows.clear();
   w->work.clear();
-  w->cut.clear();
   w->wide_start.assign((size_t)b->n_seq + 1, 0);
   w->wide_pages.clear();
+  p.wide_blocks = 0;
+  p.pages = 0;
   for (int s = 0; s < b->n_seq; ++s) {
     const int rows = b->row_start[s + 1] - b->row_start[s];
     w->wide_start[s] = (int32_t)w->wide_pages.size();
-    if (is_wide(r, rows)) {
+    if (rows > most_narrow) {
       if (const int rc = add_blocks(w, b, s, r)) return rc;
       w->wide_pages.insert(w->wide_pages.end(), b->page_ids + b->page_start[s], b->page_ids + b->page_start[s + 1]);
     } else if (const int rc = add_rows(w, b, s, 0, rows, r.per_unit)) {
@@ -242,7 +320,51 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, int hkv, int n_cu
     }
   }
   w->wide_start[b->n_seq] = (int32_t)w->wide_pages.size();
-  if (const int rc = add_units(w, b, divide(w->rows, hkv, n_cu))) return rc;
+  return BS_OK;
+}
+
+int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cfg &g, int n_cu) {
+  Planned &p = w->p;
+  w->items.clear();
+  w->item_pages.clear();
+  w->cut.clear();
+  // Sequences with more rows than a unit, or than four, are wide work, or none is: whichever is expected to be shortest.  A few blocks of
+  // rows are shorter as narrow work, whose units spread over the chip: four segments of 32 rows, window 1024, 8 KV heads 18.6 us
+  // against 25, sixteen of 64 rows, 16 heads without groups 79 against 44.
+  int rows_of[3] = {std::numeric_limits<int>::max(), 4 * r.per_unit, r.per_unit}, most = 0, next = 0;
+  for (int s = 0; s < b->n_seq; ++s) {
+    const int n = b->row_start[s + 1] - b->row_start[s];
+    most = std::max(most, n);
+    if (n > r.per_unit && n <= 4 * r.per_unit) next = 1;
+  }
+  Division div = {1, 2, 0.0};
+  Cut cut = {0, 0.0};
+  double best = -1.0;
+  int chosen = rows_of[0];
+  for (int k = 2; k >= 0; --k) {
+    const int rows = rows_of[k];
+    if (rows < most ? (k == 2 && !next) : k != 0) continue;  // (the same as another)
+    if (k == 0 && best >= 0.0) {  // many rows as narrow work: more pages than could be worth it
+      int64_t pages = 0;
+      for (const bs_window::Work &x : w->work) pages += (int64_t)x.blocks * (r.rows / r.per_unit);
+      if (pages * g.n_kv_heads * 0.1 > 2.0 * best * n_cu) continue;
+    }
+    if (const int rc = sort_rows(w, b, r, rows)) return rc;
+    const Division d = divide(w->rows, g.n_kv_heads, g.head_dim, n_cu);
+    const Cut c = w->work.empty() ? Cut{0, 0.0} : cut_choice(w->work, g.n_q_heads / r.heads, g.head_dim, r.rows, n_cu);
+    if (best < 0.0 || d.us + c.us < best) {
+      best = d.us + c.us;
+      div = d;
+      cut = c;
+      chosen = rows;
+    }
+  }
+  if (const int rc = sort_rows(w, b, r, chosen)) return rc;
+  if (!w->work.empty()) {
+    cut_blocks(w, cut.blocks);
+    div = {4, std::max(div.pages, 8), 0.0};  // (one launch for both kinds, of workgroups of four wavefronts)
+  }
+  if (const int rc = add_units(w, b, div)) return rc;
   p.n_items = (int)w->items.size();
   p.pages += (long)w->item_pages.size();
   // longest first: the short ones then fill the end of the launch
@@ -371,7 +493,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     p.sinks = std::min(sinks, MAX_LEN);
     const auto fail_with = [&](int rc) { w->p = Planned(); return rc; };
     const Route route = route_of(g);
-    if (const int rc = plan_work(w, b, route, g.n_kv_heads, v.n_cu > 0 ? v.n_cu : 256)) return fail_with(rc);
+    if (const int rc = plan_work(w, b, route, g, v.n_cu)) return fail_with(rc);
     plan_appends(w, b);
     // (grids count units of a KV head, workgroups of some heads, and shares of the heads of a run)
     if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff ||
@@ -529,7 +651,18 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
       f.page_start = w->d_words + p.off_page_start; f.page_ids = w->d_words + p.off_page_ids;
       f.q = a.q; f.kv_pool = a.kv_pool; f.out = a.out;
       f.window = p.window; f.sinks = p.sinks; f.q_stride = q_stride; f.out_stride = out_stride;
-      CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
+      if (p.n_items > 0) CTX_HIP_TRY(c, launch_window_step(a, f, route.heads, st));
+      else CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
+      if (p.n_cut) {
+        WindowMergeArgs m{};
+        m.s = a.s;
+        m.row_start = f.row_start;
+        m.out = a.out; m.out_stride = out_stride;
+        m.cut = w->d_words + p.off_cut; m.n_cut = p.n_cut; m.cut_heads = route.heads; m.cut_rows = route.rows;
+        m.cut_acc = f.part_acc; m.cut_m = f.part_m; m.cut_l = f.part_l;
+        CTX_HIP_TRY(c, launch_window_merge(m, st));
+      }
+      if (p.n_items > 0) return BS_OK;
     }
     CTX_HIP_TRY(c, launch_window_units(a, st));
     return BS_OK;

@@ -40,9 +40,9 @@ def _attention(lib, shape, batch, window, sinks, seed=0, poison=True, layer=None
         used = np.zeros((batch.n_pages, 16), dtype=bool)
         for s in range(batch.n_seq):
             n, rows = int(batch.kv_len[s]), int(batch.row_start[s + 1] - batch.row_start[s])
-            for t in range(n):
-                if any(OS.visible(p, t, window, sinks) for p in range(n - rows, n)):
-                    used[batch.page_ids[batch.page_start[s] + t // 16], t % 16] = True
+            p, t = np.arange(n - rows, n)[:, None], np.arange(n)
+            seen = np.flatnonzero(((t <= p) & ((t > p - window) | (t < sinks))).any(axis=0))
+            used[batch.page_ids[batch.page_start[s] + seen // 16], seen % 16] = True
         k[~used], v[~used] = 0x7FC0, 0xFF80
     pool = layer.pack_pool(k, v)
     q = _bits(rng, (batch.n_rows, q_stride or width))
@@ -96,6 +96,46 @@ def test_long_contexts_are_split_and_joined(lib, hq, hkv, dh):
     shape = W.LayerShape(256, hq, hkv, dh, 256)
     layer, plan, *_ = _attention(lib, shape, make_batch([(1, 3000), (2, 2500), (1, 5)]), 2000, 40)
     assert plan.division().split_rows == 3
+
+
+WIDE = [(8, 2, 128), (4, 4, 64), (12, 2, 64), (6, 2, 128), (16, 1, 64)]
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [h for h in WIDE if h[0] != h[1]])
+def test_blocks_of_rows(lib, hq, hkv, dh):
+    # enough rows that blocks of them are the shorter way: odd lengths, windows that begin in the chunk, before it and
+    # before the sequence, rows in front of it
+    shape = W.LayerShape(256, hq, hkv, dh, 256)
+    batch = make_batch([(700 + 13 * i, 900 + 101 * i) for i in range(7)] + [(230, 100), (700, 700), (629, 629)], seed=hq, spare=200)
+    for window, sinks in ((150, 20), (333, 0), (900, 4), (10_000, 3), (17, 100)):
+        _, plan, *_ = _attention(lib, shape, batch, window, sinks, seed=window, poison=window < 500)
+        assert plan.division().wide_blocks >= 29
+
+
+@pytest.mark.parametrize("hq,hkv,dh", WIDE)
+def test_blocks_of_rows_cut_into_ranges(lib, hq, hkv, dh):
+    shape = W.LayerShape(256, hq, hkv, dh, 256)
+    for seqs, window, sinks in (([(257, 4500), (260, 4400)], 3001, 1000), ([(600, 6100)], 5000, 50)):
+        _, plan, *_ = _attention(lib, shape, make_batch(seqs, seed=dh), window, sinks, seed=window)
+        assert plan.division().wide_cut >= 3
+
+
+@pytest.mark.parametrize("hq,hkv,dh", WIDE)
+def test_blocks_and_units_in_one_launch(lib, hq, hkv, dh):
+    shape = W.LayerShape(256, hq, hkv, dh, 256)
+    seqs = [(850 + i, 1700 + 90 * i) for i in range(6)] + [(1, n) for n in (1, 0, 500, 2000, 900, 33, 64)] * 3 + [(3, 1000), (2, 1), (0, 77)]
+    for window, sinks in ((1500, 0),) if hq == hkv else ((400, 4), (1500, 0)):
+        _, plan, *_ = _attention(lib, shape, make_batch(seqs, seed=hkv), window, sinks, seed=window, poison=window < 500)
+        d = plan.division()
+        assert d.wide_blocks >= 24 and d.units >= 20
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (8, 8, 64)])
+def test_streams_shared_by_wavefronts(lib, heads):
+    # numbers of streams and windows for which a unit's pages are shared by one, two, four and eight wavefronts, whole and cut
+    shape = W.LayerShape(256, *heads, 256)
+    for n, ctx, window in ((200, 60, 20), (40, 700, 500), (150, 2100, 2000), (90, 2500, 2300), (1, 5000, 4800), (3, 4000, 100_000)):
+        _attention(lib, shape, make_batch([(1, ctx - 7 * (i % 9)) for i in range(n)], seed=n), window, 9, poison=n < 50)
 
 
 def test_pages_given_up_and_strided_rows(lib):

@@ -23,6 +23,23 @@ def test_oracle_attention_without_a_limit_is_causal_attention():
     np.testing.assert_allclose(out[3], V[28].repeat(2, axis=0), atol=1e-13)
 
 
+@pytest.mark.parametrize("first,window,sinks", [(25, 7, 2), (-3, 4, 1), (0, 1, 0), (12, 30, 14), (40, 5, 33)])
+def test_oracle_attention_is_what_every_row_sees(first, window, sinks):
+    rng = np.random.default_rng(first + 9)
+    n = max(0, first + 6)
+    q, K, V = rng.standard_normal((6, 4, 8)), rng.standard_normal((n, 2, 8)), rng.standard_normal((n, 2, 8))
+    out, weight = OS.window_attention(q, K, V, first, window, sinks)
+    for j in range(6):
+        see = [t for t in range(n) if OS.visible(first + j, t, window, sinks)]
+        for h in range(4):
+            if not see:
+                assert not out[j, h].any() and not weight[j, h].any()
+                continue
+            e = np.exp([K[t, h // 2] @ q[j, h] / 8 ** 0.5 for t in see])
+            np.testing.assert_allclose(out[j, h], sum(w * V[t, h // 2] for w, t in zip(e, see)) / e.sum(), atol=1e-13)
+            np.testing.assert_allclose(weight[j, h], sum(w * abs(V[t, h // 2]) for w, t in zip(e, see)) / e.sum(), atol=1e-13)
+
+
 def test_oracle_rope_of_equal_axes_is_rope():
     rng = np.random.default_rng(2)
     v, pos = rng.standard_normal((6, 3, 16)), np.array([0, 1, 5, 100, 7, 3])
