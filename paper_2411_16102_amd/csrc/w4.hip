@@ -48,19 +48,13 @@ __device__ __forceinline__ Place place(int splits, int tiles) {
   return {rest % splits, tile, z, z * tiles + tile};
 }
 
-// four outputs n0 .. n0 + 3 of row m
-__device__ __forceinline__ void store_four(const W4Args &a, int m, int n0, f32x4_t v, bool wide) {
-  if (m >= a.m) return;
-  uint16_t *y = a.y + m * a.y_stride + n0;
-  if (wide && n0 + 4 <= a.n) {
-    *reinterpret_cast<u32x2_t *>(y) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    return;
-  }
+// output n of rows m .. m + 3
+__device__ __forceinline__ void store_four(const W4Args &a, int m, int n, f32x4_t v) {
+  if (n >= a.n) return;
 #pragma unroll
   for (int r = 0; r < 4; ++r)
-    if (n0 + r < a.n) y[r] = (uint16_t)pack_bf16x2(v[r], 0.f);
+    if (m + r < a.m) a.y[(m + r) * a.y_stride + n] = (uint16_t)pack_bf16x2(v[r], 0.f);
 }
-__device__ __forceinline__ bool wide_rows(const W4Args &a) { return (a.y_stride & 3) == 0 && (reinterpret_cast<uintptr_t>(a.y) & 7) == 0; }
 
 // d += a b.  The compiler may give the sum other registers than d's, and a following product that adds to it then waits for it as for
 // any other result: where less than two independent products come between (NEAR), the wait is written out.
@@ -74,27 +68,38 @@ __device__ __forceinline__ f32x4_t mfma(f32x4_t d, bf16x8_t a, bf16x8_t b) {
 // Matrix instructions behind this stay behind it; others may move across.
 __device__ __forceinline__ void products_in_order() { __builtin_amdgcn_sched_barrier(0x3F6); }
 
-// Scales (and zero points) of four outputs in one group, as 32-bit numbers.
-template <bool ZEROS>
-struct Group {
-  u32x2_t s;
+// Scales (and zero points) of a lane's output j in the groups of a block, as loaded: whole words, with those of neighbours
+// where a lane's own are less (a narrower load would have to be extended, and be waited for where it is loaded).
+template <int GPB, bool ZEROS>
+struct Groups {
+  uint32_t s[(GPB + 1) / 2];
   uint32_t z;
-  __device__ __forceinline__ void load(const W4Args &a, const W4Layout &l, int64_t at, int g4) {
-    s = *reinterpret_cast<const u32x2_t *>(a.weight + l.scales + at * 32 + 8 * g4);
-    if constexpr (ZEROS) z = *reinterpret_cast<const uint32_t *>(a.weight + l.zeros + at * 16 + 4 * g4);
+  __device__ __forceinline__ void load(const W4Args &a, const W4Layout &l, int64_t block, int j) {
+    const int64_t at = (block * 16 + j) * GPB;
+    const unsigned char *sp = a.weight + l.scales + (GPB == 1 ? at & ~(int64_t)1 : at) * 2;
+    if constexpr (GPB == 4) {
+      const u32x2_t v = *reinterpret_cast<const u32x2_t *>(sp);
+      s[0] = v[0];
+      s[1] = v[1];
+    } else {
+      s[0] = *reinterpret_cast<const uint32_t *>(sp);
+    }
+    if constexpr (ZEROS) z = *reinterpret_cast<const uint32_t *>(a.weight + l.zeros + (at & ~(int64_t)3));
   }
   __device__ __forceinline__ void here() {
-    asm volatile("" : "+v"(s));
+#pragma unroll
+    for (int i = 0; i < (GPB + 1) / 2; ++i) asm volatile("" : "+v"(s[i]));
     if constexpr (ZEROS) asm volatile("" : "+v"(z));
   }
-  __device__ __forceinline__ float scale(int r) const { return __uint_as_float(r & 1 ? s[r >> 1] & 0xFFFF0000u : s[r >> 1] << 16); }
+  __device__ __forceinline__ float scale(int g, int j) const {
+    if constexpr (GPB == 1) return __uint_as_float((s[0] << (j & 1 ? 0 : 16)) & 0xFFFF0000u);
+    return __uint_as_float(g & 1 ? s[g >> 1] & 0xFFFF0000u : s[g >> 1] << 16);
+  }
   // where the accumulators of a group begin, from the product with sum_operand
-  __device__ __forceinline__ f32x4_t first(f32x4_t sum) const {
+  __device__ __forceinline__ f32x4_t first(int g, int j, f32x4_t sum) const {
     if constexpr (!ZEROS) return sum;
-    f32x4_t c;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] = -(128.f + (float)((z >> (8 * r)) & 0xFFu)) * sum[r];
-    return c;
+    const float c = -(128.f + (float)((z >> (8 * ((j * GPB + g) & 3))) & 0xFFu));
+    return f32x4_t{c * sum[0], c * sum[1], c * sum[2], c * sum[3]};
   }
 };
 
@@ -114,7 +119,7 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
   const int kb0 = first + n_mine * (wave % KW) / KW, kb1 = first + n_mine * (wave % KW + 1) / KW;
   struct Blocks {
     u32x4_t w[U];
-    Group<ZEROS> g[U][GPB];
+    Groups<GPB, ZEROS> g[U];
   };
   const unsigned char *wp = a.weight + nb * n_kb * 1024 + lane * 16;
   auto load = [&](int kb, Blocks &f) __attribute__((always_inline)) {
@@ -122,8 +127,7 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
     for (int u = 0; u < U; ++u) {
       const int k = max(min(kb + u, kb1 - 1), 0);  // (past the end: the last block again, not used)
       f.w[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(wp + (int64_t)k * 1024));
-#pragma unroll
-      for (int g = 0; g < GPB; ++g) f.g[u][g].load(a, l, nb * l.groups + k * GPB + g, g4);
+      f.g[u].load(a, l, nb * n_kb + k, j);
     }
   };
   Blocks fa, fb;
@@ -148,8 +152,7 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (kb + u >= kb1) break;  // wave-uniform
-#pragma unroll
-      for (int g = 0; g < GPB; ++g) f.g[u][g].here();
+      f.g[u].here();
       bf16x8_t xv[4];
 #pragma unroll
       for (int s = 0; s < 4; ++s) xv[s] = as_bf16x8(*reinterpret_cast<const u32x4_t *>(x + (kb + u) * 128 + 32 * s));
@@ -157,12 +160,12 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
       for (int g = 0; g < GPB; ++g) {
         f32x4_t d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) d = mfma<true>(d, summing, xv[g * STEPS + s]);
-        d = f.g[u][g].first(d);
+        for (int s = 0; s < STEPS; ++s) d = mfma<true>(d, xv[g * STEPS + s], summing);
+        d = f.g[u].first(g, j, d);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) d = mfma<true>(d, unpack(f.w[u][g * STEPS + s]), xv[g * STEPS + s]);
+        for (int s = 0; s < STEPS; ++s) d = mfma<true>(d, xv[g * STEPS + s], unpack(f.w[u][g * STEPS + s]));
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = __builtin_fmaf(f.g[u][g].scale(r), d[r], y[r]);
+        for (int r = 0; r < 4; ++r) y[r] = __builtin_fmaf(f.g[u].scale(g, j), d[r], y[r]);
       }
     }
   };
@@ -197,35 +200,43 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
       for (int i = 0; i < splits; ++i) y += get_part(rs, part + i * step);
     }
   }
-  if (mine) store_four(a, j, (int)block * 16 + 4 * g4, y, wide_rows(a));
+  if (mine) store_four(a, 4 * g4, (int)block * 16 + j, y);
 }
 
-// ---- up to 64 rows: a workgroup of four wavefronts takes 16 * MB rows and 128 outputs, two blocks of 16 each wavefront ----
-// x travels to LDS as matrix operands (a wavefront's load of 1 KB is one operand of 16 rows by 32 inputs), in a ring of RING
-// blocks of 128 inputs that all four wavefronts read; weights go straight to registers, two blocks before they are used.
-constexpr int TILE_RING = 4, TILE_NB = 2;
+// ---- up to 64 rows: a workgroup of two shares of the inputs, four wavefronts each, takes 16 * MB rows and 64 * NB outputs ----
+// x travels to LDS as matrix operands (a wavefront's load of 1 KB is one operand of 16 rows by 32 inputs), in a ring for each share of RING
+// blocks of 128 inputs that its four wavefronts read; weights go straight to registers, two blocks before they are used.  The shares keep
+// two wavefronts on a SIMD, of which one computes while the other waits for LDS (half the wavefronts: 81 us for 51 at 8192 x 28672, 61 rows), and
+// are added up in LDS, which two workgroups would do through memory (53 us).
+// What bounds it: products and reads of LDS together.  A block is 12 MB products of a wavefront (a third of them the sum of x, which takes the place
+// of unpacking to signed numbers: twice the instructions) beside 4 MB reads of 1 KB, which a CU answers at 64 bytes a clock.  For 8192 x 28672, 61 rows
+// those are 21 and 25 us, the weights from memory 27, and all of it 50.5: 2.5 TB/s of weights, 0.85 PFLOP/s with the sums.  With up to 16 rows it is
+// bound by memory: 8192 x 28672 28 us, 4.4 TB/s.
+constexpr int TILE_RING = 4, TILE_KW = 2;
 
 __device__ __forceinline__ void x_to_lds(const void *src, unsigned char *lds) {
   __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
 }
 
-template <int GROUP, bool ZEROS, int MB>
-__global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W4Layout l, int splits, int tiles) {
-  constexpr int NB = TILE_NB, GPB = 128 / GROUP, STEPS = GROUP / 32, BLK = 4 * MB * 1024;
+template <int GROUP, bool ZEROS, int MB, int NB>
+__global__ __launch_bounds__(256 * TILE_KW, 2) void w4_tile_kernel(const W4Args a, const W4Layout l, int splits, int tiles) {
+  constexpr int KW = TILE_KW, GPB = 128 / GROUP, STEPS = GROUP / 32, BLK = 4 * MB * 1024;
   // (dynamic: the compiler would let every read of a ring that it knows wait for all that is on the way to it)
-  extern __shared__ __align__(16) unsigned char ring[];
-  unsigned *flag = reinterpret_cast<unsigned *>(ring);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, kw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
   const Place at = place(splits, tiles);
   const int tile = at.tile, split = at.split, m0 = at.z * 64;
   const int64_t nb0 = ((int64_t)tile * 4 + wave) * NB;
-  const int n_kb = (int)l.k_blocks, kb0 = (int)((int64_t)n_kb * split / splits), kb1 = (int)((int64_t)n_kb * (split + 1) / splits);
+  const int n_kb = (int)l.k_blocks, begin = (int)((int64_t)n_kb * split / splits), end = (int)((int64_t)n_kb * (split + 1) / splits);
+  // (all shares take as many steps: they meet at barriers)
+  const int n_steps = (end - begin + KW - 1) / KW, kb0 = begin + kw * n_steps, kb1 = min(kb0 + n_steps, end);
+  unsigned char *ring = lds + kw * (TILE_RING * BLK);
   const uint16_t *x[MB];
 #pragma unroll
   for (int i = 0; i < MB; ++i) x[i] = a.x + min(m0 + 16 * i + j, a.m - 1) * a.x_stride + 8 * g4;  // (rows past the last repeat it)
   // wavefront w brings step w of a block (past the inputs: the last step again, under scales of zero)
   auto request = [&](int kb) __attribute__((always_inline)) {
-    const int k0 = min(min(kb, kb1 - 1) * 128 + 32 * wave, a.k - 32);
+    const int k0 = min(min(kb, end - 1) * 128 + 32 * wave, a.k - 32);
 #pragma unroll
     for (int i = 0; i < MB; ++i) x_to_lds(x[i] + k0, ring + (kb % TILE_RING) * BLK + (wave * MB + i) * 1024);
   };
@@ -235,19 +246,18 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
   for (int b = 0; b < NB; ++b) {
     const int64_t nb = min(nb0 + b, l.n_blocks - 1);
     wp[b] = a.weight + nb * n_kb * 1024 + lane * 16;
-    gp[b] = nb * l.groups;
+    gp[b] = nb * n_kb;
   }
   struct Block {
     u32x4_t w[NB];
-    Group<ZEROS> g[NB][GPB];
+    Groups<GPB, ZEROS> g[NB];
   };
   auto load = [&](int kb, Block &f) __attribute__((always_inline)) {
-    const int k = min(kb, kb1 - 1);
+    const int k = min(kb, end - 1);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       f.w[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(wp[b] + (int64_t)k * 1024));
-#pragma unroll
-      for (int g = 0; g < GPB; ++g) f.g[b][g].load(a, l, gp[b] + k * GPB + g, g4);
+      f.g[b].load(a, l, gp[b] + k, j);
     }
   };
   f32x4_t y[NB][MB];
@@ -260,9 +270,7 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
   auto compute = [&](int kb, Block &f) __attribute__((always_inline)) {
     // scales are unpacked here, and not where they are loaded (which would wait for them there)
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int g = 0; g < GPB; ++g) f.g[b][g].here();
+    for (int b = 0; b < NB; ++b) f.g[b].here();
     const unsigned char *blk = ring + (kb % TILE_RING) * BLK + lane * 16;
 #pragma unroll
     for (int g = 0; g < GPB; ++g) {
@@ -278,33 +286,33 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
       for (int s = 0; s < STEPS; ++s)
 #pragma unroll
         for (int i = 0; i < MB; ++i) {
-          sum[i] = mfma<(MB < 3)>(sum[i], summing, xv[s][i]);
-          if (i == MB - 1) products_in_order();
+          sum[i] = mfma<(MB < 3)>(sum[i], xv[s][i], summing);
+          if (NB > 2 || i == MB - 1) products_in_order();
         }
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         f32x4_t d[MB];
 #pragma unroll
-        for (int i = 0; i < MB; ++i) d[i] = f.g[b][g].first(sum[i]);
+        for (int i = 0; i < MB; ++i) d[i] = f.g[b].first(g, j, sum[i]);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
           const bf16x8_t w = unpack(f.w[b][g * STEPS + s]);
 #pragma unroll
           for (int i = 0; i < MB; ++i) {
-            d[i] = mfma<(MB < 3)>(d[i], w, xv[s][i]);
-            if (i == MB - 1) products_in_order();
+            d[i] = mfma<(MB < 3)>(d[i], xv[s][i], w);
+            if (NB > 2 || i == MB - 1) products_in_order();
           }
         }
 #pragma unroll
         for (int i = 0; i < MB; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[b][i][r] = __builtin_fmaf(f.g[b][g].scale(r), d[i][r], y[b][i][r]);
+          for (int r = 0; r < 4; ++r) y[b][i][r] = __builtin_fmaf(f.g[b].scale(g, j), d[i][r], y[b][i][r]);
       }
     }
   };
   // Block kb: behind the barrier its x has landed for everybody, and the slot of block kb - 1 is free for kb + 3.  What may be
   // in flight still: x of kb + 2 and weights of kb + 1, asked for behind the weights of kb.
-  constexpr int IN_FLIGHT = MB + NB * (1 + GPB * (ZEROS ? 2 : 1));
+  constexpr int IN_FLIGHT = MB + NB * (ZEROS ? 3 : 2);
   static_assert(IN_FLIGHT < 64, "the counter's range");
   auto step = [&](int kb, Block &f) __attribute__((always_inline)) {
     asm volatile("" ::: "memory");
@@ -312,7 +320,7 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     request(kb + TILE_RING - 1);
-    compute(kb, f);
+    if (kb < kb1) compute(kb, f);
     __builtin_amdgcn_sched_barrier(0);
     load(kb + 2, f);
     __builtin_amdgcn_sched_barrier(0);
@@ -329,20 +337,39 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
   load(kb0 + 1, fb);
   __builtin_amdgcn_sched_barrier(0);
   int kb = kb0;
-  for (; kb + 1 < kb1; kb += 2) {
+  for (; kb + 1 < kb0 + n_steps; kb += 2) {
     step(kb, fa);
     step(kb + 1, fb);
   }
-  if (kb < kb1) step(kb, fa);
+  if (kb < kb0 + n_steps) step(kb, fa);
   __builtin_amdgcn_s_waitcnt(0x0F70);  // the look-ahead has landed before the LDS is released
+  {  // the first share's wavefronts add the second's
+    static_assert(KW == 2 && NB * MB * 4096 <= KW * TILE_RING * BLK, "room where x was");
+    __syncthreads();
+    f32x4_t *sums = reinterpret_cast<f32x4_t *>(lds) + (threadIdx.x & 255);
+    if (kw > 0)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) sums[(b * MB + i) * 256] = y[b][i];
+    __syncthreads();
+    if (kw == 0)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) y[b][i] += sums[(b * MB + i) * 256];
+    __syncthreads();
+  }
   if (splits > 1) {
     const __amdgpu_buffer_rsrc_t rs = parts_of(a.ws);
-    const unsigned step_bytes = NB * MB * 256 * 16u, part = (unsigned)(at.cell * splits) * step_bytes + threadIdx.x * 16u;
+    const unsigned step_bytes = NB * MB * 256 * 16u, part = (unsigned)(at.cell * splits) * step_bytes + (threadIdx.x & 255) * 16u;
+    if (kw == 0)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int i = 0; i < MB; ++i) put_part(rs, part + split * step_bytes + (b * MB + i) * 4096u, y[b][i]);
-    if (!last_of(a.counters + at.cell, splits, flag)) return;
+    if (!last_of(a.counters + at.cell, splits, reinterpret_cast<unsigned *>(lds))) return;
+    if (kw > 0) return;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -359,11 +386,11 @@ __global__ __launch_bounds__(256, 2) void w4_tile_kernel(const W4Args a, const W
         for (int i = 0; i < MB; ++i) y[b][i] += v[b][i];
     }
   }
-  const bool wide = wide_rows(a);
+  if (kw > 0) return;
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int i = 0; i < MB; ++i) store_four(a, m0 + 16 * i + j, (int)(nb0 + b) * 16 + 4 * g4, y[b][i], wide);
+    for (int i = 0; i < MB; ++i) store_four(a, m0 + 16 * i + 4 * g4, (int)(nb0 + b) * 16 + j, y[b][i]);
 }
 
 // products over no inputs
@@ -391,7 +418,8 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *packed, con
   }
   const int64_t e = i - n_words;
   if (e >= l.n_blocks * l.groups * 16) return;
-  const int64_t row = e / 16 / l.groups * 16 + e % 16, g = e / 16 % l.groups;
+  const int gpb = 128 / group;
+  const int64_t block = e / gpb / 16, row = block / l.k_blocks * 16 + e / gpb % 16, g = block % l.k_blocks * gpb + e % gpb;
   const bool in = row < n && g * group < k;
   reinterpret_cast<uint16_t *>(weight + l.scales)[e] = in ? scales[row * (k / group) + g] : (uint16_t)0;
   if (zeros) weight[l.zeros + e] = in ? zeros[row * (k / group) + g] : (unsigned char)0;
@@ -405,8 +433,6 @@ int within(const W4Args &a, int want, int64_t cells, int floats_per_part) {
   return std::max(1, (int)std::min<int64_t>(want, (int64_t)a.ws_floats / (cells * floats_per_part)));
 }
 
-constexpr int FEW_LDS = 128 * 1024;  // for x
-
 template <int GROUP, bool ZEROS, int KW, int U>
 hipError_t run_few(const W4Args &a, const W4Layout &l, int splits, hipStream_t stream) {
   const int tiles = ceil_div(l.n_blocks, 8 / KW), rows = a.m;
@@ -418,23 +444,29 @@ hipError_t run_few(const W4Args &a, const W4Layout &l, int splits, hipStream_t s
   return hipGetLastError();
 }
 
-template <int GROUP, bool ZEROS, int MB>
+template <int GROUP, bool ZEROS, int MB, int NB>
 hipError_t run_tile(const W4Args &a, const W4Layout &l, int splits, hipStream_t stream) {
-  const int tiles = ceil_div(l.n_blocks, 4 * TILE_NB), z = ceil_div(a.m, 64);
-  hipLaunchKernelGGL((w4_tile_kernel<GROUP, ZEROS, MB>), dim3((unsigned)(tiles * splits * z)), dim3(256), TILE_RING * 4 * MB * 1024, stream, a, l, splits,
-                     tiles);
+  constexpr int LDS = TILE_KW * TILE_RING * 4 * MB * 1024;
+  const int tiles = ceil_div(l.n_blocks, 4 * NB), z = ceil_div(a.m, 64);
+  static OncePerDevice once;
+  if (const hipError_t e = allow_lds(once, reinterpret_cast<const void *>(&w4_tile_kernel<GROUP, ZEROS, MB, NB>), LDS)) return e;
+  hipLaunchKernelGGL((w4_tile_kernel<GROUP, ZEROS, MB, NB>), dim3((unsigned)(tiles * splits * z)), dim3(256 * TILE_KW), LDS, stream, a, l, splits, tiles);
   return hipGetLastError();
 }
 
+// One workgroup a CU: so many share outputs, as long as each has five blocks of inputs (4096 x 4096, 61 rows: 6 workgroups 15.0 us, 8 15.8, 3
+// 16.9).  Where 32 outputs a wavefront would give more workgroups than CUs it takes 64, which also halve what it reads from LDS for
+// a product: 57344 x 8192, 61 rows 74 us for 89, 12 rows 48 for 51; 28672 x 4096, 61 rows on fewer CUs 31.4 for 28.0.
 template <int GROUP, bool ZEROS, int MB>
 hipError_t launch_tile(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  const int64_t cells = (int64_t)ceil_div(l.n_blocks, 4 * TILE_NB) * ceil_div(a.m, 64);
-  const int want = std::min(std::min(ceil_div(2 * a.n_cu, cells), 8), (int)l.k_blocks / 4);
-  return run_tile<GROUP, ZEROS, MB>(a, l, within(a, want, cells, TILE_NB * MB * 1024), stream);
+  const int64_t z = ceil_div(a.m, 64), cells = ceil_div(l.n_blocks, 8) * z;
+  if (cells > a.n_cu) return run_tile<GROUP, ZEROS, MB, 4>(a, l, 1, stream);
+  const int want = std::max(1, std::min(std::min(a.n_cu / (int)cells, 8), (int)l.k_blocks / 5));
+  return run_tile<GROUP, ZEROS, MB, 2>(a, l, within(a, want, cells, 2 * MB * 1024), stream);
 }
 
 // Few rows: how many wavefronts share the inputs of a block of outputs, and how many workgroups.  Timed on 9 shapes from 1536 x 2048 to
-// 57344 x 8192 with 1 to 16 rows, each with 1 to 8 wavefronts and 1 to 16 workgroups: one workgroup of eight where there are
+// 57344 x 8192 with 1 to 8 rows, each with 1 to 8 wavefronts and 1 to 16 workgroups: one workgroup of eight where there are
 // few blocks (4096 x 4096, one row 5.0 us; two wavefronts and four workgroups 6.5), else two wavefronts, and workgroups for about 3840 wavefronts
 // in all (28672 x 4096, 4 rows 15.3 us, one wavefront 17.1, four 16.4; 10240 x 8192 on three workgroups 14.2, eight wavefronts 15.4).
 template <int GROUP, bool ZEROS>
@@ -442,9 +474,7 @@ hipError_t launch_few(const W4Args &a, const W4Layout &l, hipStream_t stream) {
   const int nb = (int)l.n_blocks, kb = (int)l.k_blocks;
   const int kw = nb <= 256 || (a.m == 1 && nb < 1024) ? 8 : nb <= 448 ? 4 : 2;
   const int want = std::min(((kw == 8 ? 2048 : 3840) + nb * kw / 2) / (nb * kw), kb / (kw == 8 ? 8 : 20));
-  const int most_kb = std::max(1, (FEW_LDS / a.m / 2 - 8) / 128), fit = ceil_div(kb, most_kb);  // so many that x fits
-  const int splits = within(a, std::max(std::max(want, fit), 1), ceil_div(nb, 8 / kw), 8 / kw * 256);
-  if (splits < fit) return launch_tile<GROUP, ZEROS, 1>(a, l, stream);
+  const int splits = within(a, std::max(want, 1), ceil_div(nb, 8 / kw), 8 / kw * 256);
   if (kw == 2) return run_few<GROUP, ZEROS, 2, 2>(a, l, splits, stream);
   if (kw == 4) return run_few<GROUP, ZEROS, 4, 2>(a, l, splits, stream);
   // (a block at a time where a wavefront has four at most: 6144 x 4096 6.0 us, two at a time 6.4)
@@ -454,10 +484,10 @@ hipError_t launch_few(const W4Args &a, const W4Layout &l, hipStream_t stream) {
 
 template <int GROUP, bool ZEROS>
 hipError_t launch_group(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  // Beyond eight rows, three of large weights, a copy of x in every workgroup costs more than the tiles' ring: 8192 x 28672, 8 rows
-  // 28.9 us against 26.9, 57344 x 8192 64 against 49; 4096 x 4096 6.6 against 8.7.
-  const bool large = l.n_blocks * l.k_blocks >= 96 << 10;
-  if (a.m <= (large ? 3 : 8)) return launch_few<GROUP, ZEROS>(a, l, stream);
+  // Each workgroup's copy of x costs more than the tiles' ring beyond eight rows (10240 x 8192, 8 rows 15.3 us, tiles 15.0; 28672 x 4096 16.9
+  // against 17.5), where x does not fit into LDS whole (4096 x 14336, 4 rows 12.8 against 13.4, 6 rows 18.3 against 13.4), and where
+  // every CU has a tile of its own (57344 x 8192, 2 rows 54.5 against 52.4).
+  if (a.m <= 8 && a.m * l.k_blocks <= 512 && l.n_blocks <= 8 * a.n_cu) return launch_few<GROUP, ZEROS>(a, l, stream);
   if (a.m <= 16) return launch_tile<GROUP, ZEROS, 1>(a, l, stream);
   if (a.m <= 32) return launch_tile<GROUP, ZEROS, 2>(a, l, stream);
   if (a.m <= 48) return launch_tile<GROUP, ZEROS, 3>(a, l, stream);

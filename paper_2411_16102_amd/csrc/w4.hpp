@@ -4,8 +4,8 @@
 // and k hold zeros.  A block is 1 KB, 16 bytes for each of 64 lanes: lane (j = lane % 16, g = lane / 16) holds,
 // in 32-bit word s, inputs 32 s + 8 g .. + 7 of output j, the operand of one 16x16x32 matrix instruction.  Within a word the
 // even inputs stand in the low 16 bits, the odd ones in the high 16 (nibble i: input 2 i, nibble i + 4: input
-// 2 i + 1), so that shifting and masking yields pairs of neighbours.  Behind the blocks come the scales, [16 outputs' block][group][16] bf16,
-// and, where there are any, the zero points in the same order, a byte each.
+// 2 i + 1), so that shifting and masking yields pairs of neighbours.  Behind the blocks come the scales, for each block [16 outputs][groups of
+// 128 inputs] bf16, so that a lane has those of its output in one load, and, where there are any, the zero points in the same order, a byte each.
 #pragma once
 #include <stdint.h>
 #include <hip/hip_runtime.h>

@@ -295,6 +295,17 @@ def test_w4_linear(lib, m, n, k, group, zeros):
     _w4(lib, m, n, k, group, zeros)
 
 
+@pytest.mark.parametrize("m,n,k,group,zeros", [(1, 33000, 256, 128, True), (9, 32785, 384, 64, False), (30, 40003, 160, 32, True), (40, 32800, 640, 128, False),
+                                               (61, 33001, 384, 64, True), (61, 32900, 1280, 64, False), (130, 16500, 384, 128, True)])
+def test_w4_more_tiles_than_cus(lib, m, n, k, group, zeros):
+    _w4(lib, m, n, k, group, zeros)
+
+
+@pytest.mark.parametrize("m,k", [(8, 8192), (8, 8320), (3, 21888), (1, 65536), (1, 65664)])
+def test_w4_inputs_that_just_fit(lib, m, k):
+    _w4(lib, m, 70, k, 128, True)
+
+
 @pytest.mark.parametrize("k,group", [(32, 32), (96, 32), (64, 64), (192, 64), (160, 32), (0, 128)])
 def test_w4_inputs_that_end_inside_a_block(lib, k, group):
     _w4(lib, 3, 50, k, group, True)
