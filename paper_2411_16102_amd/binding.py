@@ -263,6 +263,7 @@ class Layer:
         # of every call on streams
         self._bf16_type = torch.bfloat16
         self._q_width = shape.n_q_heads * shape.head_dim
+        self._qkv_width = shape.n_qkv
         self._page_elems = self.page_bytes() // 2
 
     def close(self):
@@ -469,35 +470,40 @@ class Layer:
     def window_attention(self, plan: "WindowPlan", q, kv_pool, out=None, stream=None):
         """Sliding-window attention with sinks of the plan's rows; q and out: [n_rows, Hq * dh] bf16, rows at any stride."""
         width = self._q_width
-        self._check_rows(plan, q, width)
+        q_stride = self._row_stride(plan, q, width)
         if out is None:
-            out = q.new_empty((plan.n_rows, width))
+            out, out_stride = q.new_empty((plan.n_rows, width)), width
         else:
-            self._check_rows(plan, out, width)
+            out_stride = self._row_stride(plan, out, width)
         self._check_pool(plan, kv_pool)
-        self._check(self.lib.bs_window_attention(plan.h, q.data_ptr(), q.stride(0), out.data_ptr(), out.stride(0), kv_pool.data_ptr(),
-                                                 self._raw_stream(stream)))
+        rc = self.lib.bs_window_attention(plan.h, q.data_ptr(), q_stride, out.data_ptr(), out_stride, kv_pool.data_ptr(), self._raw_stream(stream))
+        if rc:
+            self._check(rc)
         return out
 
     def rope_append(self, plan: "WindowPlan", qkv, kv_pool, q=None, stream=None):
         """Turns queries and keys of fused rows [n_rows, (Hq + 2 Hkv) * dh] and appends keys and values to kv_pool; the
         turned queries [n_rows, Hq * dh] (q: where they go; qkv[:, :Hq * dh] for in place)."""
-        self._check_rows(plan, qkv, self.shape.n_qkv)
+        stride = self._row_stride(plan, qkv, self._qkv_width)
         if q is None:
-            q = qkv.new_empty((plan.n_rows, self._q_width))
+            q, q_stride = qkv.new_empty((plan.n_rows, self._q_width)), self._q_width
         else:
-            self._check_rows(plan, q, self._q_width)
+            q_stride = self._row_stride(plan, q, self._q_width)
         self._check_pool(plan, kv_pool)
-        self._check(self.lib.bs_rope_append(plan.h, qkv.data_ptr(), qkv.stride(0), q.data_ptr(), q.stride(0), kv_pool.data_ptr(),
-                                            self._raw_stream(stream)))
+        rc = self.lib.bs_rope_append(plan.h, qkv.data_ptr(), stride, q.data_ptr(), q_stride, kv_pool.data_ptr(), self._raw_stream(stream))
+        if rc:
+            self._check(rc)
         return q
 
     def _raw_stream(self, stream):
         return _current_stream(self.device) if stream is None else stream.cuda_stream
 
-    def _check_rows(self, plan, t, width):
-        if t.dtype is not self._bf16_type or tuple(t.shape) != (plan.n_rows, width) or t.stride(1) != 1:
-            raise ValueError("expected bf16 rows [%d, %d], got %s %s" % (plan.n_rows, width, t.dtype, tuple(t.shape)))
+    def _row_stride(self, plan, t, width):
+        if t.dtype is self._bf16_type and t.shape == (plan.n_rows, width):
+            stride, inner = t.stride()
+            if inner == 1:
+                return stride
+        raise ValueError("expected bf16 rows [%d, %d], got %s %s" % (plan.n_rows, width, t.dtype, tuple(t.shape)))
 
     def _check_pool(self, plan, kv_pool):
         if kv_pool.dtype is not self._bf16_type or not kv_pool.is_contiguous() or kv_pool.numel() < plan.n_pages * self._page_elems:
@@ -523,15 +529,25 @@ class Layer:
 
     def w4_linear(self, x, weight: "W4Weight", out=None, stream=None):
         """x [m, k] bf16 times a laid-out 4-bit weight: [m, n] bf16."""
-        if x.dtype is not self._bf16_type or x.dim() != 2 or x.shape[1] != weight.k or (x.stride(1) != 1 and x.numel()):
-            raise ValueError("w4_linear: bf16 rows of %d inputs, got %s %s" % (weight.k, x.dtype, tuple(x.shape)))
-        m = x.shape[0]
+        shape = x.shape
+        if x.dtype is not self._bf16_type or len(shape) != 2 or shape[1] != weight.k:
+            raise ValueError("w4_linear: bf16 rows of %d inputs, got %s %s" % (weight.k, x.dtype, tuple(shape)))
+        m = shape[0]
+        stride, inner = x.stride()
+        if not m or not weight.k:
+            stride = 0
+        elif inner != 1:
+            raise ValueError("w4_linear: rows of x are not contiguous")
         if out is None:
-            out = x.new_empty((m, weight.n))
-        elif out.dtype != x.dtype or tuple(out.shape) != (m, weight.n) or out.stride(1) != 1:
-            raise ValueError("w4_linear: out is not bf16 [%d, %d]" % (m, weight.n))
-        self._check(self.lib.bs_w4_linear(self.h, x.data_ptr(), x.stride(0) if x.numel() else 0, weight.data.data_ptr(), m, weight.n, weight.k, weight.group,
-                                          weight.with_zeros, out.data_ptr(), out.stride(0), self._raw_stream(stream)))
+            out, out_stride = x.new_empty((m, weight.n)), weight.n
+        else:
+            if out.dtype is not x.dtype or out.shape != (m, weight.n) or out.stride(1) != 1:
+                raise ValueError("w4_linear: out is not bf16 [%d, %d]" % (m, weight.n))
+            out_stride = out.stride(0)
+        rc = self.lib.bs_w4_linear(self.h, x.data_ptr(), stride, weight.data.data_ptr(), m, weight.n, weight.k, weight.group, weight.with_zeros, out.data_ptr(),
+                                   out_stride, self._raw_stream(stream))
+        if rc:
+            self._check(rc)
         return out
 
     def _pools(self, pools):
