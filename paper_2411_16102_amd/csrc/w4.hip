@@ -105,7 +105,8 @@ struct Groups {
 
 // ---- up to 8 rows: a workgroup of eight wavefronts, 8 / KW of them blocks of 16 outputs, KW a share each of the inputs ----
 // x of the workgroup's inputs lies in LDS, so that the vector memory path carries weights alone and wavefronts do not wait for each
-// other behind the first barrier; a wavefront has U blocks of weights in use and U on the way.
+// other behind the first barrier; a wavefront has U blocks of weights in use and U on the way.  Bound by reading the weights: 28672 x 4096 with
+// zero points (62 MB) one row 14.3 us, 7 rows 16.7 (a kernel that only reads as much: 10); 6144 x 4096 5.4 us, of which 2.2 are a launch.
 template <int GROUP, bool ZEROS, int KW, int U>
 __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Layout l, int splits, int tiles, int x_row) {
   constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32, NW = 8 / KW;  // groups of a block of inputs, matrix instructions of a group

@@ -18,6 +18,11 @@ using namespace attn_dev;
 // computed while the other is on the way.  Elements that no row of the unit sees are never multiplied into a result: scores
 // become -inf, values zero (a slot that was never written may hold NaN, and zero times NaN is NaN); pairs that all
 // rows see whole, which is most of them, need neither.
+//
+// Probabilities are rounded to bf16 for their product with V (at most 2^-8 of the sum of p |v|, as elsewhere in this
+// library); scores, statistics and accumulators are 32 bits wide.  Bound by reading the pages: 256 streams of window 1024, 8 KV
+// heads (1.07 GB) take 175 us, 6.1 TB/s, what reads alone reach; 129 streams and two segments of a 64-wide layer (141 MB) 29 us, 4.9 TB/s; one
+// stream 8.7 us: a launch, a round trip each for the plan, the pages and the join.
 template <int DH>
 struct Columns {  // the softmax of a wavefront's columns
   f32x4_t o[DH / 16];
