@@ -209,10 +209,11 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
 // blocks of 128 inputs that its four wavefronts read; weights go straight to registers, two blocks before they are used.  The shares keep
 // two wavefronts on a SIMD, of which one computes while the other waits for LDS (half the wavefronts: 81 us for 51 at 8192 x 28672, 61 rows), and
 // are added up in LDS, which two workgroups would do through memory (53 us).
-// What bounds it: products and reads of LDS together.  A block is 12 MB products of a wavefront (a third of them the sum of x, which takes the place
-// of unpacking to signed numbers: twice the instructions) beside 4 MB reads of 1 KB, which a CU answers at 64 bytes a clock.  For 8192 x 28672, 61 rows
-// those are 21 and 25 us, the weights from memory 27, and all of it 50.5: 2.5 TB/s of weights, 0.85 PFLOP/s with the sums.  With up to 16 rows it is
-// bound by memory: 8192 x 28672 28 us, 4.4 TB/s.
+// What bounds it: issuing products and vector arithmetic.  A block is 12 MB products of a wavefront (a third of them the sum of x, which takes the
+// place of unpacking to signed numbers: twice the instructions), three vector instructions for each and 4 MB reads of LDS; by themselves 12
+// products take a SIMD 98 ns, with 36 vector instructions and 4 reads 146.  For 8192 x 28672, 61 rows that makes 33 us (the weights from memory
+// 27), to which come a launch, the first loads, waits at barriers and 4 us of joining: 50.5 to 53 us, 2.4 TB/s of weights, 0.8 PFLOP/s with
+// the sums.  With up to 16 rows it is bound by memory: 8192 x 28672 28 us, 4.4 TB/s.
 constexpr int TILE_RING = 4, TILE_KW = 2;
 
 __device__ __forceinline__ void x_to_lds(const void *src, unsigned char *lds) {
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(256 * TILE_KW, 2) void w4_tile_kernel(const W4Args 
         for (int i = 0; i < MB; ++i) y[b][i] += sums[(b * MB + i) * 256];
     __syncthreads();
   }
-  if (splits > 1) {
+  if (NB == 2 && splits > 1) {  // (64 outputs a wavefront are never shared: parts of 64 KB take 9 us to join)
     const __amdgpu_buffer_rsrc_t rs = parts_of(a.ws);
     const unsigned step_bytes = NB * MB * 256 * 16u, part = (unsigned)(at.cell * splits) * step_bytes + (threadIdx.x & 255) * 16u;
     if (kw == 0)
@@ -456,8 +457,8 @@ hipError_t run_tile(const W4Args &a, const W4Layout &l, int splits, hipStream_t 
 }
 
 // One workgroup a CU: so many share outputs, as long as each has five blocks of inputs (4096 x 4096, 61 rows: 6 workgroups 15.0 us, 8 15.8, 3
-// 16.9).  Where 32 outputs a wavefront would give more workgroups than CUs it takes 64, which also halve what it reads from LDS for
-// a product: 57344 x 8192, 61 rows 74 us for 89, 12 rows 48 for 51; 28672 x 4096, 61 rows on fewer CUs 31.4 for 28.0.
+// 16.9).  Where 32 outputs a wavefront would give more workgroups than CUs it takes 64, which also need fewer sums of x
+// for a product: 57344 x 8192, 61 rows 74 us for 89, 12 rows 48 for 51; 28672 x 4096, 61 rows on fewer CUs 31.4 for 28.0.
 template <int GROUP, bool ZEROS, int MB>
 hipError_t launch_tile(const W4Args &a, const W4Layout &l, hipStream_t stream) {
   const int64_t z = ceil_div(a.m, 64), cells = ceil_div(l.n_blocks, 8) * z;
