@@ -103,13 +103,14 @@ struct Groups {
   }
 };
 
-// ---- up to 8 rows: a workgroup of eight wavefronts, 8 / KW of them blocks of 16 outputs, KW a share each of the inputs ----
+// ---- up to 16 rows: a workgroup takes up to eight blocks of 16 outputs, each on KW wavefronts, a share of the inputs each ----
 // x of the workgroup's inputs lies in LDS, so that the vector memory path carries weights alone and wavefronts do not wait for each
 // other behind the first barrier; a wavefront has U blocks of weights in use and U on the way.  Bound by reading the weights: 28672 x 4096 with
-// zero points (62 MB) one row 14.3 us, 7 rows 16.7 (a kernel that only reads as much: 10); 6144 x 4096 5.4 us, of which 2.2 are a launch.
+// zero points (62 MB) one row 14.4 us, 8 rows 15.7 to 16.3 (a kernel that only reads as much: 10); 6144 x 4096 5.4 us, of which 2.2 are a launch.
 template <int GROUP, bool ZEROS, int KW, int U>
-__global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Layout l, int splits, int tiles, int x_row) {
-  constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32, NW = 8 / KW;  // groups of a block of inputs, matrix instructions of a group
+__global__ __launch_bounds__(1024) void w4_few_kernel(const W4Args a, const W4Layout l, int splits, int tiles, int x_row) {
+  constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32;  // groups of a block of inputs, matrix instructions of a group
+  const int threads = blockDim.x, NW = threads / (64 * KW);  // blocks of outputs
   extern __shared__ __align__(16) unsigned char lds[];
   uint16_t *xs = reinterpret_cast<uint16_t *>(lds);  // [rows][x_row]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
   __builtin_amdgcn_sched_barrier(0);
   {  // inputs [128 first, 128 (first + n_mine)) of the rows; zeros past the last
     const int per_row = n_mine * 16;
-    for (int i = threadIdx.x; i < rows * per_row; i += 512) {
+    for (int i = threadIdx.x; i < rows * per_row; i += threads) {
       const int r = i / per_row, c = i % per_row, k = first * 128 + c * 8;
       u32x4_t v = {0u, 0u, 0u, 0u};
       if (k < a.k) v = *reinterpret_cast<const u32x4_t *>(a.x + r * a.x_stride + k);
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(512) void w4_few_kernel(const W4Args a, const W4Lay
     const __amdgpu_buffer_rsrc_t rs = parts_of(a.ws);
     const unsigned part = (unsigned)((at.cell * splits * NW + wave / KW) * 64 + lane) * 16u, step = NW * 64 * 16u;
     if (mine) put_part(rs, part + split * step, y);
-    if (!last_of(a.counters + at.cell, splits, reinterpret_cast<unsigned *>(lds + 512 * 16))) return;
+    if (!last_of(a.counters + at.cell, splits, reinterpret_cast<unsigned *>(lds + threads * 16))) return;
     if (mine) {
       y = f32x4_t{0.f, 0.f, 0.f, 0.f};
       for (int i = 0; i < splits; ++i) y += get_part(rs, part + i * step);
@@ -436,13 +437,13 @@ int within(const W4Args &a, int want, int64_t cells, int floats_per_part) {
 }
 
 template <int GROUP, bool ZEROS, int KW, int U>
-hipError_t run_few(const W4Args &a, const W4Layout &l, int splits, hipStream_t stream) {
-  const int tiles = ceil_div(l.n_blocks, 8 / KW), rows = a.m;
-  const int x_row = ceil_div(l.k_blocks, splits) * 128 + 8, lds = std::max(rows * x_row * 2, 512 * 16 + 16);
+hipError_t run_few(const W4Args &a, const W4Layout &l, int blocks, int splits, hipStream_t stream) {
+  const int tiles = ceil_div(l.n_blocks, blocks), rows = a.m, threads = blocks * KW * 64;
+  const int x_row = ceil_div(l.k_blocks, splits) * 128 + 8, lds = std::max(rows * x_row * 2, threads * 16 + 16);
   static OncePerDevice once;
   if (const hipError_t e = allow_lds(once, reinterpret_cast<const void *>(&w4_few_kernel<GROUP, ZEROS, KW, U>), 160 * 1024)) return e;
   if (lds > 160 * 1024) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((w4_few_kernel<GROUP, ZEROS, KW, U>), dim3((unsigned)(tiles * splits)), dim3(512), lds, stream, a, l, splits, tiles, x_row);
+  hipLaunchKernelGGL((w4_few_kernel<GROUP, ZEROS, KW, U>), dim3((unsigned)(tiles * splits)), dim3(threads), lds, stream, a, l, splits, tiles, x_row);
   return hipGetLastError();
 }
 
@@ -467,29 +468,26 @@ hipError_t launch_tile(const W4Args &a, const W4Layout &l, hipStream_t stream) {
   return run_tile<GROUP, ZEROS, MB, 2>(a, l, within(a, want, cells, 2 * MB * 1024), stream);
 }
 
-// Few rows: how many wavefronts share the inputs of a block of outputs, and how many workgroups.  Timed on 9 shapes from 1536 x 2048 to
-// 57344 x 8192 with 1 to 8 rows, each with 1 to 8 wavefronts and 1 to 16 workgroups: one workgroup of eight where there are
-// few blocks (4096 x 4096, one row 5.0 us; two wavefronts and four workgroups 6.5), else two wavefronts, and workgroups for about 3840 wavefronts
-// in all (28672 x 4096, 4 rows 15.3 us, one wavefront 17.1, four 16.4; 10240 x 8192 on three workgroups 14.2, eight wavefronts 15.4).
+// Few rows: one workgroup a CU of as many blocks of outputs as it takes, up to 16 wavefronts, two to eight of them to a block. Where there are
+// fewer blocks than CUs workgroups share outputs, as long as each of their wavefronts has a block of inputs, or four where half the CUs have
+// work anyway.  Timed on 9 shapes from 4096 x 4096 to 28672 x 8192 with 1 to 8 rows, each with 1 to 8 blocks, 2 to 8 wavefronts
+// and 1 to 8 workgroups: 28672 x 8192, 4 rows 26.5 us, in workgroups of four blocks 30.7; 10240 x 8192 13.1, eight blocks on three workgroups
+// 14.5; 6144 x 4096 7.0, one block 7.2; 4096 x 14336 on two workgroups 11.2, on one 12.6 (4096 x 4096 6.7 and 5.9).
 template <int GROUP, bool ZEROS>
 hipError_t launch_few(const W4Args &a, const W4Layout &l, hipStream_t stream) {
   const int nb = (int)l.n_blocks, kb = (int)l.k_blocks;
-  const int kw = nb <= 256 || (a.m == 1 && nb < 1024) ? 8 : nb <= 448 ? 4 : 2;
-  const int want = std::min(((kw == 8 ? 2048 : 3840) + nb * kw / 2) / (nb * kw), kb / (kw == 8 ? 8 : 20));
-  const int splits = within(a, std::max(want, 1), ceil_div(nb, 8 / kw), 8 / kw * 256);
-  if (kw == 2) return run_few<GROUP, ZEROS, 2, 2>(a, l, splits, stream);
-  if (kw == 4) return run_few<GROUP, ZEROS, 4, 2>(a, l, splits, stream);
-  // (a block at a time where a wavefront has four at most: 6144 x 4096 6.0 us, two at a time 6.4)
-  if (kb <= 32 * splits) return run_few<GROUP, ZEROS, 8, 1>(a, l, splits, stream);
-  return run_few<GROUP, ZEROS, 8, 2>(a, l, splits, stream);
+  const int want = nb > a.n_cu ? 1 : nb > a.n_cu / 2 ? (kb >= 64 ? 2 : 1) : std::max(1, std::min(a.n_cu / nb, kb / 8));
+  const int splits = within(a, want, nb, 256), blocks = ceil_div((int64_t)nb * splits, a.n_cu);
+  if (blocks <= 2) return run_few<GROUP, ZEROS, 8, 1>(a, l, blocks, splits, stream);
+  if (blocks <= 4) return run_few<GROUP, ZEROS, 4, 2>(a, l, blocks, splits, stream);
+  return run_few<GROUP, ZEROS, 2, 2>(a, l, blocks, splits, stream);
 }
 
 template <int GROUP, bool ZEROS>
 hipError_t launch_group(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  // Each workgroup's copy of x costs more than the tiles' ring beyond eight rows (10240 x 8192, 8 rows 15.3 us, tiles 15.0; 28672 x 4096 16.9
-  // against 17.5), where x does not fit into LDS whole (4096 x 14336, 4 rows 12.8 against 13.4, 6 rows 18.3 against 13.4), and where
-  // every CU has a tile of its own (57344 x 8192, 2 rows 54.5 against 52.4).
-  if (a.m <= 8 && a.m * l.k_blocks <= 512 && l.n_blocks <= 8 * a.n_cu) return launch_few<GROUP, ZEROS>(a, l, stream);
+  // One operand's rows, where x fits into LDS whole and no CU needs a second workgroup: 6144 x 4096, 16 rows 8.5 us, in tiles 9.5;
+  // 28672 x 8192, 8 rows 28.1 against 31.0.  Else tiles (57344 x 8192, 2 rows, 14 blocks a CU: 52.4 against 54.5).
+  if (a.m <= 16 && a.m * l.k_blocks <= 600 && l.n_blocks <= 8 * a.n_cu) return launch_few<GROUP, ZEROS>(a, l, stream);
   if (a.m <= 16) return launch_tile<GROUP, ZEROS, 1>(a, l, stream);
   if (a.m <= 32) return launch_tile<GROUP, ZEROS, 2>(a, l, stream);
   if (a.m <= 48) return launch_tile<GROUP, ZEROS, 3>(a, l, stream);

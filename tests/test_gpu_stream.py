@@ -301,6 +301,17 @@ def test_w4_more_tiles_than_cus(lib, m, n, k, group, zeros):
     _w4(lib, m, n, k, group, zeros)
 
 
+@pytest.mark.parametrize("m,k", [(16, 4736), (16, 4864), (9, 8448), (9, 8576), (1, 76800), (1, 76928)])
+def test_w4_rows_that_fill_the_lds(lib, m, k):
+    _w4(lib, m, 35, k, 128, True)
+
+
+@pytest.mark.parametrize("n", [16 * 255 + 1, 16 * 256 + 1, 16 * 512 + 1, 16 * 1024 + 16, 16 * 2048, 16 * 2048 + 1])
+@pytest.mark.parametrize("m,k,group", [(1, 384, 128), (9, 544, 32), (16, 256, 64), (17, 320, 64)])
+def test_w4_blocks_of_a_cu(lib, n, m, k, group):
+    _w4(lib, m, n, k, group, n % 2 == 1)
+
+
 @pytest.mark.parametrize("m,k", [(8, 8192), (8, 8320), (3, 21888), (1, 65536), (1, 65664)])
 def test_w4_inputs_that_just_fit(lib, m, k):
     _w4(lib, m, 70, k, 128, True)
