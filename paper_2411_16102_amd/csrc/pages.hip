@@ -62,15 +62,15 @@ int bs_kv_copy_pages(bs_ctx *c, void *const *pools, int32_t n_pools, int64_t n_p
   return ctx_guarded(c, [&]() -> int {
     if (const int rc = check_pools(c, pools, n_pools, n_pages)) return rc;
     if (n < 0 || (n > 0 && (!src || !dst))) return ctx_fail(c, BS_EINVAL, "bs_kv_copy_pages: bad list of %d pairs", n);
-    std::vector<char> mark((size_t)n_pages, 0);
-    for (int i = 0; i < n; ++i) {
+    for (int i = 0; i < n; ++i)
       if (src[i] < 0 || src[i] >= n_pages || dst[i] < 0 || dst[i] >= n_pages)
         return ctx_fail(c, BS_EINVAL, "pair %d (%d, %d) outside the pool of %lld pages", i, src[i], dst[i], (long long)n_pages);
-      if (mark[dst[i]]) return ctx_fail(c, BS_EINVAL, "page %d is copied to twice", dst[i]);
-      mark[dst[i]] = 1;
-    }
+    std::vector<int32_t> to(dst, dst + n);
+    std::sort(to.begin(), to.end());
+    const auto twice = std::adjacent_find(to.begin(), to.end());
+    if (twice != to.end()) return ctx_fail(c, BS_EINVAL, "page %d is copied to twice", *twice);
     for (int i = 0; i < n; ++i)
-      if (mark[src[i]]) return ctx_fail(c, BS_EINVAL, "page %d is copied from and to", src[i]);
+      if (std::binary_search(to.begin(), to.end(), src[i])) return ctx_fail(c, BS_EINVAL, "page %d is copied from and to", src[i]);
     return copy_pairs(c, pools, n_pools, src, dst, n, (hipStream_t)stream);
   });
 }

@@ -80,21 +80,30 @@ int check_batch(bs_ctx *c, const bs_batch *b, int64_t n_pages) {
   return BS_OK;
 }
 
-// pages that a step appends to are there, and named once
+// pages that a step appends to are there, and named once (refs: zero between calls, so that a plan costs what it names, not what the pool has)
 int check_appends(bs_window *w, const bs_batch *b, int64_t n_pages) {
-  w->refs.assign((size_t)n_pages, 0);
-  for (int i = 0; b->n_seq > 0 && i < b->page_start[b->n_seq]; ++i)
-    if (b->page_ids[i] >= 0) ++w->refs[b->page_ids[i]];
-  for (int s = 0; s < b->n_seq; ++s) {
-    const int rows = b->row_start[s + 1] - b->row_start[s];
-    if (rows == 0 || b->kv_len[s] == 0) continue;
-    for (int pg = std::max(0, b->kv_len[s] - rows) / PAGE; pg <= (b->kv_len[s] - 1) / PAGE; ++pg) {
-      const int id = b->page_ids[b->page_start[s] + pg];
-      if (id < 0) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d appends to page %d of its table, which was given up", s, pg);
-      if (w->refs[id] != 1) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d appends into page %d, which is referenced more than once", s, id);
+  const int named = b->n_seq > 0 ? b->page_start[b->n_seq] : 0;
+  if (w->refs.size() < (size_t)n_pages) w->refs.resize((size_t)n_pages, 0);
+  const auto count = [&](int by) {
+    for (int i = 0; i < named; ++i)
+      if (b->page_ids[i] >= 0) w->refs[b->page_ids[i]] += by;
+  };
+  const auto check = [&]() -> int {
+    for (int s = 0; s < b->n_seq; ++s) {
+      const int rows = b->row_start[s + 1] - b->row_start[s];
+      if (rows == 0 || b->kv_len[s] == 0) continue;
+      for (int pg = std::max(0, b->kv_len[s] - rows) / PAGE; pg <= (b->kv_len[s] - 1) / PAGE; ++pg) {
+        const int id = b->page_ids[b->page_start[s] + pg];
+        if (id < 0) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d appends to page %d of its table, which was given up", s, pg);
+        if (w->refs[id] != 1) return ctx_fail(w->ctx, BS_EINVAL, "sequence %d appends into page %d, which is referenced more than once", s, id);
+      }
     }
-  }
-  return BS_OK;
+    return BS_OK;
+  };
+  count(1);
+  const int rc = check();
+  count(-1);
+  return rc;
 }
 
 // The pages that rows at positions [p0, p1] see: the first n_sink, then [first, last].
@@ -561,9 +570,9 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     if (const int rc = grow(c, &w->d_states, &w->cap_states, p.state_floats, sizeof(float))) return fail_with(rc);
     if (p.states * g.n_kv_heads > w->cap_counters) {
       if (const int rc = grow(c, &w->d_counters, &w->cap_counters, p.states * g.n_kv_heads, sizeof(unsigned))) return fail_with(rc);
-      if (hipError_t e = hipMemset(w->d_counters, 0, sizeof(unsigned) * (size_t)w->cap_counters)) {
+      if (hipError_t e = hipMemsetAsync(w->d_counters, 0, sizeof(unsigned) * (size_t)w->cap_counters, st)) {
         w->cap_counters = 0;
-        return fail_with(ctx_fail(c, BS_EHIP, "hipMemset: %s", hipGetErrorString(e)));
+        return fail_with(ctx_fail(c, BS_EHIP, "hipMemsetAsync: %s", hipGetErrorString(e)));
       }
     }
     int32_t *pinned = nullptr;
