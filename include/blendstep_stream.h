@@ -97,7 +97,8 @@ int bs_w4_pack(bs_ctx *ctx, const void *packed, const void *scales, const void *
                void *weight, void *stream);
 
 /* x: device bf16, row i at x + i * x_stride elements (x_stride a multiple of 8, 16-byte aligned); y: device bf16, row i at
- * y + i * y_stride; with_zeros as the weight was packed.  Sums in 32 bits, y rounded once.  The calls on one context share
+ * y + i * y_stride; with_zeros as the weight was packed.  Sums in 32 bits, y rounded once.  (They carry an offset of the weights that
+ * cancels: an infinity in a row of x makes its outputs NaN, and sums of 143 |x| have to be in range.)  The calls on one context share
  * a workspace and must not overlap in time on different streams. */
 int bs_w4_linear(bs_ctx *ctx, const void *x, int64_t x_stride, const void *weight, int64_t m, int64_t n, int64_t k, int32_t group,
                  int32_t with_zeros, void *y, int64_t y_stride, void *stream);

@@ -501,7 +501,7 @@ class Layer:
     def _row_stride(self, plan, t, width):
         if t.dtype is self._bf16_type and t.shape == (plan.n_rows, width):
             stride, inner = t.stride()
-            if inner == 1:
+            if inner == 1 or not plan.n_rows:
                 return stride
         raise ValueError("expected bf16 rows [%d, %d], got %s %s" % (plan.n_rows, width, t.dtype, tuple(t.shape)))
 

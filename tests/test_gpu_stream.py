@@ -144,6 +144,15 @@ def test_pages_given_up_and_strided_rows(lib):
     _attention(lib, shape, batch, 100, 20, q_stride=8 * 64 + 2 * 2 * 64)
 
 
+def test_steps_without_rows(lib):
+    import torch
+    layer, _, _, _, out = _attention(lib, W.LayerShape(256, 3, 1, 64, 256), make_batch([(0, 40), (0, 0)]), 16, 2)
+    assert tuple(out.shape) == (0, 192)
+    plan = layer.window_plan(make_batch([], spare=0), 16, 2)
+    pool = torch.zeros(0, device="cuda", dtype=torch.bfloat16)
+    assert layer.rope_append(plan, torch.zeros((0, 5 * 64), device="cuda", dtype=torch.bfloat16), pool).shape == (0, 192)
+
+
 def test_in_place_and_strided_results_equal(lib):
     import torch
     shape = W.LayerShape(256, 8, 2, 64, 256)
