@@ -457,15 +457,26 @@ hipError_t run_tile(const W4Args &a, const W4Layout &l, int splits, hipStream_t 
   return hipGetLastError();
 }
 
-// One workgroup a CU: so many share outputs, as long as each has five blocks of inputs (4096 x 4096, 61 rows: 6 workgroups 15.0 us, 8 15.8, 3
-// 16.9).  Where 32 outputs a wavefront would give more workgroups than CUs it takes 64, which also need fewer sums of x
-// for a product: 57344 x 8192, 61 rows 74 us for 89, 12 rows 48 for 51; 28672 x 4096, 61 rows on fewer CUs 31.4 for 28.0.
+// How many workgroups share outputs, by expected microseconds: rounds of workgroups on the chip, in each a start and its share's steps of one block,
+// and the join, which one workgroup does.  At least five blocks for a workgroup.  61 rows: 4096 x 4096 on 6 workgroups 15.0 us, 3 16.9; 17000 x 8192, 133
+// tiles, on 3 in two rounds 44.2, on one 47.5 (30 rows 29.2 and 36.9).  Where 32 outputs a wavefront would give more workgroups than CUs it takes
+// 64, which also need fewer sums of x for a product: 57344 x 8192, 61 rows 74 us for 89, 12 rows 48 for 51; 28672 x 4096, 61 rows
+// on fewer CUs 31.4 for 28.0.
 template <int GROUP, bool ZEROS, int MB>
 hipError_t launch_tile(const W4Args &a, const W4Layout &l, hipStream_t stream) {
   const int64_t z = ceil_div(a.m, 64), cells = ceil_div(l.n_blocks, 8) * z;
   if (cells > a.n_cu) return run_tile<GROUP, ZEROS, MB, 4>(a, l, 1, stream);
-  const int want = std::max(1, std::min(std::min(a.n_cu / (int)cells, 8), (int)l.k_blocks / 5));
-  return run_tile<GROUP, ZEROS, MB, 2>(a, l, within(a, want, cells, 2 * MB * 1024), stream);
+  int splits = 1;
+  double best = 0;
+  for (int s = 1; s <= 8 && (s == 1 || (int)l.k_blocks >= 5 * s); ++s) {
+    const int rounds = ceil_div(cells * s, a.n_cu), steps = ceil_div(ceil_div(l.k_blocks, s), 2);
+    const double us = rounds * (2.5 + (0.65 + 0.2 * MB) * (GROUP == 32 ? 1.25 : 1.0) * steps) + (s > 1 ? 2.5 + 0.65 * s : 0.0);
+    if (s == 1 || us < best) {
+      best = us;
+      splits = s;
+    }
+  }
+  return run_tile<GROUP, ZEROS, MB, 2>(a, l, within(a, splits, cells, 2 * MB * 1024), stream);
 }
 
 // Few rows: one workgroup a CU of as many blocks of outputs as it takes, up to 16 wavefronts, two to eight of them to a block. Where there are
