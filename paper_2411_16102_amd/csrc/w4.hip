@@ -103,7 +103,7 @@ struct Groups {
   }
 };
 
-// ---- up to 16 rows: a workgroup takes up to eight blocks of 16 outputs, each on KW wavefronts, a share of the inputs each ----
+// ---- slices of 16 rows: a workgroup takes up to eight blocks of 16 outputs, each on KW wavefronts, a share of the inputs each ----
 // x of the workgroup's inputs lies in LDS, so that the vector memory path carries weights alone and wavefronts do not wait for each
 // other behind the first barrier; a wavefront has U blocks of weights in use and U on the way.  Bound by reading the weights: 28672 x 4096 with
 // zero points (62 MB) one row 14.4 us, 8 rows 15.7 to 16.3 (a kernel that only reads as much: 10); 6144 x 4096 5.4 us, of which 2.2 are a launch.
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(1024) void w4_few_kernel(const W4Args a, const W4La
   uint16_t *xs = reinterpret_cast<uint16_t *>(lds);  // [rows][x_row]
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
   const Place at = place(splits, tiles);
-  const int tile = at.tile, split = at.split, rows = a.m;
+  const int tile = at.tile, split = at.split, m0 = at.z * 16, rows = min(16, a.m - m0);
   const int64_t block = (int64_t)tile * NW + wave / KW, nb = min(block, l.n_blocks - 1);
   const int n_kb = (int)l.k_blocks, first = (int)((int64_t)n_kb * split / splits), n_mine = (int)((int64_t)n_kb * (split + 1) / splits) - first;
   const int kb0 = first + n_mine * (wave % KW) / KW, kb1 = first + n_mine * (wave % KW + 1) / KW;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(1024) void w4_few_kernel(const W4Args a, const W4La
     for (int i = threadIdx.x; i < rows * per_row; i += threads) {
       const int r = i / per_row, c = i % per_row, k = first * 128 + c * 8;
       u32x4_t v = {0u, 0u, 0u, 0u};
-      if (k < a.k) v = *reinterpret_cast<const u32x4_t *>(a.x + r * a.x_stride + k);
+      if (k < a.k) v = *reinterpret_cast<const u32x4_t *>(a.x + (m0 + r) * a.x_stride + k);
       *reinterpret_cast<u32x4_t *>(xs + r * x_row + c * 8) = v;
     }
   }
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(1024) void w4_few_kernel(const W4Args a, const W4La
       for (int i = 0; i < splits; ++i) y += get_part(rs, part + i * step);
     }
   }
-  if (mine) store_four(a, 4 * g4, (int)block * 16 + j, y);
+  if (mine) store_four(a, m0 + 4 * g4, (int)block * 16 + j, y);
 }
 
 // ---- up to 64 rows: a workgroup of two shares of the inputs, four wavefronts each, takes 16 * MB rows and 64 * NB outputs ----
@@ -436,17 +436,6 @@ int within(const W4Args &a, int want, int64_t cells, int floats_per_part) {
   return std::max(1, (int)std::min<int64_t>(want, (int64_t)a.ws_floats / (cells * floats_per_part)));
 }
 
-template <int GROUP, bool ZEROS, int KW, int U>
-hipError_t run_few(const W4Args &a, const W4Layout &l, int blocks, int splits, hipStream_t stream) {
-  const int tiles = ceil_div(l.n_blocks, blocks), rows = a.m, threads = blocks * KW * 64;
-  const int x_row = ceil_div(l.k_blocks, splits) * 128 + 8, lds = std::max(rows * x_row * 2, threads * 16 + 16);
-  static OncePerDevice once;
-  if (const hipError_t e = allow_lds(once, reinterpret_cast<const void *>(&w4_few_kernel<GROUP, ZEROS, KW, U>), 160 * 1024)) return e;
-  if (lds > 160 * 1024) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((w4_few_kernel<GROUP, ZEROS, KW, U>), dim3((unsigned)(tiles * splits)), dim3(threads), lds, stream, a, l, splits, tiles, x_row);
-  return hipGetLastError();
-}
-
 template <int GROUP, bool ZEROS, int MB, int NB>
 hipError_t run_tile(const W4Args &a, const W4Layout &l, int splits, hipStream_t stream) {
   constexpr int LDS = TILE_KW * TILE_RING * 4 * MB * 1024;
@@ -457,52 +446,85 @@ hipError_t run_tile(const W4Args &a, const W4Layout &l, int splits, hipStream_t 
   return hipGetLastError();
 }
 
-// How many workgroups share outputs, by expected microseconds: rounds of workgroups on the chip, in each a start and its share's steps of one block,
-// and the join, which one workgroup does.  At least five blocks for a workgroup.  61 rows: 4096 x 4096 on 6 workgroups 15.0 us, 3 16.9; 17000 x 8192, 133
-// tiles, on 3 in two rounds 44.2, on one 47.5 (30 rows 29.2 and 36.9).  Where 32 outputs a wavefront would give more workgroups than CUs it takes
-// 64, which also need fewer sums of x for a product: 57344 x 8192, 61 rows 74 us for 89, 12 rows 48 for 51; 28672 x 4096, 61 rows
-// on fewer CUs 31.4 for 28.0.
-template <int GROUP, bool ZEROS, int MB>
-hipError_t launch_tile(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  const int64_t z = ceil_div(a.m, 64), cells = ceil_div(l.n_blocks, 8) * z;
-  if (cells > a.n_cu) return run_tile<GROUP, ZEROS, MB, 4>(a, l, 1, stream);
-  int splits = 1;
-  double best = 0;
-  for (int s = 1; s <= 8 && (s == 1 || (int)l.k_blocks >= 5 * s); ++s) {
-    const int rounds = ceil_div(cells * s, a.n_cu), steps = ceil_div(ceil_div(l.k_blocks, s), 2);
-    const double us = rounds * (2.5 + (0.65 + 0.2 * MB) * (GROUP == 32 ? 1.25 : 1.0) * steps) + (s > 1 ? 2.5 + 0.65 * s : 0.0);
-    if (s == 1 || us < best) {
-      best = us;
-      splits = s;
-    }
+// How a product is done is chosen by expected microseconds, fitted to 12 sets of rows (1 to 64), groups and zero points times 26 shapes from 256 x
+// 28672 to 28672 x 4096, each in tiles and as few rows on 1 to 8 workgroups: within 1 % of the best of them on average, 22 % at worst
+// (2048 x 4096, 41 rows, groups of 32: 11.1 us for 8.7); tiles alone 36 %.
+struct Way {
+  int splits = 1, blocks = 0;  // workgroups that share outputs; blocks of outputs of a workgroup (tiles: of a wavefront; 0: not possible)
+  double us = 0;
+};
+
+// Slices of 16 rows on one workgroup a CU of as many blocks of outputs as it takes, up to 16 wavefronts, two to eight of them to a block: a
+// start, the blocks and the slice's x, a wavefront's blocks in turn, and the join.  28672 x 8192, 4 rows 26.5 us, in workgroups of four
+// blocks 30.7; 4096 x 14336, 4 rows on two workgroups 11.2, on one 12.6.
+constexpr int few_wavefronts(int blocks) { return blocks <= 2 ? 8 : blocks <= 4 ? 4 : 2; }  // of a block
+constexpr int FEW_LDS = 160 * 1024;
+int few_x_row(const W4Layout &l, int splits) { return ceil_div(l.k_blocks, splits) * 128 + 8; }
+
+Way few_way(const W4Args &a, const W4Layout &l) {
+  const int nb = (int)l.n_blocks, kb = (int)l.k_blocks, rows = std::min(a.m, 16);
+  const int64_t z = ceil_div(a.m, 16);
+  Way best;
+  for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+    const int per_slice = (int)(a.n_cu / (s * z));
+    if (per_slice == 0 || (s > 1 && kb < 4 * s)) break;
+    const int blocks = ceil_div(nb, per_slice), steps = ceil_div(kb, s);
+    const int64_t cells = ceil_div(nb, std::max(blocks, 1)) * z;
+    if (blocks > 8 || rows * few_x_row(l, s) * 2 > FEW_LDS) continue;
+    if (s > 1 && (cells > a.n_counters || cells * s * blocks * 256 > (int64_t)a.ws_floats)) continue;
+    const double us = 3.4 + steps * (blocks * (a.group == 32 ? 0.047 : 0.032) + rows * 0.0044) + 0.29 * ceil_div(steps, few_wavefronts(blocks)) +
+                      (s > 1 ? 0.6 + 0.45 * s : 0.0);
+    if (!best.blocks || us < best.us) best = {s, blocks, us};
   }
-  return run_tile<GROUP, ZEROS, MB, 2>(a, l, within(a, splits, cells, 2 * MB * 1024), stream);
+  return best;
 }
 
-// Few rows: one workgroup a CU of as many blocks of outputs as it takes, up to 16 wavefronts, two to eight of them to a block. Where there are
-// fewer blocks than CUs workgroups share outputs, as long as each of their wavefronts has a block of inputs, or four where half the CUs have
-// work anyway.  Timed on 9 shapes from 4096 x 4096 to 28672 x 8192 with 1 to 8 rows, each with 1 to 8 blocks, 2 to 8 wavefronts
-// and 1 to 8 workgroups: 28672 x 8192, 4 rows 26.5 us, in workgroups of four blocks 30.7; 10240 x 8192 13.1, eight blocks on three workgroups
-// 14.5; 6144 x 4096 7.0, one block 7.2; 4096 x 14336 on two workgroups 11.2, on one 12.6 (4096 x 4096 6.7 and 5.9).
-template <int GROUP, bool ZEROS>
-hipError_t launch_few(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  const int nb = (int)l.n_blocks, kb = (int)l.k_blocks;
-  const int want = nb > a.n_cu ? 1 : nb > a.n_cu / 2 ? (kb >= 64 ? 2 : 1) : std::max(1, std::min(a.n_cu / nb, kb / 8));
-  const int splits = within(a, want, nb, 256), blocks = ceil_div((int64_t)nb * splits, a.n_cu);
-  if (blocks <= 2) return run_few<GROUP, ZEROS, 8, 1>(a, l, blocks, splits, stream);
-  if (blocks <= 4) return run_few<GROUP, ZEROS, 4, 2>(a, l, blocks, splits, stream);
-  return run_few<GROUP, ZEROS, 2, 2>(a, l, blocks, splits, stream);
+// Tiles: rounds of workgroups on the chip, in each a start and its share's steps of one block, and the join, which one workgroup does.  17000 x 8192,
+// 133 tiles, 61 rows on 3 workgroups in two rounds 45.7 us, on one 48.5.  Where 32 outputs a wavefront would give more workgroups than CUs it
+// takes 64, which also need fewer sums of x for a product: 57344 x 8192, 61 rows 78 us for 89, 12 rows 48 for 51; 28672 x 4096, 61
+// rows on fewer CUs 31.4 for 28.0.
+Way tile_way(const W4Args &a, const W4Layout &l) {
+  const int64_t z = ceil_div(a.m, 64), cells = ceil_div(l.n_blocks, 8) * z;
+  const int kb = (int)l.k_blocks;
+  const double step = (0.65 + 0.2 * std::min(4, ceil_div(a.m, 16))) * (a.group == 32 ? 1.25 : 1.0);
+  if (cells > a.n_cu) return {1, 4, 2.0 + ceil_div(ceil_div(l.n_blocks, 16) * z, a.n_cu) * (2.5 + 1.6 * step * ceil_div(kb, 2))};
+  Way best;
+  for (int s = 1; s <= 8 && (s == 1 || kb >= 5 * s); ++s) {
+    const double us = 2.0 + ceil_div(cells * s, a.n_cu) * (2.5 + step * ceil_div(ceil_div(kb, s), 2)) + (s > 1 ? 2.5 + 0.65 * s : 0.0);
+    if (!best.blocks || us < best.us) best = {s, 2, us};
+  }
+  return best;
+}
+
+template <int GROUP, bool ZEROS, int KW, int U>
+hipError_t run_few(const W4Args &a, const W4Layout &l, const Way &way, hipStream_t stream) {
+  const int tiles = ceil_div(l.n_blocks, way.blocks), z = ceil_div(a.m, 16), threads = way.blocks * KW * 64, x_row = few_x_row(l, way.splits);
+  const int lds = std::max(std::min(a.m, 16) * x_row * 2, threads * 16 + 16);
+  static OncePerDevice once;
+  if (const hipError_t e = allow_lds(once, reinterpret_cast<const void *>(&w4_few_kernel<GROUP, ZEROS, KW, U>), FEW_LDS)) return e;
+  hipLaunchKernelGGL((w4_few_kernel<GROUP, ZEROS, KW, U>), dim3((unsigned)(tiles * way.splits * z)), dim3(threads), lds, stream, a, l, way.splits, tiles, x_row);
+  return hipGetLastError();
+}
+
+template <int GROUP, bool ZEROS, int MB>
+hipError_t launch_tile(const W4Args &a, const W4Layout &l, const Way &way, hipStream_t stream) {
+  if (way.blocks == 4) return run_tile<GROUP, ZEROS, MB, 4>(a, l, 1, stream);
+  return run_tile<GROUP, ZEROS, MB, 2>(a, l, within(a, way.splits, (int64_t)ceil_div(l.n_blocks, 8) * ceil_div(a.m, 64), 2 * MB * 1024), stream);
 }
 
 template <int GROUP, bool ZEROS>
 hipError_t launch_group(const W4Args &a, const W4Layout &l, hipStream_t stream) {
-  // One operand's rows, where x fits into LDS whole and no CU needs a second workgroup: 6144 x 4096, 16 rows 8.5 us, in tiles 9.5;
-  // 28672 x 8192, 8 rows 28.1 against 31.0.  Else tiles (57344 x 8192, 2 rows, 14 blocks a CU: 52.4 against 54.5).
-  if (a.m <= 16 && a.m * l.k_blocks <= 600 && l.n_blocks <= 8 * a.n_cu) return launch_few<GROUP, ZEROS>(a, l, stream);
-  if (a.m <= 16) return launch_tile<GROUP, ZEROS, 1>(a, l, stream);
-  if (a.m <= 32) return launch_tile<GROUP, ZEROS, 2>(a, l, stream);
-  if (a.m <= 48) return launch_tile<GROUP, ZEROS, 3>(a, l, stream);
-  return launch_tile<GROUP, ZEROS, 4>(a, l, stream);
+  const Way few = few_way(a, l), tile = tile_way(a, l);
+  if (few.blocks && few.us < tile.us) {
+    const int wavefronts = few_wavefronts(few.blocks);
+    if (wavefronts == 8) return run_few<GROUP, ZEROS, 8, 1>(a, l, few, stream);
+    if (wavefronts == 4) return run_few<GROUP, ZEROS, 4, 2>(a, l, few, stream);
+    return run_few<GROUP, ZEROS, 2, 2>(a, l, few, stream);
+  }
+  if (a.m <= 16) return launch_tile<GROUP, ZEROS, 1>(a, l, tile, stream);
+  if (a.m <= 32) return launch_tile<GROUP, ZEROS, 2>(a, l, tile, stream);
+  if (a.m <= 48) return launch_tile<GROUP, ZEROS, 3>(a, l, tile, stream);
+  return launch_tile<GROUP, ZEROS, 4>(a, l, tile, stream);
 }
 
 template <int GROUP>
