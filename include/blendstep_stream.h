@@ -84,8 +84,8 @@ int bs_window_division(const bs_window *w, bs_window_parts *out);
 
 /* ---- 4-bit products --------------------------------------------------------------------------------------------
  * y[m, n] = sum over groups g of scale[n, g] * sum over k in g of x[m, k] * (w[n, k] - zero[n, g]),  w in 0 .. 15.
- * group is 32, 64 or 128; k a multiple of it; n any; m >= 0.  Meant for few rows (up to 64 the weights are read
- * once; beyond, once for every 64 rows). */
+ * group is 32, 64 or 128; k a multiple of it; n any; m >= 0.  Meant for few rows (up to 64 the weights come from
+ * memory once; beyond, once for every 64 rows). */
 
 /* Bytes of the laid-out weight; 0 for a shape that is not supported. */
 int64_t bs_w4_bytes(int64_t n, int64_t k, int32_t group, int32_t with_zeros);

@@ -446,9 +446,9 @@ hipError_t run_tile(const W4Args &a, const W4Layout &l, int splits, hipStream_t 
   return hipGetLastError();
 }
 
-// How a product is done is chosen by expected microseconds, fitted to 12 sets of rows (1 to 64), groups and zero points times 26 shapes from 256 x
-// 28672 to 28672 x 4096, each in tiles and as few rows on 1 to 8 workgroups: within 1 % of the best of them on average, 22 % at worst
-// (2048 x 4096, 41 rows, groups of 32: 11.1 us for 8.7); tiles alone 36 %.
+// How a product is done is chosen by expected microseconds, fitted to 11 sets of rows (1 to 64), groups and zero points times 26 shapes from 256 x
+// 28672 to 28672 x 4096, each in tiles and in slices of 16 rows on 1 to 8 workgroups: 0.6 % longer than the best of them on average, 11 % at
+// worst (6144 x 4096, 48 rows); tiles alone 36 %.
 struct Way {
   int splits = 1, blocks = 0;  // workgroups that share outputs; blocks of outputs of a workgroup (tiles: of a wavefront; 0: not possible)
   double us = 0;
@@ -472,8 +472,9 @@ Way few_way(const W4Args &a, const W4Layout &l) {
     const int64_t cells = ceil_div(nb, std::max(blocks, 1)) * z;
     if (blocks > 8 || rows * few_x_row(l, s) * 2 > FEW_LDS) continue;
     if (s > 1 && (cells > a.n_counters || cells * s * blocks * 256 > (int64_t)a.ws_floats)) continue;
-    const double us = 3.4 + steps * (blocks * (a.group == 32 ? 0.047 : 0.032) + rows * 0.0044) + 0.29 * ceil_div(steps, few_wavefronts(blocks)) +
-                      (s > 1 ? 0.6 + 0.45 * s : 0.0);
+    const int wavefronts = few_wavefronts(blocks);
+    const double us = 1.6 + steps * (blocks * (a.group == 32 ? 0.036 : 0.020) + rows * 0.0058) +
+                      (wavefronts == 8 ? 0.17 : wavefronts == 4 ? 0.23 : 0.38) * ceil_div(steps, wavefronts) + (s > 1 ? 0.5 + 0.48 * s : 0.0);
     if (!best.blocks || us < best.us) best = {s, blocks, us};
   }
   return best;
@@ -487,10 +488,10 @@ Way tile_way(const W4Args &a, const W4Layout &l) {
   const int64_t z = ceil_div(a.m, 64), cells = ceil_div(l.n_blocks, 8) * z;
   const int kb = (int)l.k_blocks;
   const double step = (0.65 + 0.2 * std::min(4, ceil_div(a.m, 16))) * (a.group == 32 ? 1.25 : 1.0);
-  if (cells > a.n_cu) return {1, 4, 2.0 + ceil_div(ceil_div(l.n_blocks, 16) * z, a.n_cu) * (2.5 + 1.6 * step * ceil_div(kb, 2))};
+  if (cells > a.n_cu) return {1, 4, 2.5 + ceil_div(ceil_div(l.n_blocks, 16) * z, a.n_cu) * (2.5 + 1.6 * step * ceil_div(kb, 2))};
   Way best;
   for (int s = 1; s <= 8 && (s == 1 || kb >= 5 * s); ++s) {
-    const double us = 2.0 + ceil_div(cells * s, a.n_cu) * (2.5 + step * ceil_div(ceil_div(kb, s), 2)) + (s > 1 ? 2.5 + 0.65 * s : 0.0);
+    const double us = 2.5 + ceil_div(cells * s, a.n_cu) * (2.5 + step * ceil_div(ceil_div(kb, s), 2)) + (s > 1 ? 2.5 + 0.65 * s : 0.0);
     if (!best.blocks || us < best.us) best = {s, 2, us};
   }
   return best;

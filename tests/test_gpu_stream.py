@@ -310,6 +310,11 @@ def test_w4_more_tiles_than_cus(lib, m, n, k, group, zeros):
     _w4(lib, m, n, k, group, zeros)
 
 
+@pytest.mark.parametrize("m,n,k,group,zeros", [(16, 16500, 4992, 128, True), (30, 8210, 4896, 32, False), (40, 6203, 5120, 64, False), (61, 4200, 5120, 64, True)])
+def test_w4_tiles_that_share_outputs(lib, m, n, k, group, zeros):
+    _w4(lib, m, n, k, group, zeros)
+
+
 @pytest.mark.parametrize("m,k", [(16, 4736), (16, 4864), (9, 8448), (9, 8576), (1, 76800), (1, 76928)])
 def test_w4_rows_that_fill_the_lds(lib, m, k):
     _w4(lib, m, 35, k, 128, True)
