@@ -128,9 +128,9 @@ int bs_pages_free(bs_pages *p, const int32_t *ids, int32_t n);
 /* Moves the live pages to the numbers below their count, each number above it to the smallest free one in ascending order, and
  * rewrites the tables.  src, dst: arrays of n_pages entries. */
 int bs_pages_compact(bs_pages *p, int32_t *src, int32_t *dst, int32_t *n_moves, int32_t *n_live);
-/* Lengths, and tables one behind the other (page_start[n + 1]; page_ids of at least page_start[n] entries).  With page_ids = NULL only the
- * lengths and page_start are written. */
-int bs_pages_tables(const bs_pages *p, const int32_t *ids, int32_t n, int32_t *tokens, int32_t *page_start, int32_t *page_ids);
+/* Lengths, and tables one behind the other (page_start[n + 1]; page_ids of `room` entries).  With page_ids = NULL or room for fewer than
+ * page_start[n] entries only the lengths and page_start are written. */
+int bs_pages_tables(const bs_pages *p, const int32_t *ids, int32_t n, int32_t *tokens, int32_t *page_start, int32_t *page_ids, int64_t room);
 int bs_pages_stats(const bs_pages *p, int32_t *n_free, int32_t *n_sequences);
 
 /* Copies page src[i] to page dst[i], i < n, in each of n_pools pools of n_pages pages.  pools, src, dst: HOST.  No dst may

@@ -198,7 +198,7 @@ def raw():
         lib.bs_pages_trim.argtypes = [_p, _p, _i32, _i32, _i32]
         lib.bs_pages_free.argtypes = [_p, _p, _i32]
         lib.bs_pages_compact.argtypes = [_p, _p, _p, _p, _p]
-        lib.bs_pages_tables.argtypes = [_p, _p, _i32, _p, _p, _p]
+        lib.bs_pages_tables.argtypes = [_p, _p, _i32, _p, _p, _p, C.c_int64]
         lib.bs_pages_stats.argtypes = [_p, _p, _p]
         lib.bs_kv_copy_pages.argtypes = [_p, _p, _i32, _i64, _p, _p, _i32, _p]
         lib.bs_kv_compact.argtypes = [_p, _p, _i32, _i64, _p, _i64, _p, _p, _p]
@@ -687,7 +687,7 @@ class Pages:
         if rc != 0:
             raise BlendStepError(rc, (self.lib.bs_pages_last_error(None) or b"").decode())
         self.h = h
-        self._ids, self._out, self._src, self._dst, self._count = (_Words() for _ in range(5))
+        self._ids, self._out, self._src, self._dst, self._count, self._start, self._held = (_Words() for _ in range(7))
 
     def close(self):
         if getattr(self, "h", None):
@@ -744,21 +744,20 @@ class Pages:
         return self._src.a[:n].copy(), self._dst.a[:n].copy(), live
 
     def lengths(self, ids) -> np.ndarray:
-        return self._tables(ids, False)[0]
+        at, n = self._ids.put(ids)
+        self._check(self.lib.bs_pages_tables(self.h, at, n, self._out.room(n), self._start.room(n + 1), None, 0))
+        return self._out.a[:n].copy()
 
     def tables(self, ids):
         """(page_start, page_ids) of the sequences, as a batch holds them."""
-        return self._tables(ids, True)[1:]
-
-    def _tables(self, ids, whole):
         at, n = self._ids.put(ids)
-        tokens, start = self._out.room(n), np.empty(n + 1, dtype=np.int32)
-        first = _address(start)
-        self._check(self.lib.bs_pages_tables(self.h, at, n, tokens, first, None))
-        pages = np.empty(int(start[-1]) if whole else 0, dtype=np.int32)
-        if whole:
-            self._check(self.lib.bs_pages_tables(self.h, at, n, tokens, first, _address(pages)))
-        return self._out.a[:n].copy(), start, pages
+        tokens, start, held = self._out.room(n), self._start.room(n + 1), self._held
+        self._check(self.lib.bs_pages_tables(self.h, at, n, tokens, start, held.at, held.a.size))
+        total = int(self._start.a[n])
+        if total > held.a.size:
+            room = held.room(total)
+            self._check(self.lib.bs_pages_tables(self.h, at, n, tokens, start, room, held.a.size))
+        return self._start.a[:n + 1].copy(), held.a[:total].copy()
 
     def stats(self) -> dict:
         self._check(self.lib.bs_pages_stats(self.h, self._count.at, self._count.at + 4))

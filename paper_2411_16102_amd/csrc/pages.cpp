@@ -318,7 +318,7 @@ int bs_pages_compact(bs_pages *p, int32_t *src, int32_t *dst, int32_t *n_moves, 
   });
 }
 
-int bs_pages_tables(const bs_pages *p, const int32_t *ids, int32_t n, int32_t *tokens, int32_t *page_start, int32_t *page_ids) {
+int bs_pages_tables(const bs_pages *p, const int32_t *ids, int32_t n, int32_t *tokens, int32_t *page_start, int32_t *page_ids, int64_t room) {
   if (!p) return BS_EINVAL;
   return guarded(p, [&]() -> int {
     if (const int rc = check_ids(p, ids, n, false)) return rc;
@@ -326,6 +326,7 @@ int bs_pages_tables(const bs_pages *p, const int32_t *ids, int32_t n, int32_t *t
     int64_t at = 0;
     for (int32_t i = 0; i < n; ++i) at += (int64_t)p->seqs[ids[i]].table.size();
     if (at > 0x7fffffff) return fail(p, BS_EINVAL, "tables of %lld pages", (long long)at);
+    if (at > room) page_ids = nullptr;
     page_start[0] = 0;
     for (int32_t i = 0; i < n; ++i) {
       const Sequence &s = p->seqs[ids[i]];

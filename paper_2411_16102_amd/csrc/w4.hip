@@ -106,7 +106,7 @@ struct Groups {
 // ---- slices of 16 rows: a workgroup takes up to eight blocks of 16 outputs, each on KW wavefronts, a share of the inputs each ----
 // x of the workgroup's inputs lies in LDS, so that the vector memory path carries weights alone and wavefronts do not wait for each
 // other behind the first barrier; a wavefront has U blocks of weights in use and U on the way.  Bound by reading the weights: 28672 x 4096 with
-// zero points (62 MB) one row 14.4 us, 8 rows 15.7 to 16.3 (a kernel that only reads as much: 10); 6144 x 4096 5.4 us, of which 2.2 are a launch.
+// zero points (62 MB) one row 14.4 us, 8 rows 15.7 to 16.3 (a kernel that only reads as much: 10); 6144 x 4096 6.3 us, of which 2.2 are a launch.
 template <int GROUP, bool ZEROS, int KW, int U>
 __global__ __launch_bounds__(1024) void w4_few_kernel(const W4Args a, const W4Layout l, int splits, int tiles, int x_row) {
   constexpr int GPB = 128 / GROUP, STEPS = GROUP / 32;  // groups of a block of inputs, matrix instructions of a group
