@@ -132,19 +132,26 @@ __global__ __launch_bounds__(1024) void w4_few_kernel(const W4Args a, const W4La
       f.g[u].load(a, l, nb * n_kb + k, j);
     }
   };
+  // inputs [128 first, 128 (first + n_mine)) of the rows; zeros past the last.  Asked for in front of the weights, so that they do not wait for those.
+  const int per_row = n_mine * 16, total = rows * per_row;
+  auto x_chunk = [&](int i) __attribute__((always_inline)) {
+    const int r = i / per_row, k = first * 128 + (i - r * per_row) * 8;
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (i < total && k < a.k) v = *reinterpret_cast<const u32x4_t *>(a.x + (m0 + r) * a.x_stride + k);
+    return v;
+  };
+  auto put_x = [&](int i, u32x4_t v) __attribute__((always_inline)) {
+    const int r = i / per_row;
+    if (i < total) *reinterpret_cast<u32x4_t *>(xs + r * x_row + (i - r * per_row) * 8) = v;
+  };
   Blocks fa, fb;
+  const u32x4_t x0 = x_chunk(threadIdx.x);
+  __builtin_amdgcn_sched_barrier(0);
   load(kb0, fa);
   load(kb0 + U, fb);
   __builtin_amdgcn_sched_barrier(0);
-  {  // inputs [128 first, 128 (first + n_mine)) of the rows; zeros past the last
-    const int per_row = n_mine * 16;
-    for (int i = threadIdx.x; i < rows * per_row; i += threads) {
-      const int r = i / per_row, c = i % per_row, k = first * 128 + c * 8;
-      u32x4_t v = {0u, 0u, 0u, 0u};
-      if (k < a.k) v = *reinterpret_cast<const u32x4_t *>(a.x + (m0 + r) * a.x_stride + k);
-      *reinterpret_cast<u32x4_t *>(xs + r * x_row + c * 8) = v;
-    }
-  }
+  put_x(threadIdx.x, x0);
+  for (int i = threadIdx.x + threads; i < total; i += threads) put_x(i, x_chunk(i));
   __syncthreads();
   const Unpack unpack;
   const bf16x8_t summing = sum_operand<ZEROS>();
