@@ -265,6 +265,7 @@ class Layer:
         self._q_width = shape.n_q_heads * shape.head_dim
         self._qkv_width = shape.n_qkv
         self._page_elems = self.page_bytes() // 2
+        self._plan_key = (device, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.page_size, shape.rope_theta)
 
     def close(self):
         if getattr(self, "h", None):
@@ -463,12 +464,14 @@ class Layer:
 
     # -- streams (blendstep_stream.h) ---------------------------------------------------
     def window_plan(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages: Optional[int] = None, stream=None):
-        """The plan of a step for window_attention and rope_append (bs_window_plan): one for all layers with this window.
+        """The plan of a step for window_attention and rope_append (bs_window_plan): one for all layers with this window, which may
+        be other Layer objects with the same heads, pages and rope_theta on the same device.
         positions [n_axes, n_rows] and axis_of_pair [head_dim / 2]: rotary positions with several axes."""
         return WindowPlan(self, batch, window, sinks, positions, axis_of_pair, n_pages, stream)
 
     def window_attention(self, plan: "WindowPlan", q, kv_pool, out=None, stream=None):
         """Sliding-window attention with sinks of the plan's rows; q and out: [n_rows, Hq * dh] bf16, rows at any stride."""
+        self._check_plan(plan)
         width = self._q_width
         q_stride = self._row_stride(plan, q, width)
         if out is None:
@@ -478,12 +481,13 @@ class Layer:
         self._check_pool(plan, kv_pool)
         rc = self.lib.bs_window_attention(plan.h, q.data_ptr(), q_stride, out.data_ptr(), out_stride, kv_pool.data_ptr(), self._raw_stream(stream))
         if rc:
-            self._check(rc)
+            plan.layer._check(rc)
         return out
 
     def rope_append(self, plan: "WindowPlan", qkv, kv_pool, q=None, stream=None):
         """Turns queries and keys of fused rows [n_rows, (Hq + 2 Hkv) * dh] and appends keys and values to kv_pool; the
         turned queries [n_rows, Hq * dh] (q: where they go; qkv[:, :Hq * dh] for in place)."""
+        self._check_plan(plan)
         stride = self._row_stride(plan, qkv, self._qkv_width)
         if q is None:
             q, q_stride = qkv.new_empty((plan.n_rows, self._q_width)), self._q_width
@@ -492,8 +496,13 @@ class Layer:
         self._check_pool(plan, kv_pool)
         rc = self.lib.bs_rope_append(plan.h, qkv.data_ptr(), stride, q.data_ptr(), q_stride, kv_pool.data_ptr(), self._raw_stream(stream))
         if rc:
-            self._check(rc)
+            plan.layer._check(rc)
         return q
+
+    def _check_plan(self, plan):
+        # widths, pages and angles of a call are those of the plan's context, the checks of its tensors go by this layer's
+        if plan.layer is not self and plan.layer._plan_key != self._plan_key:
+            raise ValueError("the plan is of a layer on another device, or with other heads, pages or rope_theta")
 
     def _raw_stream(self, stream):
         return _current_stream(self.device) if stream is None else stream.cuda_stream

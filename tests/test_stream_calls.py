@@ -1,0 +1,80 @@
+"""What the Python calls of the stream operators check before the library is reached, on contexts without a device.
+
+A layer here is host-only (CPU tensors are then those of its device) and its library is one that writes down what it
+is asked, so that a call that passes the checks is seen and nothing runs."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_16102_amd import binding, workloads as W
+from stream_cases import make_batch
+
+SHAPE = W.LayerShape(256, 8, 2, 64, 256)
+
+
+class Asked:
+    """The library, but for the calls that would launch something: those are kept in `calls` and answer `rc`."""
+
+    def __init__(self, lib, rc=0):
+        self._lib, self.rc, self.calls = lib, rc, []
+
+    def __getattr__(self, name):
+        if name not in ("bs_window_attention", "bs_rope_append", "bs_w4_pack", "bs_w4_linear", "bs_kv_copy_pages", "bs_kv_compact"):
+            return getattr(self._lib, name)
+
+        def call(*args):
+            self.calls.append((name, args))
+            return self.rc
+        return call
+
+
+class Stream:
+    cuda_stream = 0
+
+
+def make_layer(shape=SHAPE, rc=0):
+    layer = binding.Layer(shape, device=-1)
+    layer.lib = Asked(layer.lib, rc)
+    return layer
+
+
+def bf16(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+# ---- plans of other layers ------------------------------------------------------------------
+@pytest.mark.parametrize("other", [W.LayerShape(256, 4, 4, 128, 256), W.LayerShape(256, 8, 1, 64, 256), W.LayerShape(256, 4, 1, 128, 256),
+                                   W.LayerShape(256, 8, 2, 64, 256, rope_theta=10000.0)])
+def test_plans_of_layers_with_other_shapes_are_refused(other):
+    # (the queries of all of these are as wide as the layer's: their pages, their groups or their angles differ)
+    layer, owner = make_layer(), make_layer(other)
+    batch = make_batch([(1, 40), (3, 20)])
+    plan = owner.window_plan(batch, 8)
+    pool = bf16(batch.n_pages * max(layer.page_bytes(), owner.page_bytes()))
+    with pytest.raises(ValueError, match="another device, or with other heads"):
+        layer.window_attention(plan, bf16(4, 512), pool, stream=Stream)
+    with pytest.raises(ValueError, match="another device, or with other heads"):
+        layer.rope_append(plan, bf16(4, SHAPE.n_qkv), pool, stream=Stream)
+    assert not layer.lib.calls and not owner.lib.calls
+
+
+def test_plans_of_layers_on_other_devices_are_refused():
+    layer, owner = make_layer(), make_layer()
+    batch = make_batch([(1, 40)])
+    plan, pool = owner.window_plan(batch, 8), bf16(batch.n_pages * layer.page_bytes() // 2)
+    layer.window_attention(plan, bf16(1, 512), pool, stream=Stream)  # (a layer of the same kind: its plan is as good)
+    assert len(layer.lib.calls) == 1
+    owner._plan_key = (1,) + owner._plan_key[1:]  # as if it had been made on device 1
+    with pytest.raises(ValueError, match="another device"):
+        layer.window_attention(plan, bf16(1, 512), pool, stream=Stream)
+    assert len(layer.lib.calls) == 1
+
+
+def test_the_message_of_a_plans_error_is_the_plans():
+    layer, owner = binding.Layer(SHAPE, device=-1), binding.Layer(SHAPE, device=-1)
+    batch = make_batch([(1, 40)])
+    plan, pool = owner.window_plan(batch, 8), bf16(batch.n_pages * layer.page_bytes() // 2)
+    with pytest.raises(binding.BlendStepError, match="host-only context"):
+        layer.window_attention(plan, bf16(1, 512), pool, stream=Stream)
+    with pytest.raises(binding.BlendStepError, match="host-only context"):
+        layer.rope_append(plan, bf16(1, SHAPE.n_qkv), pool, stream=Stream)
