@@ -260,6 +260,7 @@ class Layer:
         if rc != 0:
             raise BlendStepError(rc, (self.lib.bs_last_error(None) or b"").decode())
         self.h = h
+        self._plans = set()  # handles of the plans that use this context, which end before it
         # of every call on streams
         self._bf16_type = torch.bfloat16
         self._q_width = shape.n_q_heads * shape.head_dim
@@ -269,6 +270,8 @@ class Layer:
 
     def close(self):
         if getattr(self, "h", None):
+            while self._plans:
+                self._plans.pop().close()
             self.lib.bs_destroy(self.h)
             self.h = None
 
@@ -471,7 +474,7 @@ class Layer:
 
     def window_attention(self, plan: "WindowPlan", q, kv_pool, out=None, stream=None):
         """Sliding-window attention with sinks of the plan's rows; q and out: [n_rows, Hq * dh] bf16, rows at any stride."""
-        self._check_plan(plan)
+        handle = self._plan_handle(plan)
         width = self._q_width
         q_stride = self._row_stride(plan, q, width)
         if out is None:
@@ -479,7 +482,7 @@ class Layer:
         else:
             out_stride = self._row_stride(plan, out, width)
         self._check_pool(plan, kv_pool)
-        rc = self.lib.bs_window_attention(plan.h, q.data_ptr(), q_stride, out.data_ptr(), out_stride, kv_pool.data_ptr(), self._raw_stream(stream))
+        rc = self.lib.bs_window_attention(handle, q.data_ptr(), q_stride, out.data_ptr(), out_stride, kv_pool.data_ptr(), self._raw_stream(stream))
         if rc:
             plan.layer._check(rc)
         return out
@@ -487,22 +490,27 @@ class Layer:
     def rope_append(self, plan: "WindowPlan", qkv, kv_pool, q=None, stream=None):
         """Turns queries and keys of fused rows [n_rows, (Hq + 2 Hkv) * dh] and appends keys and values to kv_pool; the
         turned queries [n_rows, Hq * dh] (q: where they go; qkv[:, :Hq * dh] for in place)."""
-        self._check_plan(plan)
+        handle = self._plan_handle(plan)
         stride = self._row_stride(plan, qkv, self._qkv_width)
         if q is None:
             q, q_stride = qkv.new_empty((plan.n_rows, self._q_width)), self._q_width
         else:
             q_stride = self._row_stride(plan, q, self._q_width)
         self._check_pool(plan, kv_pool)
-        rc = self.lib.bs_rope_append(plan.h, qkv.data_ptr(), stride, q.data_ptr(), q_stride, kv_pool.data_ptr(), self._raw_stream(stream))
+        rc = self.lib.bs_rope_append(handle, qkv.data_ptr(), stride, q.data_ptr(), q_stride, kv_pool.data_ptr(), self._raw_stream(stream))
         if rc:
             plan.layer._check(rc)
         return q
 
-    def _check_plan(self, plan):
-        # widths, pages and angles of a call are those of the plan's context, the checks of its tensors go by this layer's
+    def _plan_handle(self, plan):
+        """The handle of a plan that is open and whose calls may be checked against this layer."""
+        h = plan._handle.h
+        if h is None:
+            plan._open()
+        # (widths, pages and angles of a call are those of the plan's context)
         if plan.layer is not self and plan.layer._plan_key != self._plan_key:
             raise ValueError("the plan is of a layer on another device, or with other heads, pages or rope_theta")
+        return h
 
     def _raw_stream(self, stream):
         return _current_stream(self.device) if stream is None else stream.cuda_stream
@@ -638,19 +646,38 @@ class W4Weight:
     with_zeros: bool
 
 
+class _PlanHandle:
+    """A bs_window, which its context has to outlive: the layer knows the handle, not the plan, and closes it before its own, whichever
+    of layer and plan ends first (the collector may take both in any order)."""
+
+    def __init__(self, layer: Layer):
+        if layer.h is None:
+            raise ValueError("the layer is closed")
+        self.h, self._lib, self._of = None, layer.lib, layer._plans
+        h = C.c_void_p()
+        layer._check(layer.lib.bs_window_create(layer.h, C.byref(h)))
+        self.h = h
+        self._of.add(self)
+
+    def close(self):
+        if self.h is not None:
+            self._lib.bs_window_destroy(self.h)
+            self.h = None
+            self._of.discard(self)
+
+
 class WindowPlan:
     """The plan of one step (bs_window): made once, used by every layer with its window and sinks."""
 
     def __init__(self, layer: Layer, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages=None, stream=None):
         self.layer = layer
         self.n_rows = self.n_pages = 0
-        h = C.c_void_p()
-        layer._check(layer.lib.bs_window_create(layer.h, C.byref(h)))
-        self.h = h
+        self._handle = _PlanHandle(layer)
         self.update(batch, window, sinks, positions, axis_of_pair, n_pages, stream)
 
     def update(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages=None, stream=None):
         """Plans another step on the same buffers."""
+        self._open()
         lay = self.layer
         d, keep = marshal_batch(batch)
         axes, pos, axis = 0, None, None
@@ -668,15 +695,23 @@ class WindowPlan:
         self.n_rows, self.n_pages = batch.n_rows, pages
         return self
 
+    @property
+    def h(self):
+        return self._handle.h
+
+    def _open(self):
+        if self._handle.h is None:
+            raise ValueError("the plan is closed, or its layer is")
+
     def division(self) -> WindowParts:
+        self._open()
         out = WindowParts()
         self.layer._check(self.layer.lib.bs_window_division(self.h, C.byref(out)))
         return out
 
     def close(self):
-        if getattr(self, "h", None):
-            self.layer.lib.bs_window_destroy(self.h)
-            self.h = None
+        if hasattr(self, "_handle"):
+            self._handle.close()
 
     def __del__(self):
         try:

@@ -78,3 +78,64 @@ def test_the_message_of_a_plans_error_is_the_plans():
         layer.window_attention(plan, bf16(1, 512), pool, stream=Stream)
     with pytest.raises(binding.BlendStepError, match="host-only context"):
         layer.rope_append(plan, bf16(1, SHAPE.n_qkv), pool, stream=Stream)
+
+
+# ---- plans and contexts that end --------------------------------------------------------------
+class Ends:
+    """The library, with the order in which contexts (True) and plans (False) end."""
+
+    def __init__(self, lib):
+        self._lib, self.order = lib, []
+
+    def __getattr__(self, name):
+        if name not in ("bs_destroy", "bs_window_destroy"):
+            return getattr(self._lib, name)
+
+        def call(h):
+            self.order.append(name == "bs_destroy")
+            if not all(self.order):  # (a plan that outlives its context must not be ended through it)
+                getattr(self._lib, name)(h)
+        return call
+
+
+@pytest.mark.parametrize("how", ["layer first", "plan first", "dropped", "a cycle", "a cycle that was closed"])
+def test_plans_end_before_their_layer(how):
+    import gc
+    layer = binding.Layer(SHAPE, device=-1)
+    ends = layer.lib = Ends(layer.lib)
+    plans = [layer.window_plan(make_batch([(1, 40)]), 8) for _ in range(2)]
+    if how.startswith("a cycle"):
+        layer.plans = plans
+    if how in ("layer first", "a cycle that was closed"):
+        layer.close()
+    elif how == "plan first":
+        for p in plans:
+            p.close()
+        layer.close()
+    if not how.startswith("a cycle"):
+        for p in plans:
+            p.close()
+        p = None
+    del layer, plans
+    gc.collect()
+    assert ends.order == [False, False, True]
+
+
+def test_a_closed_layers_plans_raise():
+    layer = binding.Layer(SHAPE, device=-1)
+    batch = make_batch([(1, 40)])
+    plan = layer.window_plan(batch, 8)
+    gone = layer.window_plan(batch, 8)
+    gone.close()
+    gone.close()
+    with pytest.raises(ValueError, match="closed"):
+        gone.division()
+    assert plan.division().pages == 1
+    layer.close()
+    for call in (lambda: plan.update(batch, 8), lambda: plan.division(), lambda: layer.window_plan(batch, 8),
+                 lambda: layer.window_attention(plan, bf16(1, 512), bf16(3 * 16 * 256), stream=Stream),
+                 lambda: layer.rope_append(plan, bf16(1, SHAPE.n_qkv), bf16(3 * 16 * 256), stream=Stream)):
+        with pytest.raises(ValueError, match="closed"):
+            call()
+    plan.close()
+    layer.close()
