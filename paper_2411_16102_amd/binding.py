@@ -516,13 +516,21 @@ class Layer:
         return _current_stream(self.device) if stream is None else stream.cuda_stream
 
     def _row_stride(self, plan, t, width):
-        if t.dtype is self._bf16_type and t.shape == (plan.n_rows, width):
+        if t.dtype is self._bf16_type and t.shape == (plan.n_rows, width) and t.get_device() == self.device:
             stride, inner = t.stride()
             if inner == 1 or not plan.n_rows:
                 return stride
-        raise ValueError("expected bf16 rows [%d, %d], got %s %s" % (plan.n_rows, width, t.dtype, tuple(t.shape)))
+        raise ValueError("expected bf16 rows [%d, %d] on device %d, got %s %s on %s" % (plan.n_rows, width, self.device, t.dtype, tuple(t.shape), t.device))
+
+    def _here(self, what, *tensors):
+        # (a kernel that is given another device's address, or the host's, faults)
+        for t in tensors:
+            if t.get_device() != self.device:
+                raise ValueError("%s: a tensor is on %s, the layer on device %d" % (what, t.device, self.device))
 
     def _check_pool(self, plan, kv_pool):
+        if kv_pool.get_device() != self.device:
+            self._here("the pool", kv_pool)
         if kv_pool.dtype is not self._bf16_type or not kv_pool.is_contiguous() or kv_pool.numel() < plan.n_pages * self._page_elems:
             raise ValueError("the pool is smaller than the %d pages of the plan, or not contiguous bf16" % plan.n_pages)
 
@@ -530,6 +538,7 @@ class Layer:
         """Lays 4-bit weights out for w4_linear (bs_w4_pack).  packed: uint8 [n, k / 2], the even input in the low four bits;
         scales: bf16 [n, k / group]; zeros: uint8 [n, k / group] or None (8 everywhere)."""
         torch = self.torch
+        self._here("w4_pack", packed, scales, *(() if zeros is None else (zeros,)))
         n, k = packed.shape[0], packed.shape[1] * 2
         groups = scales.shape[1]
         group = k // groups if groups else 128
@@ -547,6 +556,8 @@ class Layer:
     def w4_linear(self, x, weight: "W4Weight", out=None, stream=None):
         """x [m, k] bf16 times a laid-out 4-bit weight: [m, n] bf16."""
         shape = x.shape
+        if x.get_device() != self.device or weight.data.get_device() != self.device:
+            self._here("w4_linear", x, weight.data)
         if x.dtype is not self._bf16_type or len(shape) != 2 or shape[1] != weight.k:
             raise ValueError("w4_linear: bf16 rows of %d inputs, got %s %s" % (weight.k, x.dtype, tuple(shape)))
         m = shape[0]
@@ -558,6 +569,7 @@ class Layer:
         if out is None:
             out, out_stride = x.new_empty((m, weight.n)), weight.n
         else:
+            self._here("w4_linear", out)
             if out.dtype is not x.dtype or out.shape != (m, weight.n) or out.stride(1) != 1:
                 raise ValueError("w4_linear: out is not bf16 [%d, %d]" % (m, weight.n))
             out_stride = out.stride(0)
@@ -571,12 +583,14 @@ class Layer:
         """(array of addresses, pages of each) of a tensor [n_pools, elements] or a list of flat pools."""
         size = self._page_elems
         if hasattr(pools, "shape"):
+            self._here("pools", pools)
             if pools.dtype is not self._bf16_type or pools.dim() != 2 or not pools.is_contiguous() or pools.shape[1] % size:
                 raise ValueError("pools are contiguous bf16 [n_pools, elements], whole pages each")
             n, elems = pools.shape
             first = pools.data_ptr()
             return np.arange(first, first + 2 * elems * n, 2 * elems, dtype=np.uint64)[:n] if elems else np.zeros(n, dtype=np.uint64), elems // size
         pools = list(pools)
+        self._here("pools", *pools)
         for p in pools:
             if p.dtype is not self._bf16_type or not p.is_contiguous() or p.numel() != pools[0].numel() or p.numel() % size:
                 raise ValueError("pools are contiguous bf16 tensors of one size, whole pages each")

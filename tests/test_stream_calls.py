@@ -139,3 +139,69 @@ def test_a_closed_layers_plans_raise():
             call()
     plan.close()
     layer.close()
+
+
+# ---- tensors of other devices --------------------------------------------------------------------
+def test_tensors_of_other_devices_are_refused():
+    layer = make_layer()
+    layer.device = 0  # as a layer of the first GPU: the tensors below are the host's
+    batch = make_batch([(1, 40), (3, 20)])
+    own = make_layer()
+    plan = own.window_plan(batch, 8)
+    plan.layer = layer
+    q, qkv, pool = bf16(4, 512), bf16(4, SHAPE.n_qkv), bf16(batch.n_pages * layer.page_bytes() // 2)
+    packed, scales, zeros = torch.zeros((16, 64), dtype=torch.uint8), bf16(16, 2), torch.zeros((16, 2), dtype=torch.uint8)
+    weight = own.w4_pack(packed, scales, zeros, stream=Stream)
+    calls = (lambda l: l.window_attention(plan, q, pool, stream=Stream), lambda l: l.window_attention(plan, q, pool, out=q, stream=Stream),
+             lambda l: l.rope_append(plan, qkv, pool, stream=Stream), lambda l: l.rope_append(plan, qkv, pool, q=q, stream=Stream),
+             lambda l: l.w4_pack(packed, scales, stream=Stream), lambda l: l.w4_pack(packed, scales, zeros, stream=Stream),
+             lambda l: l.w4_linear(bf16(2, 128), weight, stream=Stream), lambda l: l.w4_linear(bf16(2, 128), weight, out=bf16(2, 16), stream=Stream),
+             lambda l: l.copy_pages(pool.view(1, -1), [0], [1], stream=Stream), lambda l: l.copy_pages([pool, pool], [0], [1], stream=Stream),
+             lambda l: l.compact_pages([pool], [0, 2], stream=Stream), lambda l: l.compact_pages(pool.view(1, -1), [0, 2], stream=Stream))
+    for call in calls:
+        with pytest.raises(ValueError, match=" on cpu"):
+            call(layer)
+    assert not layer.lib.calls
+    # the same calls on a layer of their own device are asked
+    plan.layer = own
+    own.lib.calls.clear()
+    for call in calls:
+        call(own)
+    assert len(own.lib.calls) == len(calls)
+
+
+def test_every_tensor_of_a_call_is_looked_at():
+    # one of them elsewhere is enough
+    layer = make_layer()
+    batch = make_batch([(1, 40)])
+    plan = layer.window_plan(batch, 8)
+    pool, far = bf16(batch.n_pages * layer.page_bytes() // 2), lambda *shape: Elsewhere(bf16(*shape))
+    weight = layer.w4_pack(torch.zeros((16, 64), dtype=torch.uint8), bf16(16, 2), stream=Stream)
+    there = binding.W4Weight(Elsewhere(weight.data), weight.n, weight.k, weight.group, weight.with_zeros)
+    u8 = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    layer.lib.calls.clear()
+    for call in (lambda: layer.window_attention(plan, far(1, 512), pool, stream=Stream), lambda: layer.window_attention(plan, bf16(1, 512), Elsewhere(pool), stream=Stream),
+                 lambda: layer.window_attention(plan, bf16(1, 512), pool, out=far(1, 512), stream=Stream),
+                 lambda: layer.rope_append(plan, far(1, SHAPE.n_qkv), pool, stream=Stream), lambda: layer.rope_append(plan, bf16(1, SHAPE.n_qkv), Elsewhere(pool), stream=Stream),
+                 lambda: layer.rope_append(plan, bf16(1, SHAPE.n_qkv), pool, q=far(1, 512), stream=Stream),
+                 lambda: layer.w4_pack(Elsewhere(u8(16, 64)), bf16(16, 2), u8(16, 2), stream=Stream), lambda: layer.w4_pack(u8(16, 64), far(16, 2), u8(16, 2), stream=Stream),
+                 lambda: layer.w4_pack(u8(16, 64), bf16(16, 2), Elsewhere(u8(16, 2)), stream=Stream),
+                 lambda: layer.w4_linear(far(2, 128), weight, stream=Stream), lambda: layer.w4_linear(bf16(2, 128), there, stream=Stream),
+                 lambda: layer.w4_linear(bf16(2, 128), weight, out=far(2, 16), stream=Stream),
+                 lambda: layer.copy_pages([pool, Elsewhere(pool)], [0], [1], stream=Stream), lambda: layer.compact_pages([pool, Elsewhere(pool)], [0], stream=Stream)):
+        with pytest.raises(ValueError, match=" on cuda:3"):
+            call()
+    assert not layer.lib.calls
+
+
+class Elsewhere:
+    """A tensor that says it is on another device."""
+
+    def __init__(self, t):
+        self._t, self.device = t, torch.device("cuda", 3)
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+    def get_device(self):
+        return 3
