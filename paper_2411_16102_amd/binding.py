@@ -466,6 +466,16 @@ class Layer:
 
 
     # -- streams (blendstep_stream.h) ---------------------------------------------------
+    # `stream` (PyTorch's current one if None): where a call's work goes.  A result that the caller does not give is allocated for
+    # that stream, so that its memory is neither somebody else's yet nor anybody's before the work is done.  As with every call on a
+    # stream other than the current one, the caller orders it behind what makes its inputs, keeps these until it is done, and orders what reads
+    # the result behind it (Stream.wait_stream, Tensor.record_stream).
+    def _new(self, like, shape, stream):
+        if stream is None:
+            return like.new_empty(shape)
+        with self.torch.cuda.stream(stream):
+            return like.new_empty(shape)
+
     def window_plan(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages: Optional[int] = None, stream=None):
         """The plan of a step for window_attention and rope_append (bs_window_plan): one for all layers with this window, which may
         be other Layer objects with the same heads, pages and rope_theta on the same device.
@@ -478,7 +488,7 @@ class Layer:
         width = self._q_width
         q_stride = self._row_stride(plan, q, width)
         if out is None:
-            out, out_stride = q.new_empty((plan.n_rows, width)), width
+            out, out_stride = self._new(q, (plan.n_rows, width), stream), width
         else:
             out_stride = self._row_stride(plan, out, width)
         self._check_pool(plan, kv_pool)
@@ -493,7 +503,7 @@ class Layer:
         handle = self._plan_handle(plan)
         stride = self._row_stride(plan, qkv, self._qkv_width)
         if q is None:
-            q, q_stride = qkv.new_empty((plan.n_rows, self._q_width)), self._q_width
+            q, q_stride = self._new(qkv, (plan.n_rows, self._q_width), stream), self._q_width
         else:
             q_stride = self._row_stride(plan, q, self._q_width)
         self._check_pool(plan, kv_pool)
@@ -548,7 +558,7 @@ class Layer:
                 (zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != scales.shape)):
             raise ValueError("w4_pack: uint8 [n, k / 2], bf16 scales and uint8 zeros [n, k / group]")
         size = int(self.lib.bs_w4_bytes(n, k, group, int(zeros is not None)))
-        data = torch.empty(max(16, size), dtype=torch.uint8, device=packed.device)
+        data = self._new(packed, (max(16, size),), stream)
         self._check(self.lib.bs_w4_pack(self.h, packed.data_ptr(), scales.data_ptr(), zeros.data_ptr() if zeros is not None else None, n, k,
                                         group, data.data_ptr(), self._raw_stream(stream)))
         return W4Weight(data, n, k, group, zeros is not None)
@@ -567,9 +577,10 @@ class Layer:
         elif inner != 1:
             raise ValueError("w4_linear: rows of x are not contiguous")
         if out is None:
-            out, out_stride = x.new_empty((m, weight.n)), weight.n
+            out, out_stride = self._new(x, (m, weight.n), stream), weight.n
         else:
-            self._here("w4_linear", out)
+            if out.get_device() != self.device:
+                self._here("w4_linear", out)
             if out.dtype is not x.dtype or out.shape != (m, weight.n) or out.stride(1) != 1:
                 raise ValueError("w4_linear: out is not bf16 [%d, %d]" % (m, weight.n))
             out_stride = out.stride(0)

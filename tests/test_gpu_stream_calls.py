@@ -26,3 +26,34 @@ def test_host_tensors_are_refused(lib):
                  lambda: layer.copy_pages([pool], [0], [1]), lambda: layer.compact_pages([pool.cuda(), pool], [0, 2])):
         with pytest.raises(ValueError, match=" on cpu"):
             call()
+
+
+def test_results_of_calls_on_another_stream(lib):
+    # results that the calls allocate belong to the side stream: equal to those of the current one, and their memory
+    # does not go back to the current stream's when they are dropped
+    import torch
+    layer = lib.Layer(SHAPE, device=0)
+    batch = make_batch([(1, 3000), (200, 700), (1, 0)])
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda *shape: torch.randn(shape, device="cuda", generator=gen).to(torch.bfloat16)
+    pool, qkv, x = new(batch.n_pages * layer.page_bytes() // 2), new(batch.n_rows, SHAPE.n_qkv), new(40, 256)
+    packed, scales = torch.randint(0, 256, (520, 128), dtype=torch.uint8, device="cuda", generator=gen), new(520, 4)
+    plan = layer.window_plan(batch, 500, 4)
+
+    def results(stream=None):
+        q = layer.rope_append(plan, qkv, pool, stream=stream)
+        weight = layer.w4_pack(packed, scales, stream=stream)
+        return [q, layer.window_attention(plan, q, pool, stream=stream), weight.data, layer.w4_linear(x, weight, stream=stream)]
+
+    want = results()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        got = results(side)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        places, sizes = [t.data_ptr() for t in got], [t.shape for t in got]
+        types = [t.dtype for t in got]
+        del got
+        again = [torch.empty(s, dtype=d, device="cuda") for s, d in zip(sizes, types)]
+        assert not set(places) & {t.data_ptr() for t in again}

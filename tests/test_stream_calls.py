@@ -29,7 +29,14 @@ class Asked:
 
 
 class Stream:
+    """A stream in name: contexts without a device use none."""
     cuda_stream = 0
+
+
+@pytest.fixture(autouse=True)
+def _streams_in_name(monkeypatch):
+    from contextlib import nullcontext
+    monkeypatch.setattr(torch.cuda, "stream", nullcontext)
 
 
 def make_layer(shape=SHAPE, rc=0):
@@ -205,3 +212,38 @@ class Elsewhere:
 
     def get_device(self):
         return 3
+
+
+# ---- results on another stream ------------------------------------------------------------------
+class Allocating(torch.Tensor):
+    """A tensor that writes down under which stream memory like its own is asked for."""
+    current, asked = None, []
+
+    def new_empty(self, *args, **kw):
+        Allocating.asked.append(Allocating.current)
+        return self.as_subclass(torch.Tensor).new_empty(*args, **kw)
+
+
+def test_results_are_allocated_for_the_stream_of_the_call(monkeypatch):
+    from contextlib import contextmanager
+
+    @contextmanager
+    def under(stream):
+        Allocating.current = stream
+        yield
+        Allocating.current = None
+    monkeypatch.setattr(torch.cuda, "stream", under)
+    monkeypatch.setattr(binding, "_current_stream", lambda device: 0)
+    monkeypatch.setattr(Allocating, "asked", [])
+    layer = make_layer()
+    batch = make_batch([(1, 40)])
+    plan, pool = layer.window_plan(batch, 8), bf16(batch.n_pages * layer.page_bytes() // 2)
+    mine = lambda t: t.as_subclass(Allocating)
+    weight = layer.w4_pack(torch.zeros((16, 64), dtype=torch.uint8), bf16(16, 2))
+    for stream in (Stream, None):
+        Allocating.asked.clear()
+        layer.window_attention(plan, mine(bf16(1, 512)), pool, stream=stream)
+        layer.rope_append(plan, mine(bf16(1, SHAPE.n_qkv)), pool, stream=stream)
+        layer.w4_pack(mine(torch.zeros((16, 64), dtype=torch.uint8)), bf16(16, 2), stream=stream)
+        layer.w4_linear(mine(bf16(2, 128)), weight, stream=stream)
+        assert Allocating.asked == [stream] * 4
