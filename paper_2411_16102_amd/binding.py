@@ -528,6 +528,8 @@ class Layer:
     def _row_stride(self, plan, t, width):
         if t.dtype is self._bf16_type and t.shape == (plan.n_rows, width) and t.get_device() == self.device:
             stride, inner = t.stride()
+            if plan.n_rows == 1 and inner == 1:
+                return self._qkv_width  # (a single row has no stride: one for all tensors, so that in place stays in place)
             if inner == 1 or not plan.n_rows:
                 return stride
         raise ValueError("expected bf16 rows [%d, %d] on device %d, got %s %s on %s" % (plan.n_rows, width, self.device, t.dtype, tuple(t.shape), t.device))
@@ -576,14 +578,18 @@ class Layer:
             stride = 0
         elif inner != 1:
             raise ValueError("w4_linear: rows of x are not contiguous")
+        elif m == 1:
+            stride = weight.k  # (a single row has no stride)
         if out is None:
             out, out_stride = self._new(x, (m, weight.n), stream), weight.n
         else:
             if out.get_device() != self.device:
                 self._here("w4_linear", out)
-            if out.dtype is not x.dtype or out.shape != (m, weight.n) or out.stride(1) != 1:
+            out_stride, inner = out.stride() if out.dim() == 2 else (0, 0)
+            if out.dtype is not x.dtype or out.shape != (m, weight.n) or (inner != 1 and weight.n > 1 and m):
                 raise ValueError("w4_linear: out is not bf16 [%d, %d]" % (m, weight.n))
-            out_stride = out.stride(0)
+            if m == 1:
+                out_stride = weight.n
         rc = self.lib.bs_w4_linear(self.h, x.data_ptr(), stride, weight.data.data_ptr(), m, weight.n, weight.k, weight.group, weight.with_zeros, out.data_ptr(),
                                    out_stride, self._raw_stream(stream))
         if rc:

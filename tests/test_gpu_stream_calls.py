@@ -57,3 +57,27 @@ def test_results_of_calls_on_another_stream(lib):
         del got
         again = [torch.empty(s, dtype=d, device="cuda") for s, d in zip(sizes, types)]
         assert not set(places) & {t.data_ptr() for t in again}
+
+
+def test_single_rows_and_columns_at_any_stride(lib):
+    import torch
+    layer = lib.Layer(SHAPE, device=0)
+    batch = make_batch([(1, 300)])
+    new = lambda *shape: torch.randn(shape, device="cuda").to(torch.bfloat16)
+    row = lambda t: t.reshape(-1, 1).clone().t()
+    pool, qkv, x = new(batch.n_pages * layer.page_bytes() // 2), new(1, SHAPE.n_qkv), new(1, 256)
+    assert row(qkv).stride() == (1, 1)
+    plan = layer.window_plan(batch, 100, 4)
+    weight = layer.w4_pack(torch.randint(0, 256, (77, 128), dtype=torch.uint8, device="cuda"), new(77, 4))
+    q = layer.rope_append(plan, qkv, pool)
+    out, y = layer.window_attention(plan, q, pool), layer.w4_linear(x, weight)
+    assert torch.equal(layer.rope_append(plan, row(qkv), pool, q=row(q)), q)
+    mine = row(qkv)
+    layer.rope_append(plan, mine, pool, q=mine[:, :512])
+    assert torch.equal(mine[:, :512], q) and torch.equal(mine[:, 512:], qkv[:, 512:])
+    mine = row(q)
+    assert torch.equal(layer.window_attention(plan, mine, pool, out=mine), out)
+    assert torch.equal(layer.w4_linear(row(x), weight, out=row(y)), y)
+    one = layer.w4_pack(torch.randint(0, 256, (1, 128), dtype=torch.uint8, device="cuda"), new(1, 4))
+    xs, ys = new(5, 256), torch.zeros((1, 5), dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(layer.w4_linear(xs, one, out=ys.t()), layer.w4_linear(xs, one))

@@ -247,3 +247,53 @@ def test_results_are_allocated_for_the_stream_of_the_call(monkeypatch):
         layer.w4_pack(mine(torch.zeros((16, 64), dtype=torch.uint8)), bf16(16, 2), stream=stream)
         layer.w4_linear(mine(bf16(2, 128)), weight, stream=stream)
         assert Allocating.asked == [stream] * 4
+
+
+# ---- strides that no element uses ---------------------------------------------------------------
+def row(k, offset=0):
+    """A row of k elements, contiguous, whose stride along the rows is one."""
+    t = torch.zeros((offset + k, 1), dtype=torch.bfloat16)[offset:].t()
+    assert t.is_contiguous() and t.stride() == (1, 1)
+    return t
+
+
+def test_the_stride_of_a_single_row_is_not_looked_at():
+    layer = make_layer()
+    batch = make_batch([(1, 40)])
+    plan, pool = layer.window_plan(batch, 8), bf16(batch.n_pages * layer.page_bytes() // 2)
+    calls = layer.lib.calls
+    q, out = row(512), row(512)
+    layer.window_attention(plan, q, pool, out=out, stream=Stream)
+    layer.window_attention(plan, q, pool, out=q, stream=Stream)
+    layer.window_attention(plan, q, pool, out=bf16(1, 512), stream=Stream)
+    for _, (_, _, q_stride, _, out_stride, _, _) in calls:
+        assert q_stride >= 512 and out_stride >= 512 and q_stride % 8 == 0 and out_stride % 8 == 0
+    assert calls[1][1][2] == calls[1][1][4], "in place with one stride"
+    calls.clear()
+    qkv = row(SHAPE.n_qkv)
+    layer.rope_append(plan, qkv, pool, stream=Stream)
+    layer.rope_append(plan, qkv, pool, q=qkv[:, :512], stream=Stream)
+    layer.rope_append(plan, bf16(1, SHAPE.n_qkv), pool, q=row(512), stream=Stream)
+    for _, (_, _, stride, _, q_stride, _, _) in calls:
+        assert stride >= SHAPE.n_qkv and q_stride >= 512 and stride % 8 == 0 and q_stride % 8 == 0
+    assert calls[1][1][1] == calls[1][1][3] and calls[1][1][2] == calls[1][1][4], "in place with one stride"
+    calls.clear()
+    weight = layer.w4_pack(torch.zeros((17, 64), dtype=torch.uint8), bf16(17, 2), stream=Stream)
+    layer.w4_linear(row(128), weight, out=row(17), stream=Stream)
+    stride, out_stride = calls[-1][1][2], calls[-1][1][10]
+    assert stride >= 128 and stride % 8 == 0 and out_stride >= 17
+    # rows that are not contiguous in themselves, and strides of several rows, are refused as before
+    for bad in (lambda: layer.window_attention(plan, bf16(1, 1024)[:, ::2], pool, stream=Stream), lambda: layer.w4_linear(bf16(1, 256)[:, ::2], weight, stream=Stream),
+                lambda: layer.w4_linear(bf16(2, 128), weight, out=bf16(17, 2).t(), stream=Stream)):
+        with pytest.raises(ValueError):
+            bad()
+
+
+def test_the_stride_of_a_single_column_is_not_looked_at():
+    layer = make_layer()
+    weight = layer.w4_pack(torch.zeros((1, 64), dtype=torch.uint8), bf16(1, 2), stream=Stream)
+    out = bf16(1, 5).t()
+    assert out.shape == (5, 1) and out.stride() == (1, 5)
+    layer.w4_linear(bf16(5, 128), weight, out=out, stream=Stream)
+    assert layer.lib.calls[-1][1][10] == 1
+    layer.w4_linear(bf16(0, 128), weight, out=bf16(1, 0).t(), stream=Stream)
