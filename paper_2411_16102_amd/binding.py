@@ -10,6 +10,7 @@ import ctypes as C
 import os
 import re
 from dataclasses import dataclass
+from operator import index
 from typing import Optional
 
 import numpy as np
@@ -650,14 +651,38 @@ class _Words:
 
     def put(self, values):
         """(address, how many) of a copy."""
-        v = np.asarray(values, dtype=np.int32)
+        v = _i32(values)
         at = self.room(v.size)
         self.a[:v.size] = v.reshape(-1)
         return at, v.size
 
 
+_INT32 = np.dtype(np.int32)
+
+
 def _i32(a) -> np.ndarray:
-    return np.ascontiguousarray(a, dtype=np.int32)
+    """The whole numbers `a` in 32 bits; others, and longer ones, are refused (a cast would cut them off)."""
+    v = a if type(a) is np.ndarray else np.asarray(a)
+    if v.dtype is not _INT32:
+        with np.errstate(invalid="ignore"):
+            w = v.astype(np.int32)
+        if not (w == v).all():
+            raise ValueError("whole numbers of 32 bits are expected")
+        v = w
+    return v if v.flags.c_contiguous else np.ascontiguousarray(v)
+
+
+def _count(n) -> int:
+    """A number for an int32 argument (ctypes would cut a longer one off)."""
+    n = index(n)
+    if not -0x80000000 <= n <= 0x7FFFFFFF:
+        raise ValueError("%d does not fit 32 bits" % n)
+    return n
+
+
+def _limit(n) -> int:
+    """A window or a number of sinks, which may exceed every length."""
+    return max(-1, min(index(n), 0x7FFFFFFF))
 
 
 def _current_stream(device: int) -> int:
@@ -721,7 +746,7 @@ class WindowPlan:
                 raise ValueError("positions [n_axes, %d] and axis_of_pair [%d]" % (batch.n_rows, lay.shape.head_dim // 2))
         pages = batch.n_pages if n_pages is None else n_pages
         where = lay._raw_stream(stream) if lay.device >= 0 else None
-        lay._check(lay.lib.bs_window_plan(self.h, C.byref(d), pages, window, sinks, axes, None if pos is None else _ptr(pos),
+        lay._check(lay.lib.bs_window_plan(self.h, C.byref(d), pages, _limit(window), _limit(sinks), axes, None if pos is None else _ptr(pos),
                                           None if axis is None else _ptr(axis), where))
         self.n_rows, self.n_pages = batch.n_rows, pages
         return self
@@ -756,7 +781,7 @@ class Pages:
 
     def __init__(self, n_pages: int):
         self.lib = raw()
-        self.n_pages = int(n_pages)
+        self.n_pages = _count(n_pages)
         h = C.c_void_p()
         rc = self.lib.bs_pages_create(self.n_pages, C.byref(h))
         if rc != 0:
@@ -781,14 +806,14 @@ class Pages:
 
     def open(self, n: int = 1) -> np.ndarray:
         """Ids of n new, empty sequences."""
-        out = self._out.room(n)
+        out = self._out.room(_count(n))
         self._check(self.lib.bs_pages_open(self.h, n, out))
         return self._out.a[:n].copy()
 
     def fork(self, parents, children: int = 1) -> np.ndarray:
         """Ids of `children` new sequences for each parent, which share its pages."""
         at, n = self._ids.put(parents)
-        out = self._out.room(n * max(0, children))
+        out = self._out.room(_count(n * max(0, _count(children))))
         self._check(self.lib.bs_pages_fork(self.h, at, n, children, out))
         return self._out.a[:n * children].copy()
 
@@ -796,7 +821,7 @@ class Pages:
         """Room for further tokens; (src, dst) of the pages to copy in every pool before they are written to."""
         at, n = self._ids.put(ids)
         more = self._out.room(n)
-        self._out.a[:n] = tokens
+        self._out.a[:n] = _count(tokens) if type(tokens) is int else _i32(tokens)
         src, dst = self._src.room(n), self._dst.room(n)
         self._check(self.lib.bs_pages_extend(self.h, at, more, n, src, dst, self._count.at))
         n = int(self._count.a[0])
@@ -805,7 +830,7 @@ class Pages:
     def trim(self, ids, window: int, sinks: int = 0):
         """Gives up the pages that no later row sees; their entries in the tables become -1."""
         at, n = self._ids.put(ids)
-        self._check(self.lib.bs_pages_trim(self.h, at, n, window, sinks))
+        self._check(self.lib.bs_pages_trim(self.h, at, n, _limit(window), _limit(sinks)))
 
     def free(self, ids):
         at, n = self._ids.put(ids)

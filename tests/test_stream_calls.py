@@ -297,3 +297,59 @@ def test_the_stride_of_a_single_column_is_not_looked_at():
     layer.w4_linear(bf16(5, 128), weight, out=out, stream=Stream)
     assert layer.lib.calls[-1][1][10] == 1
     layer.w4_linear(bf16(0, 128), weight, out=bf16(1, 0).t(), stream=Stream)
+
+
+# ---- numbers that do not fit ----------------------------------------------------------------------
+BIG = 1 << 32
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    p = binding.Pages(20)
+    ids = p.open(2)
+    p.extend(ids, [5, 17])
+    for call in (lambda: binding.Pages(BIG + 3), lambda: p.open(BIG + 1), lambda: p.fork(ids, BIG + 1), lambda: p.fork(ids, (1 << 31) - 1), lambda: p.extend(ids, BIG + 1),
+                 lambda: p.extend(ids, np.array([1, BIG + 1])), lambda: p.extend(ids, np.array([1.0, 1.5])), lambda: p.extend(ids, [0.5, 1]),
+                 lambda: p.extend(ids.astype(np.int64) + BIG, 1), lambda: p.free(np.array([BIG])), lambda: p.tables(np.array([-BIG])), lambda: p.fork(np.array([np.nan]), 1)):
+        with pytest.raises(ValueError):
+            call()
+    assert p.lengths(ids).tolist() == [5, 17] and p.stats() == {"free": 17, "sequences": 2}
+    # whole numbers of any type are taken
+    p.extend(ids.astype(np.int64), np.array([1.0, 2.0]))
+    p.extend([int(i) for i in ids], np.uint8(3))
+    p.extend(ids, 1)
+    assert p.lengths(ids).tolist() == [10, 23]
+
+
+def test_tables_and_positions_beyond_32_bits_are_refused():
+    layer = make_layer()
+    pool = bf16(4 * layer.page_bytes() // 2)
+    for call in (lambda: layer.copy_pages([pool], np.array([BIG]), [1], stream=Stream), lambda: layer.copy_pages([pool], [0], np.array([BIG + 1]), stream=Stream),
+                 lambda: layer.compact_pages([pool], np.array([BIG + 1]), stream=Stream), lambda: layer.compact_pages([pool], [0.5], stream=Stream)):
+        with pytest.raises(ValueError):
+            call()
+    assert not layer.lib.calls
+    batch = make_batch([(2, 40)])
+    for bad in (np.full((1, 2), BIG), np.full((1, 2), 0.5)):
+        with pytest.raises(ValueError):
+            layer.window_plan(batch, 8, positions=bad, axis_of_pair=np.zeros(32))
+    layer.window_plan(batch, 8, positions=np.full((1, 2), 7.0), axis_of_pair=np.zeros(32))
+
+
+def test_windows_and_sinks_beyond_every_length():
+    layer = make_layer()
+    batch = make_batch([(1, 1000)])
+    for window, sinks, pages in ((BIG + 5, 0, 63), (BIG, 0, 63), (1 << 31, 0, 63), (16, BIG, 63), (16, BIG + 3, 63), (8, 0, 1), (np.int64(17), np.int64(0), 2)):
+        assert layer.window_plan(batch, window, sinks).division().pages == pages
+    for window, sinks in ((5 - BIG, 0), (16, 3 - BIG)):
+        with pytest.raises(binding.BlendStepError, match="at least"):
+            layer.window_plan(batch, window, sinks)
+    p = binding.Pages(63)
+    ids = p.open(1)
+    p.extend(ids, 1000)
+    for window, sinks in ((BIG + 5, 0), (BIG, 0), (16, BIG), (16, BIG + 3)):
+        p.trim(ids, window, sinks)
+        assert (p.tables(ids)[1] >= 0).all()
+    with pytest.raises(binding.BlendStepError, match="at least"):
+        p.trim(ids, 5 - BIG, 0)
+    p.trim(ids, 16, 0)
+    assert (p.tables(ids)[1] >= 0).sum() == 2
