@@ -701,6 +701,12 @@ class W4Weight:
     group: int
     with_zeros: bool
 
+    def __post_init__(self):
+        # (the kernels read the layout of this shape whole)
+        size = int(raw().bs_w4_bytes(self.n, self.k, self.group, int(self.with_zeros)))
+        if not self.data.is_contiguous() or self.data.numel() * self.data.element_size() < size:
+            raise ValueError("the laid-out weight [%d, %d] has %d contiguous bytes" % (self.n, self.k, size))
+
 
 class _PlanHandle:
     """A bs_window, which its context has to outlive: the layer knows the handle, not the plan, and closes it before its own, whichever

@@ -353,3 +353,17 @@ def test_windows_and_sinks_beyond_every_length():
         p.trim(ids, 5 - BIG, 0)
     p.trim(ids, 16, 0)
     assert (p.tables(ids)[1] >= 0).sum() == 2
+
+
+# ---- laid-out weights --------------------------------------------------------------------------------
+def test_weights_with_less_memory_than_their_layout_are_refused():
+    layer = make_layer()
+    w = layer.w4_pack(torch.zeros((17, 64), dtype=torch.uint8), bf16(17, 2), torch.zeros((17, 2), dtype=torch.uint8), stream=Stream)
+    size = layer.lib.bs_w4_bytes(17, 128, 64, 1)
+    assert w.data.numel() == size
+    binding.W4Weight(w.data, 17, 128, 64, True)
+    binding.W4Weight(w.data, 17, 128, 64, False)
+    binding.W4Weight(bf16(size // 2), 17, 128, 64, True)
+    for data, n, k in ((w.data[:-1], 17, 128), (w.data, 33, 128), (w.data, 17, 256), (torch.zeros(2 * size, dtype=torch.uint8)[::2], 17, 128)):
+        with pytest.raises(ValueError, match="laid-out weight"):
+            binding.W4Weight(data, n, k, 64, True)
