@@ -144,7 +144,9 @@ int add_rows(bs_window *w, const bs_batch *b, int s, int j, int end, int per_uni
 // How narrow work is cut: wavefronts of a workgroup, pages of a unit, and the microseconds that are expected of it.  Timed for 1 to 256 streams
 // of four head layouts, windows of 64 to 4096, each with 1 to 8 wavefronts and 4 to 256 pages: within 2 % of the best of them on
 // average, 11 % at worst (one stream, window 1024, 8 KV heads: 6 units of 12 pages 9.2 us, one of 66 on eight wavefronts 18; 64 of window 4096: whole
-// on eight 169, halves 187).
+// on eight 169, halves 187).  84 batches of 200 to 2048 streams of 1 to 1100 pages, most of them unequal: 2.6 % on average, 10 %
+// at worst (one stream of 100 pages beside 255 of 4, 8 KV heads: whole 38.4 us, cut 20.0; one of 256 beside 255 of 32: 139 and 101; 256 of 64 each: 163
+// whole, halves 190).
 struct Division {
   int waves, pages;
   double us;
@@ -160,6 +162,8 @@ Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int dh, int n
   }
   // A CU streams 36 GB/s of pages however many ask, a unit's pages go through one; a join waits for a round trip and one more for every
   // eight units or so.
+  // Where units are many, each is one wavefront's, which takes as long beside others as the memory keeps it waiting.
+  const double us_alone = dh == 128 ? 0.27 : 0.22;
   const double us_per_page = dh == 128 ? 0.23 : 0.13, all_us = (double)once * hkv * dh * (4.0 * PAGE / 5.9e6);
   double best = 0;
   Division div = {1, std::max(2, longest), 0.0};
@@ -167,11 +171,22 @@ Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int dh, int n
   for (int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
     const int pages = std::max(2, 2 * ((longest + 2 * n - 1) / (2 * n)));
     if (n > 1 && pages < 4) break;
-    int64_t units = 0;
-    for (const bs_window::Rows &r : rows) units += std::max(1, (r.pages + pages - 1) / pages);
+    int64_t units = 0, joined = 0;
+    for (const bs_window::Rows &r : rows) {
+      const int k = std::max(1, (r.pages + pages - 1) / pages);
+      units += k;
+      joined += k > 1 ? k : 0;
+    }
     units *= hkv;
-    const double rounds = units <= 4 * (int64_t)n_cu ? (double)((units + n_cu - 1) / n_cu) : 0.5 + (double)all * hkv / pages / n_cu;
-    const double cost = std::max(all_us, us_per_page * pages * rounds) + (n > 1 ? 2.0 + 0.25 * n + 0.004 * (double)units : 0.0);
+    joined *= hkv;
+    double cost;
+    if (units <= 4 * (int64_t)n_cu) {
+      const double rounds = (double)((units + n_cu - 1) / n_cu);
+      cost = std::max(all_us, us_per_page * pages * rounds) + (n > 1 ? 2.0 + 0.25 * n + 0.004 * (double)units : 0.0);
+    } else {
+      cost = std::max({all_us, us_per_page * (0.5 * pages + (double)all * hkv / n_cu), us_alone * std::min(pages, longest) + 0.7 * all_us}) +
+             (joined ? 2.0 + 0.25 * n + 0.0045 * (double)joined : 0.0);
+    }
     if (n == 1 || cost < best) {
       best = cost;
       div.pages = std::max(2, pages);

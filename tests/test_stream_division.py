@@ -1,0 +1,30 @@
+"""How planned steps of streams are divided (host only): the kernels' paths that a batch takes, by its lengths."""
+import numpy as np
+import pytest
+
+from paper_2411_16102_amd import binding, workloads as W
+from stream_cases import make_batch
+
+WHOLE = 1 << 30  # a window that sees everything: a stream's pages are its length's
+
+
+def streams(*runs):
+    """(how many, pages) each."""
+    return make_batch([(1, 16 * pages) for n, pages in runs for _ in range(n)])
+
+
+@pytest.mark.parametrize("hkv,dh,runs,cut", [
+    # one old stream among many young ones: whole it would outlast them all
+    (8, 128, [(255, 4), (1, 100)], True), (8, 64, [(255, 4), (1, 100)], True), (8, 128, [(255, 32), (1, 256)], True), (8, 64, [(255, 32), (1, 256)], True),
+    (16, 128, [(255, 4), (1, 200)], True), (8, 128, [(255, 64), (1, 512)], True), (8, 128, [(511, 8), (1, 256)], True),
+    # batches of equal streams fill the chip whole, and so do those whose longest ends with the others
+    (8, 128, [(256, 64)], False), (8, 64, [(256, 64)], False), (8, 128, [(512, 16)], False), (8, 128, [(128, 64), (128, 40)], False)])
+def test_long_streams_among_many(hkv, dh, runs, cut):
+    layer = binding.Layer(W.LayerShape(256, 2 * hkv, hkv, dh, 256), device=-1)
+    d = layer.window_plan(streams(*runs), WHOLE).division()
+    longest = max(pages for _, pages in runs)
+    assert (d.split_rows > 0) == cut
+    assert d.longest_pages <= longest // 2 if cut else d.longest_pages == longest
+    if cut:
+        # only streams that are longer than a unit
+        assert d.split_rows <= sum(n for n, pages in runs if pages > d.longest_pages)
