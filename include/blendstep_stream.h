@@ -78,6 +78,7 @@ typedef struct bs_window_parts {
   int32_t split_rows;    /* rows whose pages are split over several units and joined */
   int32_t wide_blocks;   /* wide work: blocks of rows of longer segments (per group of heads) */
   int32_t wide_cut;      /* of these, blocks whose pages are cut into ranges and joined */
+  int32_t waves;         /* wavefronts of a workgroup that share a unit's pages (1, 2, 4 or 8) */
   int64_t pages;         /* pages that the units and blocks name */
 } bs_window_parts;
 int bs_window_division(const bs_window *w, bs_window_parts *out);

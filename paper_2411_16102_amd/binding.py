@@ -56,7 +56,7 @@ class Division(C.Structure):
 
 
 class WindowParts(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("units", "longest_pages", "split_rows", "wide_blocks", "wide_cut")] + [("pages", C.c_int64)]
+    _fields_ = [(n, C.c_int32) for n in ("units", "longest_pages", "split_rows", "wide_blocks", "wide_cut", "waves")] + [("pages", C.c_int64)]
 
 
 class SplitInfo(C.Structure):

@@ -698,7 +698,7 @@ int bs_window_division(const bs_window *w, bs_window_parts *out) {
   if (!out) return ctx_fail(w->ctx, BS_EINVAL, "out is NULL");
   if (!w->p.made) return ctx_fail(w->ctx, BS_EINVAL, "bs_window_division: nothing is planned");
   const Planned &p = w->p;
-  *out = {p.n_items, p.longest, p.split_rows, p.wide_blocks, p.n_cut, p.pages};
+  *out = {p.n_items, p.longest, p.split_rows, p.wide_blocks, p.n_cut, p.waves, p.pages};
   return BS_OK;
 }
 

@@ -9,8 +9,21 @@ WHOLE = 1 << 30  # a window that sees everything: a stream's pages are its lengt
 
 
 def streams(*runs):
-    """(how many, pages) each."""
-    return make_batch([(1, 16 * pages) for n, pages in runs for _ in range(n)])
+    """(how many, pages) each; the last pages are not all full."""
+    return make_batch([(1, 16 * pages - i % 7) for n, pages in runs for i in range(n)])
+
+
+# KV heads, streams, wavefronts that share a unit's pages, whether units are cut and joined: every kernel of single tokens
+SHARED = [(8, [(200, 12)], 1, False), (8, [(255, 4), (1, 200)], 1, True), (4, [(100, 33)], 2, False), (1, [(1, 400)], 2, True),
+          (1, [(250, 66)], 4, False), (1, [(32, 400)], 4, True), (1, [(200, 130)], 8, False), (1, [(48, 600)], 8, True)]
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("hkv,runs,waves,cut", SHARED)
+def test_wavefronts_of_a_unit(hkv, runs, waves, cut, dh):
+    layer = binding.Layer(W.LayerShape(256, 2 * hkv, hkv, dh, 256), device=-1)
+    d = layer.window_plan(streams(*runs), WHOLE).division()
+    assert (d.waves, d.split_rows > 0, d.wide_blocks) == (waves, cut, 0)
 
 
 @pytest.mark.parametrize("hkv,dh,runs,cut", [
