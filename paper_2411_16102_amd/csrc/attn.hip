@@ -463,7 +463,7 @@ __device__ __forceinline__ void prefill_workgroup(const Args &a, int heads_per_w
         const int lim = my_pos[qb] - window - tb * 32 - 8 * g2, sink_lim = sinks - tb * 32 - 8 * g2;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          s[r] = (16 * (r >> 3) + (r & 7) <= lim) & (16 * (r >> 3) + (r & 7) >= sink_lim) ? HIDDEN : s[r];
+          s[r] = ((16 * (r >> 3) + (r & 7) <= lim) & (16 * (r >> 3) + (r & 7) >= sink_lim)) ? HIDDEN : s[r];  // (no branch: see window_device.hpp)
         mx = max_of(s);
       }
     mx *= a.s.scale_log2e;  // the scale is positive: the maximum commutes with it

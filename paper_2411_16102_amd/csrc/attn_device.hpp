@@ -50,7 +50,7 @@ __device__ __forceinline__ u32x4_t mask_tokens8(u32x4_t v, int t0, int limit) {
 __device__ __forceinline__ u32x4_t mask_between8(u32x4_t v, int t0, int lo, int hi) {
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    v[i >> 1] &= (t0 + i >= lo) & (t0 + i < hi) ? (i & 1 ? 0x0000FFFFu : 0xFFFF0000u) : 0xFFFFFFFFu;
+    v[i >> 1] &= ((t0 + i >= lo) & (t0 + i < hi)) ? (i & 1 ? 0x0000FFFFu : 0xFFFF0000u) : 0xFFFFFFFFu;  // (no branch: see window_device.hpp)
   return v;
 }
 

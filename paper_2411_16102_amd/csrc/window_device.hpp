@@ -81,7 +81,9 @@ __device__ __forceinline__ void walk_pages(const WindowArgs &a, const WindowItem
       const int unseen = first - a.window + 1;
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        // (one condition without branches: with || and && the compiler's code lost the middle one)
+        // (One condition, selected by: of an element that is written behind || and && the compiler made branches whose intermediate code is
+        // right, and machine code that is not: -inf is written ahead of them, taken back for lanes that pass the first condition, and the block
+        // for those that fail a later one is empty.)
         const int u = u0 + r;
         const bool hidden = (u > at) | ((u <= at - a.window) & (u >= sinks)) | (u >= 16 * n_pg);
         sv[r] = hidden ? -INFINITY : sv[r];
