@@ -58,13 +58,14 @@ int bs_window_plan(bs_window *w, const bs_batch *batch, int64_t n_pages, int32_t
 
 /* Turns the queries and keys of fused rows and appends keys and values to the pages of their positions.
  * qkv: device bf16, row r at qkv + r * qkv_stride elements: Hq query heads, Hkv key heads, Hkv value heads of head_dim each.
- * q: device bf16, row r at q + r * q_stride, Hq heads; may be qkv itself (the same stride: turned in place).
+ * q: device bf16, row r at q + r * q_stride, Hq heads; may be qkv itself (the same stride: turned in place), and must not overlap it otherwise.
  * Rows are 16-byte aligned: strides are multiples of 8 elements.  Angles: pos * rope_theta^(-2i/dh) from the
  * context's table (evaluated in 64 bits, kept in 32); products in 32 bits, rounded once. */
 int bs_rope_append(bs_window *w, const void *qkv, int64_t qkv_stride, void *q, int64_t q_stride, void *kv_pool, void *stream);
 
 /* Attention of the plan's rows over the pool (this step's keys and values are in it already).  q, out: device bf16, Hq heads a row,
- * strides as above; out may be q itself where both strides are equal.  Softmax statistics and sums in 32 bits;
+ * strides as above; out may be q itself where both strides are equal, and must not overlap it otherwise.  Softmax statistics and sums in 32
+ * bits (they begin at -1e30: a row that sees nothing above that gives zeros, as one that sees nothing);
  * probabilities enter their product with V in bf16.  Tokens that no row of a sequence's call sees do not reach any result, whatever bits
  * their slots hold; a NaN or an infinity in a value that one row sees may also reach
  * rows of the same sequence that do not see it. */

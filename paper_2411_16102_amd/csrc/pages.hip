@@ -15,7 +15,7 @@ using namespace bs;
 namespace {
 
 // A workgroup per page and pool.  pools [n_pools] addresses (two words each), then n pairs (src, dst), in pinned memory; 16-byte
-// units of a page.  Bound by memory: 502 pages of 64 KB in 16 pools 210 us, 5.0 TB/s; 120 copies of 15 pages in 32 pools, whose sources
+// units of a page.  Bound by memory: 502 pages of 64 KB in 16 pools 196 to 210 us, 5.0 to 5.4 TB/s; 120 copies of 15 pages in 32 pools, whose sources
 // the caches hold, 76 us; 4 pages in 32 pools 7 us.
 __global__ __launch_bounds__(256) void copy_pages_kernel(const int32_t *list, int n_pools, int units) {
   const int pool = blockIdx.y;

@@ -30,8 +30,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // (16 bytes of either half of a head) and the sines and cosines of their positions, for all of the heads that it takes.  Values go to
 // slots of a transposed tile: more than four rows of a page are turned round in LDS, so that a thread stores eight slots of a
 // dimension (16 bytes, where all eight are this step's); a few rows are stored from where they were read, 2 bytes a slot.
-// Products and sums in 32 bits, one rounding.  Bound by moving the rows: 8 segments of a 64 + 8 head layer, 587 MB, 126 us, 4.7 TB/s (a
-// large copy 4.9); 77 single rows 4.1 us, a launch and two round trips.
+// Products and sums in 32 bits, one rounding.  Bound by moving the rows: 8 segments of a 64 + 8 head layer, 587 MB, 119 to 128 us, 4.6 to
+// 4.9 TB/s (a large copy 4.9); axes in turn, a load for every angle, 12 % more; 77 single rows 4.1 us, a launch and two round trips.
 constexpr int ROPE_THREADS = 256;
 
 template <int DH, bool WHOLE>

@@ -20,7 +20,8 @@ from . import workloads as W
 
 
 class Streams:
-    """Sequences over `n_pages` pages of every layer.  weights: (Wqkv, Wo) of each layer, from Layer.w4_pack."""
+    """Sequences over `n_pages` pages of every layer, each of up to the layer's max_positions tokens (positions count from a sequence's
+    first token).  weights: (Wqkv, Wo) of each layer, from Layer.w4_pack."""
 
     def __init__(self, api, layer, weights, n_pages: int, window: int, sinks: int):
         import torch
