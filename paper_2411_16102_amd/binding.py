@@ -18,7 +18,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 _SO = os.path.join(_HERE, "libblendstep.so")
-_HEADERS = [os.path.join(_ROOT, "include", h) for h in ("blendstep.h", "blendstep_builder.h", "blendstep_stream.h")]
+_HEADERS = [os.path.join(_ROOT, "include", h) for h in ("blendstep.h", "blendstep_builder.h", "blendstep_stream.h", "blendstep_bits.h")]
 
 _i32p = C.POINTER(C.c_int32)
 
@@ -203,6 +203,13 @@ def raw():
         lib.bs_pages_stats.argtypes = [_p, _p, _p]
         lib.bs_kv_copy_pages.argtypes = [_p, _p, _i32, _i64, _p, _p, _i32, _p]
         lib.bs_kv_compact.argtypes = [_p, _p, _i32, _i64, _p, _i64, _p, _p, _p]
+        lib.bs_window_cache.argtypes = [_p, _i32, _i32]
+        lib.bs_kv4_page_bytes.argtypes = [_p, _i32]
+        lib.bs_kv4_page_bytes.restype = _i64
+        lib.bs_kv4_pack.argtypes = [_p, _p, _p, _p, _i64, _i32, _p]
+        lib.bs_kv4_unpack.argtypes = [_p, _p, _p, _p, _i64, _i32, _p]
+        lib.bs_kv4_copy_pages.argtypes = [_p, _p, _i32, _i64, _i32, _p, _p, _i32, _p]
+        lib.bs_kv4_compact.argtypes = [_p, _p, _i32, _i64, _i32, _p, _i64, _p, _p, _p]
         lib.bs_batch_free.argtypes = [C.POINTER(BatchOwned)]
         lib.bs_batch_free.restype = None
         _lib = lib
@@ -337,8 +344,14 @@ class Layer:
         pool = self.pack_pool(t.k_pool, t.v_pool)
         return DeviceState(w, keep, x, pool, int(t.k_pool.shape[0]))
 
-    def page_bytes(self) -> int:
-        return int(self.lib.bs_kv_page_bytes(self.h))
+    def page_bytes(self, cache: Optional["Kv4"] = None) -> int:
+        """Bytes of a page of a pool in bf16, or of one in four bits."""
+        if cache is None:
+            return int(self.lib.bs_kv_page_bytes(self.h))
+        size = int(self.lib.bs_kv4_page_bytes(self.h, _count(cache.group)))
+        if not size:
+            raise ValueError("a cache in four bits has groups of 32, 64 or 128 channels, at most head_dim: got %d of %d" % (cache.group, self.shape.head_dim))
+        return size
 
     # -- calls ----------------------------------------------------------------------
     def blend_step(self, dev: DeviceState, batch, flags: int = 0, stream=None, y=None, desc=None):
@@ -477,11 +490,14 @@ class Layer:
         with self.torch.cuda.stream(stream):
             return like.new_empty(shape)
 
-    def window_plan(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages: Optional[int] = None, stream=None):
+    def window_plan(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages: Optional[int] = None, stream=None,
+                    cache: Optional["Kv4"] = None):
         """The plan of a step for window_attention and rope_append (bs_window_plan): one for all layers with this window, which may
         be other Layer objects with the same heads, pages and rope_theta on the same device.
-        positions [n_axes, n_rows] and axis_of_pair [head_dim / 2]: rotary positions with several axes."""
-        return WindowPlan(self, batch, window, sinks, positions, axis_of_pair, n_pages, stream)
+        positions [n_axes, n_rows] and axis_of_pair [head_dim / 2]: rotary positions with several axes.
+        cache: Kv4(group) for a step over pools in four bits (uint8, page_bytes(cache) a page), which rope_append then writes and
+        window_attention reads."""
+        return WindowPlan(self, batch, window, sinks, positions, axis_of_pair, n_pages, stream, cache)
 
     def window_attention(self, plan: "WindowPlan", q, kv_pool, out=None, stream=None):
         """Sliding-window attention with sinks of the plan's rows; q and out: [n_rows, Hq * dh] bf16, rows at any stride."""
@@ -544,7 +560,10 @@ class Layer:
     def _check_pool(self, plan, kv_pool):
         if kv_pool.get_device() != self.device:
             self._here("the pool", kv_pool)
-        if kv_pool.dtype is not self._bf16_type or not kv_pool.is_contiguous() or kv_pool.numel() < plan.n_pages * self._page_elems:
+        if plan.cache is not None:
+            if kv_pool.dtype is not self.torch.uint8 or not kv_pool.is_contiguous() or kv_pool.numel() < plan.n_pages * plan.page_bytes:
+                raise ValueError("the pool is smaller than the %d pages of the plan in four bits, or not contiguous uint8" % plan.n_pages)
+        elif kv_pool.dtype is not self._bf16_type or not kv_pool.is_contiguous() or kv_pool.numel() < plan.n_pages * self._page_elems:
             raise ValueError("the pool is smaller than the %d pages of the plan, or not contiguous bf16" % plan.n_pages)
 
     def w4_pack(self, packed, scales, zeros=None, stream=None):
@@ -597,39 +616,80 @@ class Layer:
             self._check(rc)
         return out
 
-    def _pools(self, pools):
+    def _pools(self, pools, cache=None):
         """(array of addresses, pages of each) of a tensor [n_pools, elements] or a list of flat pools."""
-        size = self._page_elems
+        kind, bytes_of, size = (self._bf16_type, 2, self._page_elems) if cache is None else (self.torch.uint8, 1, self.page_bytes(cache))
         if hasattr(pools, "shape"):
             self._here("pools", pools)
-            if pools.dtype is not self._bf16_type or pools.dim() != 2 or not pools.is_contiguous() or pools.shape[1] % size:
-                raise ValueError("pools are contiguous bf16 [n_pools, elements], whole pages each")
+            if pools.dtype is not kind or pools.dim() != 2 or not pools.is_contiguous() or pools.shape[1] % size:
+                raise ValueError("pools are contiguous %s [n_pools, elements], whole pages each" % ("bf16" if cache is None else "uint8"))
             n, elems = pools.shape
             first = pools.data_ptr()
-            return np.arange(first, first + 2 * elems * n, 2 * elems, dtype=np.uint64)[:n] if elems else np.zeros(n, dtype=np.uint64), elems // size
+            return np.arange(first, first + bytes_of * elems * n, bytes_of * elems, dtype=np.uint64)[:n] if elems else np.zeros(n, dtype=np.uint64), elems // size
         pools = list(pools)
         self._here("pools", *pools)
         for p in pools:
-            if p.dtype is not self._bf16_type or not p.is_contiguous() or p.numel() != pools[0].numel() or p.numel() % size:
-                raise ValueError("pools are contiguous bf16 tensors of one size, whole pages each")
+            if p.dtype is not kind or not p.is_contiguous() or p.numel() != pools[0].numel() or p.numel() % size:
+                raise ValueError("pools are contiguous %s tensors of one size, whole pages each" % ("bf16" if cache is None else "uint8"))
         return np.array([p.data_ptr() for p in pools], dtype=np.uint64), pools[0].numel() // size if pools else 0
 
-    def copy_pages(self, pools, src, dst, stream=None):
-        """Page src[i] to page dst[i] in every pool (one per layer: a list, or a tensor [n_layers, elements])."""
-        at, n_pages = self._pools(pools)
+    def copy_pages(self, pools, src, dst, stream=None, cache: Optional["Kv4"] = None):
+        """Page src[i] to page dst[i] in every pool (one per layer: a list, or a tensor [n_layers, elements]); cache: of pools in four bits."""
+        at, n_pages = self._pools(pools, cache)
         src, dst = _i32(src), _i32(dst)
         if src.shape != dst.shape:
             raise ValueError("copy_pages: %d sources, %d destinations" % (src.size, dst.size))
-        self._check(self.lib.bs_kv_copy_pages(self.h, _address(at), at.size, n_pages, _address(src), _address(dst), src.size, self._raw_stream(stream)))
+        pairs = (_address(src), _address(dst), src.size, self._raw_stream(stream))
+        if cache is None:
+            self._check(self.lib.bs_kv_copy_pages(self.h, _address(at), at.size, n_pages, *pairs))
+        else:
+            self._check(self.lib.bs_kv4_copy_pages(self.h, _address(at), at.size, n_pages, cache.group, *pairs))
 
-    def compact_pages(self, pools, tables, stream=None):
+    def compact_pages(self, pools, tables, stream=None, cache: Optional["Kv4"] = None):
         """Moves the pages that `tables` names to the front of every pool: (the tables with the new numbers, pages named)."""
-        at, n_pages = self._pools(pools)
+        at, n_pages = self._pools(pools, cache)
         tables = _i32(tables)
         out, live = np.empty_like(tables), np.zeros(1, dtype=np.int32)
-        self._check(self.lib.bs_kv_compact(self.h, _address(at), at.size, n_pages, _address(tables), tables.size, _address(out), _address(live),
-                                           self._raw_stream(stream)))
+        rest = (_address(tables), tables.size, _address(out), _address(live), self._raw_stream(stream))
+        if cache is None:
+            self._check(self.lib.bs_kv_compact(self.h, _address(at), at.size, n_pages, *rest))
+        else:
+            self._check(self.lib.bs_kv4_compact(self.h, _address(at), at.size, n_pages, cache.group, *rest))
         return out, int(live[0])
+
+    # -- fewer bits (blendstep_bits.h) ----------------------------------------------------
+    def kv4_pack(self, k, v, cache: "Kv4", stream=None):
+        """Token-major keys and values [n_pages, 16, Hkv, dh] bf16 as a pool in four bits (uint8 [n_pages * page_bytes(cache)])."""
+        s = self.shape
+        self._here("kv4_pack", k, v)
+        size = self.page_bytes(cache)
+        for t in (k, v):
+            if t.dtype is not self._bf16_type or not t.is_contiguous() or t.dim() != 4 or tuple(t.shape) != (k.shape[0], s.page_size, s.n_kv_heads, s.head_dim):
+                raise ValueError("kv4_pack: contiguous bf16 [n_pages, %d, %d, %d], got %s %s" % (s.page_size, s.n_kv_heads, s.head_dim, t.dtype, tuple(t.shape)))
+        n = k.shape[0]
+        if stream is None:
+            pool = self.torch.empty(n * size, dtype=self.torch.uint8, device=k.device)
+        else:
+            with self.torch.cuda.stream(stream):
+                pool = self.torch.empty(n * size, dtype=self.torch.uint8, device=k.device)
+        self._check(self.lib.bs_kv4_pack(self.h, k.data_ptr(), v.data_ptr(), pool.data_ptr(), n, cache.group, self._raw_stream(stream)))
+        return pool
+
+    def kv4_unpack(self, pool, cache: "Kv4", stream=None):
+        """What a pool in four bits stands for: keys and values [n_pages, 16, Hkv, dh] bf16."""
+        s = self.shape
+        self._here("kv4_unpack", pool)
+        size = self.page_bytes(cache)
+        if pool.dtype is not self.torch.uint8 or not pool.is_contiguous() or pool.numel() % size:
+            raise ValueError("kv4_unpack: contiguous uint8 of whole pages of %d bytes, got %s %s" % (size, pool.dtype, tuple(pool.shape)))
+        shape = (pool.numel() // size, s.page_size, s.n_kv_heads, s.head_dim)
+        if stream is None:
+            k, v = (self.torch.empty(shape, dtype=self._bf16_type, device=pool.device) for _ in range(2))
+        else:
+            with self.torch.cuda.stream(stream):
+                k, v = (self.torch.empty(shape, dtype=self._bf16_type, device=pool.device) for _ in range(2))
+        self._check(self.lib.bs_kv4_unpack(self.h, pool.data_ptr(), k.data_ptr(), v.data_ptr(), shape[0], cache.group, self._raw_stream(stream)))
+        return k, v
 
 
 def _address(a: np.ndarray) -> int:
@@ -692,6 +752,12 @@ def _current_stream(device: int) -> int:
     return get(device) if get is not None else torch.cuda.current_stream(device).cuda_stream
 
 
+@dataclass(frozen=True)
+class Kv4:
+    """A cache in four bits: codes with two bf16 numbers for each `group` channels of a token and KV head (blendstep_bits.h)."""
+    group: int = 64
+
+
 @dataclass
 class W4Weight:
     """A laid-out 4-bit weight [n, k] (Layer.w4_pack)."""
@@ -731,10 +797,13 @@ class _PlanHandle:
 class WindowPlan:
     """The plan of one step (bs_window): made once, used by every layer with its window and sinks."""
 
-    def __init__(self, layer: Layer, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages=None, stream=None):
-        self.layer = layer
+    def __init__(self, layer: Layer, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages=None, stream=None, cache=None):
+        self.layer, self.cache = layer, cache
         self.n_rows = self.n_pages = 0
+        self.page_bytes = layer.page_bytes(cache)
         self._handle = _PlanHandle(layer)
+        if cache is not None:
+            layer._check(layer.lib.bs_window_cache(self.h, 4, cache.group))
         self.update(batch, window, sinks, positions, axis_of_pair, n_pages, stream)
 
     def update(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages=None, stream=None):
@@ -1021,6 +1090,7 @@ class _Api:
     Scheduler = Scheduler
     Pages = Pages
     WindowPlan = WindowPlan
+    Kv4 = Kv4
     W4Weight = W4Weight
     binding_device_state = DeviceState
     BlendStepError = BlendStepError

@@ -9,6 +9,7 @@
 
 #include "attn_device.hpp"
 #include "common.hpp"
+#include "rope_device.hpp"
 #include "window.hpp"
 #include "window_device.hpp"
 
@@ -16,6 +17,7 @@ namespace bs {
 namespace {
 using namespace attn_dev;
 using namespace window_dev;
+using namespace rope_dev;
 
 template <int DH, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_unit_kernel(const WindowArgs a) {
@@ -32,68 +34,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // dimension (16 bytes, where all eight are this step's); a few rows are stored from where they were read, 2 bytes a slot.
 // Products and sums in 32 bits, one rounding.  Bound by moving the rows: 8 segments of a 64 + 8 head layer, 587 MB, 119 to 128 us, 4.6 to
 // 4.9 TB/s (a large copy 4.9); axes in turn, a load for every angle, 12 % more; 77 single rows 4.1 us, a launch and two round trips.
-constexpr int ROPE_THREADS = 256;
-
-template <int DH, bool WHOLE>
-__device__ __forceinline__ void turn_heads(const RopeArgs &a, const RopeItem &it, int h0, int h1) {
-  constexpr int L = DH / 16, HALF = DH / 2;  // threads of a head
-  const int t = threadIdx.x, e = t % L * 8;
-  const int shift = it.n_rows > 8 ? 4 : it.n_rows > 4 ? 3 : it.n_rows > 2 ? 2 : it.n_rows > 1 ? 1 : 0;  // rows side by side: 2^shift
-  const int r = (t / L) & ((1 << shift) - 1), step = (ROPE_THREADS / L) >> shift;
-  if (r >= it.n_rows) return;
-  const int row = it.row0 + r;
-  float c[8], s[8];
-  if constexpr (WHOLE) {
-    const size_t at = (size_t)a.positions[(size_t)a.axis_of_pair[e] * a.n_rows + row] * HALF + e;
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-      const f32x4_t cv = *reinterpret_cast<const f32x4_t *>(a.cos + at + i), sv = *reinterpret_cast<const f32x4_t *>(a.sin + at + i);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        c[i + k] = cv[k];
-        s[i + k] = sv[k];
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const size_t at = (size_t)a.positions[(size_t)a.axis_of_pair[e + i] * a.n_rows + row] * HALF + e + i;
-      c[i] = a.cos[at];
-      s[i] = a.sin[at];
-    }
-  }
-  const uint16_t *src = a.qkv + row * a.qkv_stride + e;
-  uint16_t *to_q = a.q + row * a.q_stride + e;
-  uint16_t *to_k = a.kv_pool + ((size_t)it.page * 2 * a.n_kv_heads * 16 + it.slot0 + r) * DH + e;
-  auto turn = [&](int head, u32x4_t lo, u32x4_t hi) __attribute__((always_inline)) {
-    u32x4_t lo2, hi2;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float l0 = __uint_as_float(lo[i] << 16), l1 = __uint_as_float(lo[i] & 0xFFFF0000u);
-      const float g0 = __uint_as_float(hi[i] << 16), g1 = __uint_as_float(hi[i] & 0xFFFF0000u);
-      lo2[i] = pack_bf16x2(l0 * c[2 * i] - g0 * s[2 * i], l1 * c[2 * i + 1] - g1 * s[2 * i + 1]);
-      hi2[i] = pack_bf16x2(g0 * c[2 * i] + l0 * s[2 * i], g1 * c[2 * i + 1] + l1 * s[2 * i + 1]);
-    }
-    if (head >= a.n_q_heads && it.page < 0) return;
-    uint16_t *dst = head < a.n_q_heads ? to_q + head * DH : to_k + (size_t)(head - a.n_q_heads) * 16 * DH;
-    *reinterpret_cast<u32x4_t *>(dst) = lo2;
-    *reinterpret_cast<u32x4_t *>(dst + HALF) = hi2;
-  };
-  constexpr int U = 4;  // heads on the way
-  int h = h0 + ((t / L) >> shift);
-  for (; h + (U - 1) * step < h1; h += U * step) {
-    u32x4_t lo[U], hi[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      lo[u] = ld16(src + (h + u * step) * DH);
-      hi[u] = ld16(src + (h + u * step) * DH + HALF);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) turn(h + u * step, lo[u], hi[u]);
-  }
-  for (; h < h1; h += step) turn(h, ld16(src + h * DH), ld16(src + h * DH + HALF));
-}
-
 template <int DH>
 __device__ __forceinline__ void append_values(const RopeArgs &a, const RopeItem &it, int h0, int h1, uint16_t (*turned)[16][DH + 8]) {
   constexpr int L = DH / 8, PASS = ROPE_THREADS / (2 * DH);  // threads of a row of a head; heads that a pass takes

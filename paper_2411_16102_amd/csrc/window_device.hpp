@@ -137,7 +137,18 @@ __device__ __forceinline__ void store_quad(const WindowArgs &a, const WindowItem
 // LDS of a workgroup of NW wavefronts
 constexpr int WINDOW_UNIT_LDS(int dh, int nw) { return (nw > 1 ? nw * (dh / 16) * 1024 : 0) + nw * 128 + 16; }
 
-template <int DH, int NW>
+// The pages of a cache in bf16, as a unit walks them.
+template <int DH>
+struct Bf16Pages {
+  __device__ __forceinline__ explicit Bf16Pages(const bf16x8_t (&)[DH / 32]) {}
+  __device__ __forceinline__ void walk(const WindowArgs &a, const WindowItem &it, int kvh, int lane, int pg0, int pg1, const bf16x8_t (&qf)[DH / 32],
+                                       Columns<DH> &c) {
+    walk_pages<DH>(a, it, kvh, lane, pg0, pg1, qf, c);
+  }
+  __device__ __forceinline__ void finish(Columns<DH> &) {}
+};
+
+template <int DH, int NW, class Pages = Bf16Pages<DH>>
 __device__ __forceinline__ void window_unit(const WindowArgs &a, int block, unsigned char *lds) {
   constexpr int DB = DH / 16;
   const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -160,7 +171,9 @@ __device__ __forceinline__ void window_unit(const WindowArgs &a, int block, unsi
   for (int db = 0; db < DB; ++db) c.o[db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   c.m = NEG_BIG;
   c.l = 0.f;
-  for (int pg = pg0; pg < pg1; pg += 64) walk_pages<DH>(a, it, kvh, lane, pg, min(pg + 64, pg1), qf, c);
+  Pages pages(qf);
+  for (int pg = pg0; pg < pg1; pg += 64) pages.walk(a, it, kvh, lane, pg, min(pg + 64, pg1), qf, c);
+  pages.finish(c);
   c.l += __shfl_xor(c.l, 16, 64);
   c.l += __shfl_xor(c.l, 32, 64);
   if constexpr (NW == 1) {

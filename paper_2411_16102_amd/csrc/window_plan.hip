@@ -7,8 +7,9 @@
 #include <limits>
 #include <vector>
 
-#include "../../include/blendstep_stream.h"
+#include "../../include/blendstep_bits.h"
 #include "context.hpp"
+#include "kv4.hpp"
 #include "misc.hpp"
 #include "window.hpp"
 
@@ -32,12 +33,15 @@ struct Planned {
   long off_items = 0, off_pages = 0, off_rope = 0, off_positions = 0, off_axis = 0, words = 0;
   long off_work = 0, off_cut = 0, off_row_start = 0, off_kv_len = 0, off_page_start = 0, off_page_ids = 0;
   long at_cut_acc = 0, at_cut_m = 0, at_cut_l = 0, state_floats = 0;  // partial states, in floats
+  long off_expand = 0;
+  int n_expand = 0;                             // pages in four bits that wide work reads as bf16
 };
 
 }  // namespace
 
 struct bs_window {
   bs_ctx *ctx = nullptr;
+  int group = 0;  // channels of a group of the cache in four bits that plans are for; 0: a cache in bf16
   Planned p;
   Staging<HipRuntime> stage;
   int32_t *d_words = nullptr;
@@ -46,8 +50,10 @@ struct bs_window {
   long cap_states = 0;
   unsigned *d_counters = nullptr;
   long cap_counters = 0;
+  uint16_t *d_expanded = nullptr;  // pages in four bits as bf16
+  long cap_expanded = 0;
   // host scratch reused across plans
-  std::vector<int32_t> words, refs, item_pages, cut, wide_start, wide_pages;
+  std::vector<int32_t> words, refs, item_pages, cut, wide_start, wide_pages, expand;
   std::vector<WindowItem> items;
   std::vector<RopeItem> rope;
   struct Rows { int seq, first, n, pages; };  // rows of narrow work that share their units
@@ -304,6 +310,12 @@ Cut cut_choice(const std::vector<bs_window::Work> &work, int wg_per_work, int dh
   return best;
 }
 
+// The microseconds that are expected of the conversion of n pages in four bits: a launch, and bytes in and out.
+double expand_us(size_t n, const bs_layer_cfg &g, int group) {
+  if (n == 0) return 0.0;
+  return 2.0 + (double)n * g.n_kv_heads * (kv4_head_bytes(g.head_dim, group) + 64 * g.head_dim) / 4.0e6;
+}
+
 void cut_blocks(bs_window *w, int most) {
   Planned &p = w->p;
   if (most == 0) return;
@@ -331,6 +343,7 @@ int sort_rows(bs_window *w, const bs_batch *b, const Route &r, int most_narrow) 
   w->work.clear();
   w->wide_start.assign((size_t)b->n_seq + 1, 0);
   w->wide_pages.clear();
+  w->expand.clear();
   p.wide_blocks = 0;
   p.pages = 0;
   for (int s = 0; s < b->n_seq; ++s) {
@@ -338,7 +351,17 @@ int sort_rows(bs_window *w, const bs_batch *b, const Route &r, int most_narrow) 
     w->wide_start[s] = (int32_t)w->wide_pages.size();
     if (rows > most_narrow) {
       if (const int rc = add_blocks(w, b, s, r)) return rc;
-      w->wide_pages.insert(w->wide_pages.end(), b->page_ids + b->page_start[s], b->page_ids + b->page_start[s + 1]);
+      const int32_t *table = b->page_ids + b->page_start[s];
+      if (w->group == 0) {
+        w->wide_pages.insert(w->wide_pages.end(), table, b->page_ids + b->page_start[s + 1]);
+      } else {  // the pages that its rows see, by their places among those that are converted
+        const Seen seen = seen_by(std::max(0, b->kv_len[s] - rows), b->kv_len[s] - 1, p.window, p.sinks);
+        w->wide_pages.resize(w->wide_pages.size() + (b->page_start[s + 1] - b->page_start[s]), BS_PAGE_NONE);
+        for (int i = 0; i < seen.pages(); ++i) {
+          w->wide_pages[w->wide_start[s] + seen.page(i)] = (int32_t)w->expand.size();
+          w->expand.push_back(table[seen.page(i)]);
+        }
+      }
     } else if (const int rc = add_rows(w, b, s, 0, rows, r.per_unit)) {
       return rc;
     }
@@ -376,8 +399,9 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cf
     if (const int rc = sort_rows(w, b, r, rows)) return rc;
     const Division d = divide(w->rows, g.n_kv_heads, g.head_dim, n_cu);
     const Cut c = w->work.empty() ? Cut{0, 0.0} : cut_choice(w->work, g.n_q_heads / r.heads, g.head_dim, r.rows, n_cu);
-    if (best < 0.0 || d.us + c.us < best) {
-      best = d.us + c.us;
+    const double us = d.us + c.us + expand_us(w->expand.size(), g, w->group);
+    if (best < 0.0 || us < best) {
+      best = us;
       div = d;
       cut = c;
       chosen = rows;
@@ -394,6 +418,7 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cf
   // longest first: the short ones then fill the end of the launch
   std::stable_sort(w->work.begin(), w->work.end(), [](const auto &x, const auto &y) { return x.blocks > y.blocks; });
   p.n_work = (int)w->work.size();
+  p.n_expand = (int)w->expand.size();
   p.n_cut = (int)w->cut.size() / 4;
   return BS_OK;
 }
@@ -484,9 +509,21 @@ void bs_window_destroy(bs_window *w) {
     if (w->d_words) (void)hipFree(w->d_words);
     if (w->d_states) (void)hipFree(w->d_states);
     if (w->d_counters) (void)hipFree(w->d_counters);
+    if (w->d_expanded) (void)hipFree(w->d_expanded);
     w->stage.close();
   }
   delete w;
+}
+
+int bs_window_cache(bs_window *w, int32_t bits, int32_t group) {
+  if (!w) return BS_EINVAL;
+  return ctx_guarded(w->ctx, [&]() -> int {
+    if (bits == 4 ? bs_kv4_page_bytes(w->ctx, group) == 0 : bits != 16 || group != 0)
+      return ctx_fail(w->ctx, BS_EINVAL, "bs_window_cache: %d bits, groups of %d channels (16 and 0, or 4 and 32, 64 or 128, at most head_dim)", bits, group);
+    w->p = Planned();
+    w->group = group;
+    return BS_OK;
+  });
 }
 
 int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t window, int32_t sinks, int32_t n_axes,
@@ -521,7 +558,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     plan_appends(w, b);
     // (grids count units of a KV head, workgroups of some heads, and shares of the heads of a run)
     if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff ||
-        (int64_t)p.n_rope * (g.n_kv_heads + 1) + 4096 > 0x7fffffff)
+        (int64_t)p.n_rope * (g.n_kv_heads + 1) + 4096 > 0x7fffffff || (int64_t)p.n_expand * g.n_kv_heads > 0x7fffffff)
       return fail_with(too_large(w));
 
     for (int i = 0; n_axes > 0 && i < half; ++i) p.whole_axes = p.whole_axes && axis_of_pair[i] == axis_of_pair[i & ~7];
@@ -535,7 +572,8 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     p.off_kv_len = p.off_row_start + n_tab;
     p.off_page_start = p.off_kv_len + n_tab;
     p.off_page_ids = p.off_page_start + n_tab;
-    p.off_rope = whole_units(p.off_page_ids + n_wide_pages);
+    p.off_expand = p.off_page_ids + n_wide_pages;
+    p.off_rope = whole_units(p.off_expand + p.n_expand);
     p.off_axis = p.off_rope + 4L * p.n_rope;
     p.off_positions = p.off_axis + half;
     p.words = whole_units(p.off_positions + (long)axes * rows);
@@ -558,6 +596,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
       std::memcpy(&words[p.off_page_start], w->wide_start.data(), sizeof(int32_t) * n_tab);
       if (n_wide_pages) std::memcpy(&words[p.off_page_ids], w->wide_pages.data(), sizeof(int32_t) * n_wide_pages);
     }
+    if (p.n_expand) std::memcpy(&words[p.off_expand], w->expand.data(), sizeof(int32_t) * p.n_expand);
     if (p.n_rope) std::memcpy(&words[p.off_rope], w->rope.data(), sizeof(RopeItem) * p.n_rope);
     p.has_angles = true;
     for (int s = 0; n_axes == 0 && s < b->n_seq; ++s) {
@@ -583,6 +622,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     p.state_floats = p.at_cut_l + n_cut;
     if (p.at_cut_acc > (1L << 29)) return fail_with(too_large(w));  // (offsets of the joins: 32 bits of bytes)
     if (const int rc = grow(c, &w->d_states, &w->cap_states, p.state_floats, sizeof(float))) return fail_with(rc);
+    if (const int rc = grow(c, &w->d_expanded, &w->cap_expanded, (long)p.n_expand * 2 * PAGE * g.n_kv_heads * g.head_dim, sizeof(uint16_t))) return fail_with(rc);
     if (p.states * g.n_kv_heads > w->cap_counters) {
       if (const int rc = grow(c, &w->d_counters, &w->cap_counters, p.states * g.n_kv_heads, sizeof(unsigned))) return fail_with(rc);
       if (hipError_t e = hipMemsetAsync(w->d_counters, 0, sizeof(unsigned) * (size_t)w->cap_counters, st)) {
@@ -631,7 +671,7 @@ int bs_rope_append(bs_window *w, const void *qkv, int64_t qkv_stride, void *q, i
     a.items = reinterpret_cast<const RopeItem *>(w->d_words + p.off_rope);
     a.qkv = (const uint16_t *)qkv; a.q = (uint16_t *)q; a.kv_pool = (uint16_t *)kv_pool;
     a.qkv_stride = qkv_stride; a.q_stride = q_stride;
-    CTX_HIP_TRY(c, launch_rope_append(a, (hipStream_t)stream));
+    CTX_HIP_TRY(c, w->group ? launch_rope_append4(a, w->group, (hipStream_t)stream) : launch_rope_append(a, (hipStream_t)stream));
     return BS_OK;
   });
 }
@@ -675,7 +715,17 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
       f.page_start = w->d_words + p.off_page_start; f.page_ids = w->d_words + p.off_page_ids;
       f.q = a.q; f.kv_pool = a.kv_pool; f.out = a.out;
       f.window = p.window; f.sinks = p.sinks; f.q_stride = q_stride; f.out_stride = out_stride;
-      if (p.n_items > 0) CTX_HIP_TRY(c, launch_window_step(a, f, route.heads, st));
+      if (w->group) {
+        Kv4Expand x{};
+        x.n_kv_heads = g.n_kv_heads; x.head_dim = g.head_dim; x.group = w->group;
+        x.n = p.n_expand;
+        x.list = w->d_words + p.off_expand;
+        x.pool = (const unsigned char *)kv_pool;
+        x.out = w->d_expanded;
+        CTX_HIP_TRY(c, launch_kv4_expand(x, st));
+        f.kv_pool = w->d_expanded;
+        CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
+      } else if (p.n_items > 0) CTX_HIP_TRY(c, launch_window_step(a, f, route.heads, st));
       else CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
       if (p.n_cut) {
         WindowMergeArgs m{};
@@ -686,9 +736,9 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
         m.cut_acc = f.part_acc; m.cut_m = f.part_m; m.cut_l = f.part_l;
         CTX_HIP_TRY(c, launch_window_merge(m, st));
       }
-      if (p.n_items > 0) return BS_OK;
+      if (p.n_items > 0 && !w->group) return BS_OK;
     }
-    CTX_HIP_TRY(c, launch_window_units(a, st));
+    CTX_HIP_TRY(c, w->group ? launch_window_units4(a, w->group, st) : launch_window_units(a, st));
     return BS_OK;
   });
 }
