@@ -54,6 +54,22 @@ int bs_kv4_copy_pages(bs_ctx *ctx, void *const *pools, int32_t n_pools, int64_t 
 int bs_kv4_compact(bs_ctx *ctx, void *const *pools, int32_t n_pools, int64_t n_pages, int32_t group, const int32_t *tables, int64_t n,
                    int32_t *tables_out, int32_t *n_live, void *stream);
 
+/* ---- products of 8-bit integers ----------------------------------------------------------------------------------
+ * y[m, n] = scales[m] weight_scales[n] * sum over k of q[m, k] w[n, k].  Sums are exact; k is a multiple of 16 up to 131072; m and n any. */
+
+/* Rows as 8-bit integers, of activations (a scale for each token) or of a weight (a scale for each output): scale = the greatest magnitude
+ * of the row / 127 (at least 2^-100 / 127), q = x / scale to the nearest integer, ties to even, in 32 bits.  A row with a NaN or an infinity: its scale is
+ * NaN and its integers 0, so that all of its results are NaN.
+ * x: device bf16, row i at x + i * x_stride elements (x_stride a multiple of 8, 16-byte aligned).  q: device int8 [m, k], 16-byte aligned; scales: device
+ * float [m]. */
+int bs_w8_quantize(bs_ctx *ctx, const void *x, int64_t x_stride, int64_t m, int64_t k, void *q, float *scales, void *stream);
+
+/* q: device int8 [m, k], weight: device int8 [n, k] (any values, -128 included), 16-byte aligned; scales: device float [m], weight_scales: device float [n];
+ * y: device bf16, row i at y + i * y_stride, rounded once.  The calls on one context share a workspace and must not overlap in time on
+ * different streams. */
+int bs_w8_linear(bs_ctx *ctx, const void *q, const float *scales, const void *weight, const float *weight_scales, int64_t m, int64_t n, int64_t k, void *y,
+                 int64_t y_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

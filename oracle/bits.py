@@ -52,13 +52,13 @@ def kv4_values(v, group: int):
 
 
 def w8_rows(x):
-    """(integers, scale) of rows x [m, k]: scale = the greatest magnitude / 127 (in float32), at least 2^-100 / 127; NaN for rows with a NaN or an infinity."""
+    """(integers, scale) of rows x [m, k]: scale = the greatest magnitude / 127, at least 2^-100 / 127, integers x / scale, all in float32; NaN for rows with a NaN or an infinity."""
     x = np.asarray(x, dtype=np.float32)
     most = np.abs(x).max(axis=1) if x.shape[1] else np.zeros(len(x), dtype=np.float32)
     bad = ~np.isfinite(x).all(axis=1)
     scale = np.maximum(np.where(bad, np.float32(0), most), np.float32(2.0 ** -100)) / np.float32(127)
     with np.errstate(invalid="ignore"):
-        q = np.clip(np.rint(np.where(bad[:, None], 0, x).astype(np.float64) / scale[:, None].astype(np.float64)), -127, 127).astype(np.int64)
+        q = np.clip(np.rint(np.where(bad[:, None], np.float32(0), x) / scale[:, None]), -127, 127).astype(np.int64)
     return q, np.where(bad, np.float32(np.nan), scale)
 
 

@@ -210,6 +210,8 @@ def raw():
         lib.bs_kv4_unpack.argtypes = [_p, _p, _p, _p, _i64, _i32, _p]
         lib.bs_kv4_copy_pages.argtypes = [_p, _p, _i32, _i64, _i32, _p, _p, _i32, _p]
         lib.bs_kv4_compact.argtypes = [_p, _p, _i32, _i64, _i32, _p, _i64, _p, _p, _p]
+        lib.bs_w8_quantize.argtypes = [_p, _p, _i64, _i64, _i64, _p, _p, _p]
+        lib.bs_w8_linear.argtypes = [_p, _p, _p, _p, _p, _i64, _i64, _i64, _p, _i64, _p]
         lib.bs_batch_free.argtypes = [C.POINTER(BatchOwned)]
         lib.bs_batch_free.restype = None
         _lib = lib
@@ -692,6 +694,61 @@ class Layer:
         return k, v
 
 
+    def w8_quantize(self, x, stream=None) -> "W8Rows":
+        """Rows [m, k] bf16 as 8-bit integers with a scale each (bs_w8_quantize): the inputs of several products, or a weight [n, k]."""
+        torch = self.torch
+        if x.get_device() != self.device:
+            self._here("w8_quantize", x)
+        if x.dtype is not self._bf16_type or x.dim() != 2:
+            raise ValueError("w8_quantize: bf16 rows, got %s %s" % (x.dtype, tuple(x.shape)))
+        m, k = x.shape
+        stride, inner = x.stride()
+        if m and inner != 1:
+            raise ValueError("w8_quantize: rows of x are not contiguous")
+        if m <= 1:
+            stride = k  # (a single row has no stride)
+        if stream is None:
+            q, scales = x.new_empty((m, k), dtype=torch.int8), x.new_empty((m,), dtype=torch.float32)
+        else:
+            with torch.cuda.stream(stream):
+                q, scales = x.new_empty((m, k), dtype=torch.int8), x.new_empty((m,), dtype=torch.float32)
+        rc = self.lib.bs_w8_quantize(self.h, x.data_ptr(), stride, m, k, q.data_ptr(), scales.data_ptr(), self._raw_stream(stream))
+        if rc:
+            self._check(rc)
+        return W8Rows(q, scales)
+
+    def w8_linear(self, x, weight: "W8Weight", out=None, stream=None):
+        """Rows times a weight in 8-bit integers: [m, n] bf16.  x: bf16 [m, k], brought to integers first, or the W8Rows of w8_quantize."""
+        rows = x if type(x) is W8Rows else self.w8_quantize(x, stream)
+        q, w = rows.q, weight.q
+        if q.get_device() != self.device or w.get_device() != self.device:
+            self._here("w8_linear", q, w)
+        m, k = q.shape
+        n = w.shape[0]
+        if w.shape[1] != k:
+            raise ValueError("w8_linear: rows of %d inputs, the weight has %d" % (k, w.shape[1]))
+        if out is None:
+            if stream is None:
+                out = q.new_empty((m, n), dtype=self._bf16_type)
+            else:
+                with self.torch.cuda.stream(stream):
+                    out = q.new_empty((m, n), dtype=self._bf16_type)
+            out_stride = n
+        else:
+            if out.get_device() != self.device:
+                self._here("w8_linear", out)
+            out_stride, inner = out.stride() if out.dim() == 2 else (0, 0)
+            if out.dtype is not self._bf16_type or out.shape != (m, n) or (inner != 1 and n > 1 and m):
+                raise ValueError("w8_linear: out is not bf16 [%d, %d]" % (m, n))
+            if m == 1:
+                out_stride = n
+        rc = self.lib.bs_w8_linear(self.h, q.data_ptr(), rows.scales.data_ptr(), w.data_ptr(), weight.scales.data_ptr(), m, n, k, out.data_ptr(), out_stride,
+                                   self._raw_stream(stream))
+        if rc:
+            self._check(rc)
+        return out
+
+
 def _address(a: np.ndarray) -> int:
     return a.__array_interface__["data"][0]
 
@@ -772,6 +829,25 @@ class W4Weight:
         size = int(raw().bs_w4_bytes(self.n, self.k, self.group, int(self.with_zeros)))
         if not self.data.is_contiguous() or self.data.numel() * self.data.element_size() < size:
             raise ValueError("the laid-out weight [%d, %d] has %d contiguous bytes" % (self.n, self.k, size))
+
+
+@dataclass
+class W8Rows:
+    """8-bit integers [rows, k] with a float32 scale for each row: activations (Layer.w8_quantize) or a weight's outputs."""
+    q: "object"
+    scales: "object"
+
+    def __post_init__(self):
+        # (the kernels read both whole)
+        q, s = self.q, self.scales
+        if str(q.dtype) != "torch.int8" or q.dim() != 2 or not q.is_contiguous():
+            raise ValueError("contiguous int8 [rows, k], got %s %s" % (q.dtype, tuple(q.shape)))
+        if str(s.dtype) != "torch.float32" or tuple(s.shape) != (q.shape[0],) or not s.is_contiguous() or s.device != q.device:
+            raise ValueError("a contiguous float32 scale for each of %d rows on %s, got %s %s on %s" % (q.shape[0], q.device, s.dtype, tuple(s.shape), s.device))
+
+
+class W8Weight(W8Rows):
+    """A weight [n, k] in 8-bit integers with a scale for each output."""
 
 
 class _PlanHandle:
@@ -1092,6 +1168,8 @@ class _Api:
     WindowPlan = WindowPlan
     Kv4 = Kv4
     W4Weight = W4Weight
+    W8Rows = W8Rows
+    W8Weight = W8Weight
     binding_device_state = DeviceState
     BlendStepError = BlendStepError
     FLAG_SERIAL = FLAG_SERIAL

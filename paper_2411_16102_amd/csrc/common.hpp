@@ -13,6 +13,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 typedef uint16_t bf16_raw;  // storage type of a bfloat16 in memory
 
 __device__ __forceinline__ float bf16_to_f32(bf16_raw v) {

@@ -16,7 +16,10 @@ enum GemmEpilogue {
   EPI_RESID_NORM = 2, // x1 = resid + A B^T in fp32; also bf16(x1 * gain) and partial row sums of x1^2 for the next norm
   EPI_SWIGLU = 3,     // out = silu(s * gate) * (s * up), s = per-row RMSNorm scale
   EPI_RESID = 4,      // y = resid + A B^T (resid in bf16, or in fp32 when resid32 is set)
-  EPI_PARTIAL = 5     // internal: fp32 partial products of one k-range into the split-K workspace
+  EPI_PARTIAL = 5,    // internal: fp32 partial products of one k-range into the split-K workspace
+  // products of 8-bit integers (w8.hip); A, B, K, lda and ldb count two of them as one number
+  EPI_W8 = 6,         // C = row_scale[m] col_scale[n] (A B^T)
+  EPI_W8_PARTIAL = 7  // 32-bit sums of one k-range into the split-K workspace, rows of w8_part_stride(N)
 };
 
 struct GemmArgs {
@@ -61,7 +64,11 @@ struct GemmArgs {
   const int32_t *row_pos, *row_page, *row_slot;  // [M]
   uint16_t *q_out;    // [M, Hq*dh]
   uint16_t *kv_pool;  // pages: [2][Hkv][...]
+  // W8
+  const float *row_scale, *col_scale;  // [M], [N]
 };
+
+constexpr int w8_part_stride(int n) { return (n + 3) & ~3; }
 
 // Decode attention that shares a GEMM launch (see gemm_attn_kernel in gemm.hip).
 struct GemmRide {

@@ -117,11 +117,33 @@ __device__ __forceinline__ void sk_tile_span(const SkPlan &p, int j, int *w_firs
   *parts = n;
 }
 
+// The accumulators of a product and the matrix instruction behind them: bf16 into 32-bit numbers, or 8-bit into 32-bit integers.
+template <bool I8>
+using GemmAcc = std::conditional_t<I8, i32x4_t, f32x4_t>;
+__device__ __forceinline__ void gemm_mfma(f32x4_t &c, bf16x8_t w, bf16x8_t x) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0); }
+__device__ __forceinline__ void gemm_mfma(i32x4_t &c, bf16x8_t w, bf16x8_t x) {
+  c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x), c, 0, 0, 0);
+}
+constexpr bool gemm_in_integers(int epi) { return epi == EPI_W8 || epi == EPI_W8_PARTIAL; }
+
+// four neighbouring results of a row, of which those below n_lim exist
+__device__ __forceinline__ void store_scaled4(uint16_t *p, f32x4_t v, int n, int n_lim, bool aligned) {
+  if (aligned && n + 4 <= n_lim) {
+    store_bf16x4(p, v[0], v[1], v[2], v[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < n_lim) p[e] = f32_to_bf16(v[e]);
+  }
+}
+
 // One workgroup's tile; `bid` is the workgroup's number among the GEMM workgroups of the launch
 // (SK: the tile and the k-range come from `seg` instead).
 template <int BM, int BN, int WAVES_M, int WAVES_N, int EPI, int DH, int DEEP = 0, bool SK = false>
 __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, const SkPlan *sp = nullptr, const SkSeg seg = SkSeg{}) {
-  static_assert(!SK || (!DEEP && EPI != EPI_PARTIAL), "shared tiles use the two rings of whole tiles and a real epilogue");
+  constexpr bool I8 = gemm_in_integers(EPI), PART = EPI == EPI_PARTIAL || EPI == EPI_W8_PARTIAL;
+  typedef GemmAcc<I8> Acc;
+  static_assert(!SK || (!DEEP && !PART && !I8), "shared tiles use the two rings of whole tiles and a real epilogue");
   constexpr int NW = WAVES_M * WAVES_N;
   // DEEP: the pipeline for one round of tiles over few rows, where every CU streams a weight
   // panel of its own from HBM; the first half of the wavefronts requests the activation
@@ -146,8 +168,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
   const int n_lim = a.n_count ? a.n_begin + a.n_count : a.N;  // end of the output columns of this launch
   const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (n_lim - a.n_begin + OUT_BN - 1) / OUT_BN;
   // split-K: consecutive workgroups are the k-ranges of one tile
-  const int split = (EPI == EPI_PARTIAL) ? bid % a.k_splits : 0;
-  const int tile_id = SK ? seg.pid : (EPI == EPI_PARTIAL) ? bid / a.k_splits : bid;
+  const int split = PART ? bid % a.k_splits : 0;
+  const int tile_id = SK ? seg.pid : PART ? bid / a.k_splits : bid;
   const TileCoord tc = map_tile(tile_id, tiles_m * tiles_n, tiles_m, tiles_n);
   const int m0 = tc.tm * BM, n0 = a.n_begin + tc.tn * OUT_BN;
 
@@ -205,7 +227,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
     }
     off_b[i] = (uint32_t)(((size_t)gn * a.ldb + chunk * 8) * 2);
   }
-  constexpr bool TURNED = DEEP && EPI != EPI_PARTIAL && BM <= 128;
+  constexpr bool TURNED = DEEP && !PART && BM <= 128;
   const int nk_whole = (a.K + BK - 1) / BK;
   const int first_kt = TURNED ? first_k_tile(tile_id, a.K, a.ldb) : 0;
   auto turned_kt = [&](int kt) {
@@ -236,11 +258,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
   auto dma_a = [&](int kt, int lds_off, int i, auto checked) { dma(a.A, rsrc_a, kt, off_a[i], ka[i], lds_off + dst_a[i], checked); };
   auto dma_b = [&](int kt, int lds_off, int i, auto checked) { dma(a.B, rsrc_b, kt, off_b[i], kb[i], lds_off + dst_b[i], checked); };
 
-  f32x4_t acc[NI][MI];
+  Acc acc[NI][MI];
 #pragma unroll
   for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = Acc{0, 0, 0, 0};
 
   // fragment addresses: tile row of the lane, chunk 4*ks + lg swizzled by ((row >> 1) & 7)
   const int sw = (lr >> 1) & 7;
@@ -249,8 +271,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
 
   const int nk_all = (a.K + BK - 1) / BK;
   // this workgroup's k-tiles [kt0, kt1): all of them, or one of k_splits nearly equal ranges
-  const int kt0 = SK ? seg.kt0 : (EPI == EPI_PARTIAL) ? (int)((long)nk_all * split / a.k_splits) : 0;
-  const int kt1 = SK ? seg.kt1 : (EPI == EPI_PARTIAL) ? (int)((long)nk_all * (split + 1) / a.k_splits) : nk_all;
+  const int kt0 = SK ? seg.kt0 : PART ? (int)((long)nk_all * split / a.k_splits) : 0;
+  const int kt1 = SK ? seg.kt1 : PART ? (int)((long)nk_all * (split + 1) / a.k_splits) : nk_all;
   constexpr int NF = MI + NI;   // fragment reads per 32-wide k-step
   constexpr int NMF = MI * NI;  // MFMAs per 32-wide k-step
   // read number o of k-step ks (32 wide, two per tile) of the panels in ring slots sa, sb
@@ -269,7 +291,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
 #pragma unroll
     for (int j = 0; j < NMF; ++j) {
       const int ni = j / MI, mi = j % MI;
-      acc[ni][mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[ni], xf[mi], acc[ni][mi], 0, 0, 0);
+      gemm_mfma(acc[ni][mi], wf[ni], xf[mi]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int o = 0; o < n_ops; ++o)
@@ -488,6 +510,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
   constexpr int RS = 64 * 4 + 16;  // bytes of a row of 64 floats: rows four banks apart
   static_assert(NW * CM * 16 * RS <= LDS_BYTES, "the turned blocks fit the panel ring");
   unsigned char *turned = smem + wave * (CM * 16 * RS);
+  float row_scale[MI];
+  if constexpr (EPI == EPI_W8) {
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) row_scale[mi] = a.row_scale[min(m0 + wm0 + mi * 16 + lr, a.M - 1)];
+  }
   // blocks [c, c + CM) of rows into LDS (read and written by this wavefront alone, whose LDS operations complete in order)
   auto turn = [&](int c) {
     __builtin_amdgcn_wave_barrier();
@@ -495,7 +522,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
     for (int j = 0; j < CM; ++j)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
-        if (c + j < MI) *reinterpret_cast<f32x4_t *>(turned + (j * 16 + lr) * RS + (ni * 16 + 4 * lg) * 4) = acc[ni][c + j];
+        if (c + j < MI) {
+          auto *to = turned + (j * 16 + lr) * RS + (ni * 16 + 4 * lg) * 4;
+          if constexpr (EPI == EPI_W8) *reinterpret_cast<f32x4_t *>(to) = __builtin_convertvector(acc[ni][c + j], f32x4_t) * row_scale[c + j];
+          else *reinterpret_cast<Acc *>(to) = acc[ni][c + j];
+        }
     __builtin_amdgcn_wave_barrier();
   };
   constexpr auto rows_in = [](int c) { return (MI - c < CM ? MI - c : CM) * 16; };
@@ -559,6 +590,30 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
             if (ok) store_bf16x4(a.C + (size_t)m * a.ldc + n, v[u][0], v[u][1], v[u][2], v[u][3]);
           }
         }
+      }
+    }
+  }
+
+  if constexpr (I8) {
+    const int n = n0 + wn0 + c16;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0;
+    const int stride = w8_part_stride(a.N);
+    int32_t *ws = reinterpret_cast<int32_t *>(a.sk_ws) + (size_t)split * a.M * stride;
+    f32x4_t scale = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (EPI == EPI_W8) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) scale[e] = a.col_scale[min(n + e, a.N - 1)];
+    }
+#pragma unroll
+    for (int c = 0; c < MI; c += CM) {
+      turn(c);
+#pragma unroll 4
+      for (int g = 0; g < rows_in(c); g += 4) {
+        const int m = m0 + wm0 + c * 16 + g + r16;
+        const auto *from = turned + (g + r16) * RS + c16 * 4;
+        if (m >= a.M || n >= n_lim) continue;
+        if constexpr (EPI == EPI_W8) store_scaled4(a.C + (size_t)m * a.ldc + n, *reinterpret_cast<const f32x4_t *>(from) * scale, n, n_lim, aligned);
+        else *reinterpret_cast<i32x4_t *>(ws + (size_t)m * stride + n) = *reinterpret_cast<const i32x4_t *>(from);
       }
     }
   }
@@ -759,16 +814,17 @@ __device__ __forceinline__ void wait_for_all_but(int left, std::integer_sequence
   ((left == J ? __builtin_amdgcn_s_waitcnt(waitcnt_imm(J * L, false)) : (void)0), ...);
 }
 
-template <int MI, int NI>
+template <int MI, int NI, bool I8 = false>
 __global__ __launch_bounds__(512) void gemm_rows_kernel(const GemmArgs a, const int epi, const int dh, const int tiles_m, const int n_items) {
   typedef RowsKernel<MI, NI> R;
+  typedef GemmAcc<I8> Acc;
   constexpr int S = R::S, L = R::L;
   static_assert(S >= 2 && (S - 1) * L < 64, "look-ahead, and the vmcnt field");
   extern __shared__ __align__(16) unsigned char smem[];
-  f32x4_t *red = reinterpret_cast<f32x4_t *>(smem + 8 * S * R::STAGE);  // [8][MI][64]
+  Acc *red = reinterpret_cast<Acc *>(smem + 8 * S * R::STAGE);  // [8][MI][64]
   float *meta_rs = reinterpret_cast<float *>(smem + 8 * S * R::STAGE + R::RED);  // [ROWS_MAX_M] per row: norm factor, position, page, slot
   int *meta_pos = reinterpret_cast<int *>(meta_rs + ROWS_MAX_M), *meta_page = meta_pos + ROWS_MAX_M, *meta_slot = meta_page + ROWS_MAX_M;
-  const bool paired = epi == EPI_QKV || epi == EPI_SWIGLU;
+  const bool paired = !I8 && (epi == EPI_QKV || epi == EPI_SWIGLU);
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int lr = lane & 15, lg = lane >> 4;
   unsigned char *ring = smem + wave * S * R::STAGE;
@@ -863,11 +919,11 @@ __global__ __launch_bounds__(512) void gemm_rows_kernel(const GemmArgs a, const 
   int slot = 0, left = total, turn = 0;
   for (int item = (int)blockIdx.x; item < n_items; item += (int)gridDim.x, ++turn) {
     const int blk = item / tiles_m, m0 = item % tiles_m * 16 * MI;
-    f32x4_t acc[NI][MI];
+    Acc acc[NI][MI];
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = Acc{0, 0, 0, 0};
     for (int k = 0; k < n; ++k) {
       --left;  // k-tiles behind this one
       if (left >= S - 1) {
@@ -891,7 +947,7 @@ __global__ __launch_bounds__(512) void gemm_rows_kernel(const GemmArgs a, const 
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-          for (int mi = 0; mi < MI; ++mi) acc[ni][mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[ks][ni], x[ks][mi], acc[ni][mi], 0, 0, 0);
+          for (int mi = 0; mi < MI; ++mi) gemm_mfma(acc[ni][mi], w[ks][ni], x[ks][mi]);
       if (left >= S) issue();
       slot = slot + 1 == S ? 0 : slot + 1;
     }
@@ -908,14 +964,21 @@ __global__ __launch_bounds__(512) void gemm_rows_kernel(const GemmArgs a, const 
       for (int mi = 0; mi < MI; ++mi) {
         if (wave != ((turn * NI + ni) * MI + mi) % 8) continue;
         auto total_of = [&](int l) {
-          f32x4_t s = red[mi * 64 + l];
+          Acc s = red[mi * 64 + l];
 #pragma unroll
           for (int v = 1; v < 8; ++v) s += red[(v * MI + mi) * 64 + l];
           return s;
         };
         const int ml = m0 + 16 * mi + lr;  // (at most ROWS_MAX_M - 1)
         const bool ok = ml < a.M;
-        if (paired) {
+        if constexpr (I8) {
+          const int n0 = (blk * NI + ni) * 16 + 4 * lg;
+          if (!ok || n0 >= a.N) continue;
+          f32x4_t v = __builtin_convertvector(total_of(lane), f32x4_t) * a.row_scale[ml];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] *= a.col_scale[min(n0 + e, a.N - 1)];
+          store_scaled4(a.C + (size_t)ml * a.ldc + n0, v, n0, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
+        } else if (paired) {
           const int u = first_row(blk * NI + ni) + 4 * (lg & 1);  // first of this lane's four rows of the lower unit
           const f32x4_t lo = total_of(lane & 31) * meta_rs[ml], hi = total_of((lane & 31) + 32) * meta_rs[ml];
           if (!ok || lg > 1 || u >= a.N) continue;
