@@ -70,6 +70,15 @@ int bs_w8_quantize(bs_ctx *ctx, const void *x, int64_t x_stride, int64_t m, int6
 int bs_w8_linear(bs_ctx *ctx, const void *q, const float *scales, const void *weight, const float *weight_scales, int64_t m, int64_t n, int64_t k, void *y,
                  int64_t y_stride, void *stream);
 
+/* How bs_w8_linear divides a product, for tests (host only): rows and outputs of a workgroup, ranges of k that are added up by a second kernel. */
+int bs_w8_division(bs_ctx *ctx, int64_t m, int64_t n, int64_t k, int32_t *rows, int32_t *outputs, int32_t *ranges);
+
+/* Both for rows of bf16 (as for bs_w8_quantize), in one launch where rows are few.  scratch: device, bs_w8_scratch_bytes(m, k) bytes (0: may be NULL),
+ * 16-byte aligned, the call's own until its work is done. */
+int64_t bs_w8_scratch_bytes(int64_t m, int64_t k);
+int bs_w8_linear_rows(bs_ctx *ctx, const void *x, int64_t x_stride, const void *weight, const float *weight_scales, int64_t m, int64_t n, int64_t k, void *y,
+                      int64_t y_stride, void *scratch, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

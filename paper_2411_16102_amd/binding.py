@@ -212,6 +212,10 @@ def raw():
         lib.bs_kv4_compact.argtypes = [_p, _p, _i32, _i64, _i32, _p, _i64, _p, _p, _p]
         lib.bs_w8_quantize.argtypes = [_p, _p, _i64, _i64, _i64, _p, _p, _p]
         lib.bs_w8_linear.argtypes = [_p, _p, _p, _p, _p, _i64, _i64, _i64, _p, _i64, _p]
+        lib.bs_w8_division.argtypes = [_p, _i64, _i64, _i64, _i32p, _i32p, _i32p]
+        lib.bs_w8_scratch_bytes.argtypes = [_i64, _i64]
+        lib.bs_w8_scratch_bytes.restype = _i64
+        lib.bs_w8_linear_rows.argtypes = [_p, _p, _i64, _p, _p, _i64, _i64, _i64, _p, _i64, _p, _p]
         lib.bs_batch_free.argtypes = [C.POINTER(BatchOwned)]
         lib.bs_batch_free.restype = None
         _lib = lib
@@ -486,11 +490,11 @@ class Layer:
     # that stream, so that its memory is neither somebody else's yet nor anybody's before the work is done.  As with every call on a
     # stream other than the current one, the caller orders it behind what makes its inputs, keeps these until it is done, and orders what reads
     # the result behind it (Stream.wait_stream, Tensor.record_stream).
-    def _new(self, like, shape, stream):
+    def _new(self, like, shape, stream, dtype=None):
         if stream is None:
-            return like.new_empty(shape)
+            return like.new_empty(shape, dtype=dtype)
         with self.torch.cuda.stream(stream):
-            return like.new_empty(shape)
+            return like.new_empty(shape, dtype=dtype)
 
     def window_plan(self, batch, window: int, sinks: int = 0, positions=None, axis_of_pair=None, n_pages: Optional[int] = None, stream=None,
                     cache: Optional["Kv4"] = None):
@@ -669,11 +673,7 @@ class Layer:
             if t.dtype is not self._bf16_type or not t.is_contiguous() or t.dim() != 4 or tuple(t.shape) != (k.shape[0], s.page_size, s.n_kv_heads, s.head_dim):
                 raise ValueError("kv4_pack: contiguous bf16 [n_pages, %d, %d, %d], got %s %s" % (s.page_size, s.n_kv_heads, s.head_dim, t.dtype, tuple(t.shape)))
         n = k.shape[0]
-        if stream is None:
-            pool = self.torch.empty(n * size, dtype=self.torch.uint8, device=k.device)
-        else:
-            with self.torch.cuda.stream(stream):
-                pool = self.torch.empty(n * size, dtype=self.torch.uint8, device=k.device)
+        pool = self._new(k, (n * size,), stream, self.torch.uint8)
         self._check(self.lib.bs_kv4_pack(self.h, k.data_ptr(), v.data_ptr(), pool.data_ptr(), n, cache.group, self._raw_stream(stream)))
         return pool
 
@@ -685,55 +685,34 @@ class Layer:
         if pool.dtype is not self.torch.uint8 or not pool.is_contiguous() or pool.numel() % size:
             raise ValueError("kv4_unpack: contiguous uint8 of whole pages of %d bytes, got %s %s" % (size, pool.dtype, tuple(pool.shape)))
         shape = (pool.numel() // size, s.page_size, s.n_kv_heads, s.head_dim)
-        if stream is None:
-            k, v = (self.torch.empty(shape, dtype=self._bf16_type, device=pool.device) for _ in range(2))
-        else:
-            with self.torch.cuda.stream(stream):
-                k, v = (self.torch.empty(shape, dtype=self._bf16_type, device=pool.device) for _ in range(2))
+        k, v = self._new(pool, shape, stream, self._bf16_type), self._new(pool, shape, stream, self._bf16_type)
         self._check(self.lib.bs_kv4_unpack(self.h, pool.data_ptr(), k.data_ptr(), v.data_ptr(), shape[0], cache.group, self._raw_stream(stream)))
         return k, v
 
 
     def w8_quantize(self, x, stream=None) -> "W8Rows":
         """Rows [m, k] bf16 as 8-bit integers with a scale each (bs_w8_quantize): the inputs of several products, or a weight [n, k]."""
-        torch = self.torch
-        if x.get_device() != self.device:
-            self._here("w8_quantize", x)
-        if x.dtype is not self._bf16_type or x.dim() != 2:
-            raise ValueError("w8_quantize: bf16 rows, got %s %s" % (x.dtype, tuple(x.shape)))
+        stride = self._w8_stride("w8_quantize", x)
         m, k = x.shape
-        stride, inner = x.stride()
-        if m and inner != 1:
-            raise ValueError("w8_quantize: rows of x are not contiguous")
-        if m <= 1:
-            stride = k  # (a single row has no stride)
-        if stream is None:
-            q, scales = x.new_empty((m, k), dtype=torch.int8), x.new_empty((m,), dtype=torch.float32)
-        else:
-            with torch.cuda.stream(stream):
-                q, scales = x.new_empty((m, k), dtype=torch.int8), x.new_empty((m,), dtype=torch.float32)
+        q, scales = self._new(x, (m, k), stream, self.torch.int8), self._new(x, (m,), stream, self.torch.float32)
         rc = self.lib.bs_w8_quantize(self.h, x.data_ptr(), stride, m, k, q.data_ptr(), scales.data_ptr(), self._raw_stream(stream))
         if rc:
             self._check(rc)
         return W8Rows(q, scales)
 
     def w8_linear(self, x, weight: "W8Weight", out=None, stream=None):
-        """Rows times a weight in 8-bit integers: [m, n] bf16.  x: bf16 [m, k], brought to integers first, or the W8Rows of w8_quantize."""
-        rows = x if type(x) is W8Rows else self.w8_quantize(x, stream)
-        q, w = rows.q, weight.q
-        if q.get_device() != self.device or w.get_device() != self.device:
-            self._here("w8_linear", q, w)
-        m, k = q.shape
+        """Rows times a weight in 8-bit integers: [m, n] bf16.  x: bf16 [m, k], brought to integers on the way, or the W8Rows of w8_quantize."""
+        rows = x.q if isinstance(x, W8Rows) else x
+        w = weight.q
+        if rows.get_device() != self.device or w.get_device() != self.device:
+            self._here("w8_linear", rows, w)
+        stride = 0 if rows is not x else self._w8_stride("w8_linear", x)
+        m, k = rows.shape
         n = w.shape[0]
         if w.shape[1] != k:
             raise ValueError("w8_linear: rows of %d inputs, the weight has %d" % (k, w.shape[1]))
         if out is None:
-            if stream is None:
-                out = q.new_empty((m, n), dtype=self._bf16_type)
-            else:
-                with self.torch.cuda.stream(stream):
-                    out = q.new_empty((m, n), dtype=self._bf16_type)
-            out_stride = n
+            out, out_stride = self._new(rows, (m, n), stream, self._bf16_type), n
         else:
             if out.get_device() != self.device:
                 self._here("w8_linear", out)
@@ -742,11 +721,35 @@ class Layer:
                 raise ValueError("w8_linear: out is not bf16 [%d, %d]" % (m, n))
             if m == 1:
                 out_stride = n
-        rc = self.lib.bs_w8_linear(self.h, q.data_ptr(), rows.scales.data_ptr(), w.data_ptr(), weight.scales.data_ptr(), m, n, k, out.data_ptr(), out_stride,
-                                   self._raw_stream(stream))
+        where = self._raw_stream(stream)
+        if rows is not x:
+            rc = self.lib.bs_w8_linear(self.h, rows.data_ptr(), x.scales.data_ptr(), w.data_ptr(), weight.scales.data_ptr(), m, n, k, out.data_ptr(), out_stride, where)
+        else:
+            size = self.lib.bs_w8_scratch_bytes(m, k)
+            scratch = self._new(x, (size,), stream, self.torch.uint8) if size else None
+            rc = self.lib.bs_w8_linear_rows(self.h, x.data_ptr(), stride, w.data_ptr(), weight.scales.data_ptr(), m, n, k, out.data_ptr(), out_stride,
+                                            scratch.data_ptr() if size else None, where)
         if rc:
             self._check(rc)
         return out
+
+    def w8_division(self, m: int, n: int, k: int):
+        """(rows and outputs of a workgroup, ranges of k) of a product of 8-bit integers; host only."""
+        out = [C.c_int32() for _ in range(3)]
+        self._check(self.lib.bs_w8_division(self.h, m, n, k, *(C.byref(v) for v in out)))
+        return tuple(v.value for v in out)
+
+    def _w8_stride(self, what, x):
+        """Elements from one row of x to the next."""
+        if x.get_device() != self.device:
+            self._here(what, x)
+        if x.dtype is not self._bf16_type or x.dim() != 2:
+            raise ValueError("%s: bf16 rows, got %s %s" % (what, x.dtype, tuple(x.shape)))
+        stride, inner = x.stride()
+        m, k = x.shape
+        if m and inner != 1:
+            raise ValueError("%s: rows of x are not contiguous" % what)
+        return k if m <= 1 else stride  # (a single row has no stride)
 
 
 def _address(a: np.ndarray) -> int:

@@ -31,6 +31,17 @@ __device__ __forceinline__ float from_lane(float v) {
   return __uint_as_float(from_lane<N>(__float_as_uint(v)));
 }
 
+// c + (lane N of each sixteen's v) x in one instruction, which the compiler does not make of the two.  It does not see either that a lane's register
+// must have been written two wait states before another lane reads it: v passes through settled() when it has been written.
+template <int N>
+__device__ __forceinline__ float add_from_lane(float c, float v, float x) {
+  asm("v_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf" : "+v"(c) : "v"(v), "v"(x), "n"(N));
+  return c;
+}
+__device__ __forceinline__ void settled(float (&v)[8]) {
+  asm volatile("s_nop 1" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
+}
+
 // The columns of a unit as in window_device.hpp, on codes.  A value is mid + scale (code - 8), with numbers for each token and group g of channels, so
 //   score_t  = sum over g of scale_tg (q_g . (code_tg - 8)) + mid_tg sum(q_g)
 //   output_c = sum over t of (p_t scale_tg) (code_tc - 8) + p_t mid_tg
@@ -43,6 +54,7 @@ struct FourBitPages {
   static constexpr int KC = DH / 32, DB = DH / 16, NG = DH / GROUP, STEPS = GROUP / 32, BLOCKS = GROUP / 16;
   f32x4_t common[NG];  // of all channels of a group
   float q_sum[NG];
+  Unpack unpack;
 
   __device__ __forceinline__ explicit FourBitPages(const bf16x8_t (&qf)[KC]) {
 #pragma unroll
@@ -74,31 +86,34 @@ struct FourBitPages {
     struct Frags {
       u32x4_t k[KW], v[VW], numbers;
     };
-    const unsigned char *pool = reinterpret_cast<const unsigned char *>(a.kv_pool);
-    const uint32_t k_off = 4 * kv4_keys_at(g4, jq & 7, 0, 0, DH), v_off = 4 * kv4_values_at(g4 & 1, jq, DH);
-    const uint32_t n_off = 16 * DH + (g4 & 1) * 64 * NG + jq % (4 * NG) * 16;  // (kind, group) jq of this lane's eight tokens
+    const unsigned char *pool = reinterpret_cast<const unsigned char *>(a.kv_pool) + (size_t)kvh * HEAD;
+    const unsigned char *k_base = pool + 4 * kv4_keys_at(g4, jq & 7, 0, 0, DH), *v_base = pool + 4 * kv4_values_at(g4 & 1, jq, DH);
+    const unsigned char *n_base = pool + 16 * DH + (g4 & 1) * 64 * NG + jq % (4 * NG) * 16;  // (kind, group) jq of this lane's eight tokens
+    const uint32_t page_bytes = (uint32_t)hkv * (uint32_t)HEAD;
     auto load = [&](int pr, Frags &f) __attribute__((always_inline)) {  // (past the end: the last page again, not used)
-      const size_t p0 = (size_t)__builtin_amdgcn_readlane(my_page, min(2 * pr, n_pg - 1)), p1 = (size_t)__builtin_amdgcn_readlane(my_page, min(2 * pr + 1, n_pg - 1));
-      const unsigned char *b0 = pool + (p0 * hkv + kvh) * HEAD, *b1 = pool + (p1 * hkv + kvh) * HEAD;
-      const unsigned char *kp = (jq < 8 ? b0 : b1) + k_off, *vp = g4 < 2 ? b0 : b1;
-      f.numbers = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(vp + n_off));
+      const uint32_t p0 = __builtin_amdgcn_readlane(my_page, min(2 * pr, n_pg - 1)), p1 = __builtin_amdgcn_readlane(my_page, min(2 * pr + 1, n_pg - 1));
+      const uint64_t k_at = (uint64_t)(jq < 8 ? p0 : p1) * page_bytes, v_at = (uint64_t)(g4 < 2 ? p0 : p1) * page_bytes;
+      f.numbers = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(n_base + v_at));
 #pragma unroll
-      for (int i = 0; i < KW; ++i) f.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(kp) + i);
+      for (int i = 0; i < KW; ++i) f.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(k_base + k_at) + i);
 #pragma unroll
-      for (int i = 0; i < VW; ++i) f.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(vp + v_off) + i);
+      for (int i = 0; i < VW; ++i) f.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(v_base + v_at) + i);
     };
     auto compute = [&](int pr, Frags &f) __attribute__((always_inline)) {
-      const int tb = 32 * pr;
-      if (2 * pr >= n_pg) return;  // wave-uniform
+      const int tb = 32 * pr;  // (a pair past the end is masked whole: an early way out would cost copies of all accumulators)
       const int u0 = tb + 8 * g4;  // this lane's eight tokens
+      // (Masks are for few pairs.  What passes through an empty asm stays in its branch: left alone, the compiler computes all of them for every pair.)
       const bool whole = tb + 32 <= 16 * n_pg && tb + 31 <= first && (tb > last - a.window || tb + 32 <= sinks);
       if (!whole) {  // wave-uniform: the numbers of tokens that no row sees (the codes of such tokens are numbers whatever their bits)
+        int u = u0;
+        asm volatile("" : "+v"(f.numbers), "+v"(u));
         const int end = min(16 * n_pg, last + 1), unseen = first - a.window + 1;
-        f.numbers = mask_between8(mask_tokens8(f.numbers, u0, end), u0, sinks, unseen);
+        f.numbers = mask_between8(mask_tokens8(f.numbers, u, end), u, sinks, unseen);
       }
       float num[8];  // a kind and group of this lane's tokens
 #pragma unroll
       for (int r = 0; r < 8; ++r) num[r] = __uint_as_float(r & 1 ? f.numbers[r >> 1] & 0xFFFF0000u : f.numbers[r >> 1] << 16);
+      settled(num);
       float sv[8];
       f32x4_t s[NG][2];
 #pragma unroll
@@ -109,21 +124,23 @@ struct FourBitPages {
           for (int i = 0; i < 2; ++i) {
             const int w = i * KC + g * STEPS + k;
             const float from = -CENTRE * q_sum[g];
-            s[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(sixteen_plus(f.k[w >> 2][w & 3])), qf[g * STEPS + k],
+            s[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unpack(f.k[w >> 2][w & 3])), qf[g * STEPS + k],
                                                               k == 0 ? f32x4_t{from, from, from, from} : s[g][i], 0, 0, 0);
           }
       each<NG>([&](auto g_) __attribute__((always_inline)) {
         constexpr int g = decltype(g_)::value;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-          const float m = from_lane<NG + g>(num[r]) * q_sum[g];
-          sv[r] = __builtin_fmaf(from_lane<g>(num[r]), s[g][r >> 2][r & 3], g == 0 ? m : sv[r] + m);
+          const float x = from_lane<g>(num[r]) * s[g][r >> 2][r & 3];
+          sv[r] = add_from_lane<NG + g>(g == 0 ? x : sv[r] + x, num[r], q_sum[g]);
         }
       });
       if (!whole) {
+        int from = u0;
+        asm volatile("" : "+v"(sv[0]), "+v"(sv[1]), "+v"(sv[2]), "+v"(sv[3]), "+v"(sv[4]), "+v"(sv[5]), "+v"(sv[6]), "+v"(sv[7]), "+v"(from));
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-          const int u = u0 + r;  // (one condition, selected by: see window_device.hpp)
+          const int u = from + r;  // (one condition, selected by: see window_device.hpp)
           const bool hidden = (u > at) | ((u <= at - a.window) & (u >= sinks)) | (u >= 16 * n_pg);
           sv[r] = hidden ? -INFINITY : sv[r];
         }
@@ -161,7 +178,7 @@ struct FourBitPages {
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
           const int db = g * BLOCKS + b;
-          c.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(sixteen_plus(f.v[db >> 2][db & 3])), px, c.o[db], 0, 0, 0);
+          c.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unpack(f.v[db >> 2][db & 3])), px, c.o[db], 0, 0, 0);
         }
       });
     };

@@ -6,16 +6,22 @@
 namespace bs {
 namespace kv4_dev {
 
-// bits of two codes in a word, and 16.0 in both halves
-constexpr uint32_t CODES = 0x00780078u, SIXTEENS = 0x41804180u;
 constexpr float CENTRE = 24.f;  // 16 + code less this is code - 8
 
 __device__ __forceinline__ uint32_t turn_left3(uint32_t w) { return __builtin_amdgcn_alignbit(w, w, 29); }
 
-// The eight elements of a word as bf16 numbers 16 + code.  Bits 3 to 6 of a bf16 number between 16 and 32 count whole numbers.
-__device__ __forceinline__ u32x4_t sixteen_plus(uint32_t w) {
-  return u32x4_t{(w & CODES) | SIXTEENS, ((w >> 4) & CODES) | SIXTEENS, ((w >> 8) & CODES) | SIXTEENS, (__builtin_amdgcn_alignbit(w, w, 12) & CODES) | SIXTEENS};
-}
+// The eight elements of a word as bf16 numbers 16 + code.  Bits 3 to 6 of a bf16 number between 16 and 32 count whole numbers.  The two constants are
+// in registers of their own, so that an and and an or are one instruction (which takes one constant at most).
+struct Unpack {
+  uint32_t codes, sixteens;
+  __device__ __forceinline__ Unpack() {
+    asm("s_mov_b32 %0, 0x780078" : "=s"(codes));
+    asm("v_mov_b32 %0, 0x41804180" : "=v"(sixteens));
+  }
+  __device__ __forceinline__ u32x4_t operator()(uint32_t w) const {
+    return u32x4_t{(w & codes) | sixteens, ((w >> 4) & codes) | sixteens, ((w >> 8) & codes) | sixteens, (__builtin_amdgcn_alignbit(w, w, 12) & codes) | sixteens};
+  }
+};
 
 // element j of a word
 __device__ __forceinline__ uint32_t code_of(uint32_t w, int j) { return (__builtin_amdgcn_alignbit(w, w, 3) >> (4 * (j >> 1) + 16 * (j & 1))) & 15u; }
