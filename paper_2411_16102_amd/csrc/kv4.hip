@@ -90,8 +90,7 @@ __device__ __forceinline__ void append_codes(unsigned char *page, int n_rows, in
     }
     __syncthreads();
     for (int i = t; i < heads * 2 * DH; i += ROPE_THREADS) {
-      constexpr int B = DH / 16;
-      const int w = i % DH, half = i / DH & 1, ho = i / (2 * DH), channel = 16 * (w % B) + w / B;
+      const int w = i % DH, half = i / DH & 1, ho = i / (2 * DH), channel = w / 64 * 64 + 16 * (w % 4) + w / 4 % 16;
       const int s0 = max(slot0, 8 * half), s1 = min(slot0 + n_rows, 8 * half + 8);
       if (h + ho >= h1 || s0 >= s1) continue;
       uint32_t *at = reinterpret_cast<uint32_t *>(page + (size_t)(h + ho) * kv4_head_bytes(DH, GROUP)) + kv4_values_at(half, channel, DH);

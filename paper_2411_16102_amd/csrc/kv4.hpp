@@ -1,10 +1,10 @@
 // A paged cache in four bits (see blendstep_bits.h): where things stand in a page, and the kernels that write and read it.
 //
 // A page holds, for each KV head, one block behind the other:
-//   keys    words [4 g][8 r][2 i][dh / 32 s]: codes of channels 32 s + 8 g .. + 7 of token 8 (r / 4) + 4 i + r % 4
-//   values  words [2 halves][16][dh / 16 b]:  codes of tokens 8 half .. + 7 of channel 16 b + index
-//   numbers bf16  [2 halves][kind][group][8]: of tokens 8 half .. + 7; kinds: scale and mid of keys, then of values
-// so that a lane of a matrix product's operand loads its part of a page 16 bytes at a time.  Element j of a word is at bits
+//   keys    words [2 i][4 g][8 r][4 s] (64-wide heads: [4 g][8 r][2 i][2 s]): codes of channels 32 s + 8 g .. + 7 of token 8 (r / 4) + 4 i + r % 4
+//   values  words [dh / 64][2 halves][16][4 b]: codes of tokens 8 half .. + 7 of channel 64 first + 16 b + third index
+//   numbers bf16  [2 halves][group][kind][8]: of tokens 8 half .. + 7; kinds: scale and mid of keys, then of values
+// so that a lane of a matrix product's operand loads its part of a page 16 bytes at a time, neighbours side by side.  Element j of a word is at bits
 // 4 (j / 2) + 16 (j % 2), turned left by 3: a shift, an and and an or make two bf16 numbers 16 + code of it (see kv4_device.hpp).
 #pragma once
 #include <stdint.h>
@@ -18,10 +18,14 @@ constexpr bool kv4_shape(int head_dim, int group) {
   return (head_dim == 64 || head_dim == 128) && (group == 32 || group == 64 || group == 128) && group <= head_dim;
 }
 constexpr int kv4_head_bytes(int head_dim, int group) { return 16 * head_dim + 128 * (head_dim / group); }
-constexpr int kv4_keys_at(int g4, int r8, int i, int s, int head_dim) { return ((g4 * 8 + r8) * 2 + i) * (head_dim / 32) + s; }  // word
-constexpr int kv4_values_at(int half, int channel, int head_dim) { return 2 * head_dim + (half * 16 + channel % 16) * (head_dim / 16) + channel / 16; }  // word
+constexpr int kv4_keys_at(int g4, int r8, int i, int s, int head_dim) {  // word
+  return head_dim == 128 ? ((i * 4 + g4) * 8 + r8) * 4 + s : ((g4 * 8 + r8) * 2 + i) * 2 + s;
+}
+constexpr int kv4_values_at(int half, int channel, int head_dim) {  // word
+  return 2 * head_dim + ((channel / 64 * 2 + half) * 16 + channel % 16) * 4 + channel / 16 % 4;
+}
 constexpr int kv4_number_at(int token, int kind, int g, int head_dim, int group) {  // byte
-  return 16 * head_dim + (token >> 3) * 64 * (head_dim / group) + (kind * (head_dim / group) + g) * 16 + (token & 7) * 2;
+  return 16 * head_dim + (token >> 3) * 64 * (head_dim / group) + (g * 4 + kind) * 16 + (token & 7) * 2;
 }
 
 // bs_rope_append into such a cache: the queries turned, keys turned and coded, values coded.

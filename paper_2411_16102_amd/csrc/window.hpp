@@ -24,11 +24,12 @@ struct WindowArgs {
   const int32_t *item_pages;
   int n_items, window;
   int waves;                     // of a workgroup: 1, 2, 4 or 8, which share its run of pages
+  int heads;                     // KV heads of a workgroup (a cache in four bits, see kv4_attn.hip: 1 or 2)
   const uint16_t *q, *kv_pool;
   uint16_t *out;
   int64_t q_stride, out_stride;  // elements of a row
-  float *parts;                  // [states][Hkv][dh / 16 + 1][64 lanes][4]: accumulators as the lanes hold them, then (m, l) of a column
-  unsigned *counters;            // [states][Hkv], zero between launches
+  float *parts;                  // [states][Hkv / heads][dh / 16 + 1][64 lanes][4]: accumulators as the lanes hold them, then (m, l) of a column
+  unsigned *counters;            // [states][Hkv / heads], zero between launches
 };
 hipError_t launch_window_units(const WindowArgs &a, hipStream_t stream);
 // Narrow and wide work of a step in one launch (a.waves is 4).

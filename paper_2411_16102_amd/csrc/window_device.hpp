@@ -124,9 +124,9 @@ __device__ __forceinline__ void walk_pages(const WindowArgs &a, const WindowItem
   }
 }
 
-// four results of a column, dh = 16 db + 4 g4 ..
-__device__ __forceinline__ void store_quad(const WindowArgs &a, const WindowItem &it, int kvh, int dh, int lane, int db, f32x4_t o, float l) {
-  const int grp = a.s.n_q_heads / a.s.n_kv_heads, jq = lane & 15;
+// four results of a column (jq: its number among those of KV head kvh), dh = 16 db + 4 g4 ..
+__device__ __forceinline__ void store_quad(const WindowArgs &a, const WindowItem &it, int kvh, int jq, int dh, int lane, int db, f32x4_t o, float l) {
+  const int grp = a.s.n_q_heads / a.s.n_kv_heads;
   const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that sees nothing gives zeros; a NaN stays one)
   u32x2_t w;
   w.x = pack_bf16x2(o[0] * inv, o[1] * inv);
@@ -146,24 +146,29 @@ struct Bf16Pages {
     walk_pages<DH>(a, it, kvh, lane, pg0, pg1, qf, c);
   }
   __device__ __forceinline__ void finish(Columns<DH> &) {}
+  static constexpr int HEADS = 1;  // KV heads whose columns share a wavefront
+  static constexpr int joined(int blocks) { return blocks <= 4 ? 8 : 4; }  // states of so many blocks that a join has on the way
 };
 
 template <int DH, int NW, class Pages = Bf16Pages<DH>>
 __device__ __forceinline__ void window_unit(const WindowArgs &a, int block, unsigned char *lds) {
   constexpr int DB = DH / 16;
-  const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int CPH = 16 / Pages::HEADS;  // columns of a KV head
+  const int grp = a.s.n_q_heads / a.s.n_kv_heads, hkv = a.s.n_kv_heads / Pages::HEADS, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const WindowItem it = a.items[block / hkv];
-  const int kvh = block % hkv;
-  const bool ok = (lane & 15) < it.n_rows * grp;
+  const int kvh = block % hkv;  // (times HEADS: the first of the KV heads)
+  const int col = (lane & 15) % CPH, col_head = kvh * Pages::HEADS + (lane & 15) / CPH;
+  const bool ok = col < it.n_rows * grp;
   // pairs of pages in nearly equal shares
   const int n_pairs = (it.n_pages + 1) >> 1;
   const int pg0 = 2 * (int)((int64_t)n_pairs * wave / NW), pg1 = min(it.n_pages, 2 * (int)((int64_t)n_pairs * (wave + 1) / NW));
   bf16x8_t qf[DH / 32];
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i) {
-    const int jq = ok ? lane & 15 : 0;
+    const int jq = ok ? col : 0;
     u32x4_t v = {0u, 0u, 0u, 0u};
-    if (ok) v = ld16(a.q + (it.row0 + jq / grp) * a.q_stride + (kvh * grp + jq % grp) * DH + 32 * i + 8 * (lane >> 4));
+    if (ok) v = ld16(a.q + (it.row0 + jq / grp) * a.q_stride + (col_head * grp + jq % grp) * DH + 32 * i + 8 * (lane >> 4));
     qf[i] = as_bf16x8(v);
   }
   Columns<DH> c;
@@ -172,7 +177,7 @@ __device__ __forceinline__ void window_unit(const WindowArgs &a, int block, unsi
   c.m = NEG_BIG;
   c.l = 0.f;
   Pages pages(qf);
-  for (int pg = pg0; pg < pg1; pg += 64) pages.walk(a, it, kvh, lane, pg, min(pg + 64, pg1), qf, c);
+  for (int pg = pg0; pg < pg1; pg += 64) pages.walk(a, it, kvh * Pages::HEADS, lane, pg, min(pg + 64, pg1), qf, c);
   pages.finish(c);
   c.l += __shfl_xor(c.l, 16, 64);
   c.l += __shfl_xor(c.l, 32, 64);
@@ -180,7 +185,7 @@ __device__ __forceinline__ void window_unit(const WindowArgs &a, int block, unsi
     if (it.state < 0) {
       if (ok)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) store_quad(a, it, kvh, DH, lane, db, c.o[db], c.l);
+        for (int db = 0; db < DB; ++db) store_quad(a, it, col_head, col, DH, lane, db, c.o[db], c.l);
       return;
     }
   }
@@ -237,7 +242,7 @@ __device__ __forceinline__ void window_unit(const WindowArgs &a, int block, unsi
     m = NEG_BIG;
     l = 0.f;
     if (ok) {
-      constexpr int B = MINE <= 4 ? 8 : 4;  // states on the way
+      constexpr int B = Pages::joined(MINE);  // states on the way
       for (unsigned p = 0; p < n; p += B) {
         f32x4_t s[B], v[B][MINE];
 #pragma unroll
@@ -268,7 +273,7 @@ __device__ __forceinline__ void window_unit(const WindowArgs &a, int block, unsi
   if (ok)
 #pragma unroll
     for (int k = 0; k < MINE; ++k)
-      if (wave * MINE + k < DB) store_quad(a, it, kvh, DH, lane, wave * MINE + k, o[k], l);
+      if (wave * MINE + k < DB) store_quad(a, it, col_head, col, DH, lane, wave * MINE + k, o[k], l);
 }
 
 }  // namespace window_dev

@@ -26,7 +26,7 @@ constexpr long STAGE_WORDS = 1 << 16;   // of the plan's pinned memory at first 
 // What the kernels of a planned step need to know beside the arrays on the device.
 struct Planned {
   bool made = false, has_angles = false, whole_axes = true;
-  int n_rows = 0, n_rope = 0, n_items = 0, waves = 1, window = 1, sinks = 0;
+  int n_rows = 0, n_rope = 0, n_items = 0, waves = 1, heads = 1, window = 1, sinks = 0;
   int n_work = 0, n_cut = 0, wide_blocks = 0;   // wide work: workgroups per group of heads, blocks of rows that several share, all blocks
   int32_t longest = 0, split_rows = 0;
   long states = 0, cut_states = 0, pages = 0;
@@ -204,6 +204,13 @@ Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int dh, int n
   while (div.waves > 1 && n_units * div.waves > 12 * (int64_t)n_cu) div.waves /= 2;
   div.us = best;
   return div;
+}
+
+// Whether the columns of two KV heads have room in a wavefront over a cache in four bits (see kv4_attn.hip).
+bool two_heads(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g) {
+  int most = 1;
+  for (const bs_window::Rows &r : rows) most = std::max(most, r.n);
+  return most * (g.n_q_heads / g.n_kv_heads) <= 8 && g.n_kv_heads % 2 == 0;
 }
 
 // The units of the rows of narrow work.
@@ -412,6 +419,7 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cf
     cut_blocks(w, cut.blocks);
     div = {4, std::max(div.pages, 8), 0.0};  // (one launch for both kinds, of workgroups of four wavefronts)
   }
+  p.heads = w->group && two_heads(w->rows, g) ? 2 : 1;
   if (const int rc = add_units(w, b, div)) return rc;
   p.n_items = (int)w->items.size();
   p.pages += (long)w->item_pages.size();
@@ -701,6 +709,7 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
     a.q = (const uint16_t *)q; a.kv_pool = (const uint16_t *)kv_pool; a.out = (uint16_t *)out;
     a.q_stride = q_stride; a.out_stride = out_stride;
     a.waves = p.waves;
+    a.heads = p.heads;
     a.parts = w->d_states;
     a.counters = w->d_counters;
     if (p.n_work) {

@@ -17,7 +17,8 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -8
 
 # query heads, KV heads, head size, group
-SHAPES = [(8, 2, 128, 128), (8, 2, 128, 64), (16, 1, 128, 32), (8, 2, 64, 64), (4, 4, 64, 32), (6, 2, 128, 64), (3, 1, 64, 32), (14, 2, 128, 32)]
+SHAPES = [(8, 2, 128, 128), (8, 2, 128, 64), (16, 1, 128, 32), (8, 2, 64, 64), (4, 4, 64, 32), (6, 2, 128, 64), (3, 1, 64, 32), (14, 2, 128, 32),
+          (16, 4, 128, 64), (32, 8, 128, 128), (32, 8, 64, 32), (12, 4, 64, 64), (8, 4, 128, 32)]
 
 
 def make_layer(lib, hq, hkv, dh, **kw):
