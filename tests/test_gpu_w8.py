@@ -80,6 +80,22 @@ def test_products(lib, layer, m, n, k):
     assert torch.equal(y.view(torch.int16), again.view(torch.int16))
 
 
+@pytest.mark.parametrize("m,n,k,tile", [(9, 2857, 3952, (16, 16)), (1, 5123, 7728, (16, 32)), (51, 412, 4352, (32, 16)), (20, 13329, 2368, (32, 32)),
+                                        (53, 15186, 2432, (64, 128)), (678, 1071, 5008, (128, 128)), (845, 18071, 2880, (128, 256)),
+                                        (433, 17789, 10000, (160, 256)), (1123, 9151, 4160, (192, 256)), (2166, 13634, 20416, (256, 256))])
+def test_every_tile(lib, layer, m, n, k, tile):
+    import torch
+    assert layer.w8_division(m, n, k)[:2] == tile
+    g = torch.Generator(device="cuda").manual_seed(m)
+    q, w = (torch.randint(-128, 128, (i, k), dtype=torch.int8, device="cuda", generator=g) for i in (m, n))
+    scales, s = (1e-3 * (0.5 + torch.rand(i, device="cuda", generator=g)) for i in (m, n))
+    y = layer.w8_linear(lib.W8Rows(q, scales), lib.W8Weight(w, s)).double()
+    # (whole numbers below 2^53: exact in float64 in any order)
+    ref = (q.double() @ w.double().t()) * scales.double()[:, None] * s.double()[None]
+    wrong = (y - ref).abs() > BOUND * ref.abs() + 1e-37
+    assert not wrong.any(), "%d wrong, the first at %s" % (int(wrong.sum()), wrong.nonzero()[0].tolist())
+
+
 @pytest.mark.parametrize("m", [1, 9, 40, 150, 600])
 def test_strides_and_what_lies_between(lib, layer, m):
     # rows of x and y inside wider ones, results at odd addresses; what lies beside them stays
