@@ -36,11 +36,9 @@ int64_t bs_kv4_page_bytes(const bs_ctx *ctx, int32_t group);
 /* The cache that the steps planned on `w` from now on are for: bits 16 (group 0; what a new bs_window has), or 4 with the group's size.
  * Ends the planned step.  With four bits kv_pool of bs_rope_append and bs_window_attention is such a pool, 16-byte aligned.  All
  * that blendstep_stream.h says of them holds, but:
- *   - bs_window_plan also makes room for the pages that segments of many rows see, in bf16 (blendstep.h's page size each; it keeps the
- *     largest size seen): they are converted once a call, for all rows of their segment.  What is kept of keys and values is rounded to bf16
- *     there.  Few rows and single tokens read the codes themselves.
  *   - probabilities are rounded to bf16 after a multiplication with the scales of values
- *   - a query with an infinity gives NaN. */
+ *   - a query with an infinity gives NaN
+ *   - the wide_blocks of bs_window_division are units of one KV head too, of twice the rows of a narrow unit, with all of their pages. */
 int bs_window_cache(bs_window *w, int32_t bits, int32_t group);
 
 /* k, v: device bf16, token-major [n_pages][16][n_kv_heads][head_dim], 16-byte aligned; kv_pool: n_pages pages in four bits.  kv4_unpack gives what the

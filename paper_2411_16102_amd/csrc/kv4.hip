@@ -89,19 +89,33 @@ __device__ __forceinline__ void append_codes(unsigned char *page, int n_rows, in
       }
     }
     __syncthreads();
-    for (int i = t; i < heads * 2 * DH; i += ROPE_THREADS) {
-      const int w = i % DH, half = i / DH & 1, ho = i / (2 * DH), channel = w / 64 * 64 + 16 * (w % 4) + w / 4 % 16;
-      const int s0 = max(slot0, 8 * half), s1 = min(slot0 + n_rows, 8 * half + 8);
-      if (h + ho >= h1 || s0 >= s1) continue;
-      uint32_t *at = reinterpret_cast<uint32_t *>(page + (size_t)(h + ho) * kv4_head_bytes(DH, GROUP)) + kv4_values_at(half, channel, DH);
-      uint32_t c[8];
-      const uint32_t old = s1 - s0 == 8 ? 0u : *at;
+    // words of the halves of the page that have rows, a few of a thread on the way at a time
+    const int half0 = slot0 >> 3, halves = ((slot0 + n_rows - 1) >> 3) - half0 + 1, n_words = min(heads, h1 - h) * halves * DH;
+    constexpr int U = 4;
+    for (int i0 = t; i0 < n_words; i0 += U * ROPE_THREADS) {
+      uint32_t *at[U], old[U];
+      int half[U], channel[U], ho[U];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int s = 8 * half + j;
-        c[j] = s >= s0 && s < s1 ? codes[(ho << shift) + s - slot0][channel] : code_of(old, j);
+      for (int u = 0; u < U; ++u) {
+        const int i = min(i0 + u * ROPE_THREADS, n_words - 1), w = i % DH;
+        const int rest = i / DH;
+        half[u] = half0 + (halves == 2 ? rest & 1 : 0);
+        ho[u] = halves == 2 ? rest >> 1 : rest;
+        channel[u] = w / 64 * 64 + 16 * (w % 4) + w / 4 % 16;
+        at[u] = reinterpret_cast<uint32_t *>(page + (size_t)(h + ho[u]) * kv4_head_bytes(DH, GROUP)) + kv4_values_at(half[u], channel[u], DH);
+        old[u] = slot0 <= 8 * half[u] && slot0 + n_rows >= 8 * half[u] + 8 ? 0u : *at[u];
       }
-      *at = word_of(c);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i0 + u * ROPE_THREADS >= n_words) break;
+        uint32_t c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int s = 8 * half[u] + j - slot0;
+          c[j] = s >= 0 && s < n_rows ? codes[(ho[u] << shift) + s][channel[u]] : code_of(old[u], j);
+        }
+        *at[u] = word_of(c);
+      }
     }
     __syncthreads();
   }
@@ -171,42 +185,6 @@ __global__ __launch_bounds__(256) void kv4_unpack_kernel(const Kv4Pages p) {
   }
 }
 
-// Pages as the ring kernel of longer segments reads them (see blendstep.h: keys [Hkv][16][dh], values [Hkv][dh][16]): once per step
-// instead of once per block of rows.
-template <int DH, int GROUP>
-__global__ __launch_bounds__(256) void kv4_expand_kernel(const Kv4Expand x) {
-  constexpr int BYTES = kv4_head_bytes(DH, GROUP), C = DH / 8;
-  const int i = blockIdx.x / x.n_kv_heads, head = blockIdx.x % x.n_kv_heads;
-  const unsigned char *block = x.pool + ((size_t)x.list[i] * x.n_kv_heads + head) * BYTES;
-  const uint32_t *words = reinterpret_cast<const uint32_t *>(block);
-  for (int j = threadIdx.x; j < 4 * DH; j += 256) {
-    const bool value = j >= 2 * DH;
-    const int p = j % (2 * DH);
-    float v[8];
-    if (!value) {  // eight channels of a token
-      const int t = p / C, e = p % C * 8;
-      const uint32_t w = words[kv4_keys_at(e / 8 & 3, 4 * (t >> 3) + (t & 3), t >> 2 & 1, e >> 5, DH)];
-      const float scale = bf16_to_f32(*reinterpret_cast<const uint16_t *>(block + kv4_number_at(t, 0, e / GROUP, DH, GROUP)));
-      const float mid = bf16_to_f32(*reinterpret_cast<const uint16_t *>(block + kv4_number_at(t, 1, e / GROUP, DH, GROUP)));
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = value_of(scale, mid, code_of(w, k));
-    } else {  // eight tokens of a channel
-      const int channel = p >> 1, half = p & 1;
-      const uint32_t w = words[kv4_values_at(half, channel, DH)];
-      const u32x4_t scale = *reinterpret_cast<const u32x4_t *>(block + kv4_number_at(8 * half, 2, channel / GROUP, DH, GROUP));
-      const u32x4_t mid = *reinterpret_cast<const u32x4_t *>(block + kv4_number_at(8 * half, 3, channel / GROUP, DH, GROUP));
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        v[k] = value_of(__uint_as_float(k & 1 ? scale[k >> 1] & 0xFFFF0000u : scale[k >> 1] << 16),
-                        __uint_as_float(k & 1 ? mid[k >> 1] & 0xFFFF0000u : mid[k >> 1] << 16), code_of(w, k));
-    }
-    u32x4_t out;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) out[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
-    *reinterpret_cast<u32x4_t *>(x.out + (((size_t)i * 2 + value) * x.n_kv_heads + head) * 16 * DH + (size_t)p * 8) = out;
-  }
-}
-
 // calls f with the head size and group as constants
 template <class F>
 hipError_t with_shape(int head_dim, int group, F &&f) {
@@ -225,9 +203,9 @@ hipError_t with_shape(int head_dim, int group, F &&f) {
 
 hipError_t launch_rope_append4(const RopeArgs &a, int group, hipStream_t stream) {
   if (a.n_items <= 0) return hipSuccess;
-  // Shares of the query heads: workgroups for a few rounds of the chip, of at least four heads.  Of the KV heads: as many as a pass takes.
-  const int rows = (a.n_rows + a.n_items - 1) / a.n_items;
-  const int shares = std::max(1, std::min(2048 / a.n_items, a.n_q_heads / 4)), kv_shares = rows > 4 ? a.n_kv_heads : 1;
+  // Shares of the query heads: workgroups for a few rounds of the chip, of at least four heads.  Of the KV heads: as many as a pass takes of a whole
+  // page's rows (of few rows it takes them all, but a workgroup that has several waits for one after the other where others have whole pages).
+  const int shares = std::max(1, std::min(2048 / a.n_items, a.n_q_heads / 4)), kv_shares = std::max(1, a.n_kv_heads * a.head_dim / 128);
   const dim3 grid((unsigned)a.n_items * (unsigned)(shares + kv_shares)), block(ROPE_THREADS);
   return with_shape(a.head_dim, group, [&](auto dh, auto g) {
     if (a.whole) hipLaunchKernelGGL((rope_append4_kernel<dh(), g(), true>), grid, block, 0, stream, a, shares, kv_shares);
@@ -248,14 +226,6 @@ hipError_t launch_kv4_unpack(const Kv4Pages &p, hipStream_t stream) {
   if (p.n_pages <= 0) return hipSuccess;
   return with_shape(p.head_dim, p.group, [&](auto dh, auto g) {
     hipLaunchKernelGGL((kv4_unpack_kernel<dh(), g()>), dim3((unsigned)(p.n_pages * p.n_kv_heads)), dim3(256), 0, stream, p);
-    return hipGetLastError();
-  });
-}
-
-hipError_t launch_kv4_expand(const Kv4Expand &x, hipStream_t stream) {
-  if (x.n <= 0) return hipSuccess;
-  return with_shape(x.head_dim, x.group, [&](auto dh, auto g) {
-    hipLaunchKernelGGL((kv4_expand_kernel<dh(), g()>), dim3((unsigned)x.n * (unsigned)x.n_kv_heads), dim3(256), 0, stream, x);
     return hipGetLastError();
   });
 }

@@ -39,17 +39,18 @@ __device__ __forceinline__ void settled(float (&v)[8]) {
 // columns each.  Columns of other heads are zero in a head's queries, so that the products of all heads add up in the same accumulators,
 // and in its probabilities.  A lane's numbers are those of its column's head: four lanes have the four kinds (scale and mid of keys, of values) of
 // a group in one load, and take them from one another.
-template <int DH, int GROUP, int HEADS_>
-struct FourBitPages {
-  static constexpr int HEADS = HEADS_, CPH = 16 / HEADS;
-  static constexpr int KC = DH / 32, DB = DH / 16, NG = DH / GROUP, STEPS = GROUP / 32, BLOCKS = GROUP / 16;
-  static constexpr int joined(int blocks) { return blocks <= 1 ? 8 : blocks <= 4 ? 4 : 2; }
-  bf16x8_t q[HEADS][KC];
-  f32x4_t common[NG];  // of all channels of a group
-  float q_sum[NG], mids[NG];
+//
+// The rows of a longer segment share their pages too: BLOCKS blocks of sixteen columns to a wavefront, for which a code is brought to 16 + code once.
+template <int DH, int GROUP, int HEADS, int BLOCKS>
+struct FourBits {
+  static_assert(HEADS == 1 || BLOCKS == 1, "columns of several heads, or several blocks of them");
+  static constexpr int CPH = 16 / HEADS, KC = DH / 32, DB = DH / 16, NG = DH / GROUP, STEPS = GROUP / 32, PER = GROUP / 16;
+  bf16x8_t q[HEADS * BLOCKS][KC];
+  f32x4_t common[BLOCKS][NG];  // of all channels of a group
+  float q_sum[BLOCKS][NG], mids[BLOCKS][NG];
   Unpack unpack;
 
-  __device__ __forceinline__ explicit FourBitPages(const bf16x8_t (&qf)[KC]) {
+  __device__ __forceinline__ void begin(int b, const bf16x8_t (&qf)[KC]) {
     const int mine = (threadIdx.x & 15) / CPH;
 #pragma unroll
     for (int h = 0; h < HEADS; ++h)
@@ -57,12 +58,12 @@ struct FourBitPages {
       for (int i = 0; i < KC; ++i) {
         u32x4_t v = __builtin_bit_cast(u32x4_t, qf[i]);
         if (HEADS > 1 && mine != h) v = u32x4_t{0u, 0u, 0u, 0u};
-        q[h][i] = as_bf16x8(v);
+        q[h + b][i] = as_bf16x8(v);
       }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      common[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      mids[g] = 0.f;
+      common[b][g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      mids[b][g] = 0.f;
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < STEPS; ++i)
@@ -70,37 +71,44 @@ struct FourBitPages {
         for (int k = 0; k < 8; ++k) s += (float)qf[g * STEPS + i][k];
       s += __shfl_xor(s, 16, 64);
       s += __shfl_xor(s, 32, 64);
-      q_sum[g] = s;
+      q_sum[b][g] = s;
     }
   }
 
-  // pages [pg0, pg1) of the unit, at most 64, of KV heads kvh ..
-  __device__ __forceinline__ void walk(const WindowArgs &a, const WindowItem &it, int kvh, int lane, int pg0, int pg1, const bf16x8_t (&)[KC], Columns<DH> &c) {
+  // pages [pg0, pg1) of the unit, at most 64, of KV heads kvh ..; pages that others read too (SHARED) stay in the caches
+  template <bool SHARED>
+  __device__ __forceinline__ void walk(const WindowArgs &a, const WindowItem &it, int kvh, int lane, int pg0, int pg1, Columns<DH> (&c)[BLOCKS]) {
     constexpr int KW = DH / 64, VW = DH / 64;  // 16-byte loads of a head's keys and of its values
     constexpr int HEAD = kv4_head_bytes(DH, GROUP);
     const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv;
     const int jq = lane & 15, g4 = lane >> 4, col = jq % CPH, mine = jq / CPH;
     const float sc = a.s.scale_log2e;
-    const int j = col < it.n_rows * grp ? col / grp : 0;
     // places are counted from this wavefront's first page
-    const int n_pg = pg1 - pg0, first = it.at - 16 * pg0, last = first + it.n_rows - 1, at = first + j, sinks = it.sinks - 16 * pg0;
+    const int n_pg = pg1 - pg0, first = it.at - 16 * pg0, last = first + it.n_rows - 1, sinks = it.sinks - 16 * pg0;
+    int at[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) at[b] = first + (16 * b + col < it.n_rows * grp ? (16 * b + col) / grp : 0);
     const int my_page = a.item_pages[it.page_off + pg0 + min(lane, n_pg - 1)];  // lane i holds page i
     const unsigned char *pool = reinterpret_cast<const unsigned char *>(a.kv_pool) + (size_t)kvh * HEAD;
     const unsigned char *k_base = pool + 4 * kv4_keys_at(g4, jq & 7, 0, 0, DH), *v_base = pool + 4 * kv4_values_at(g4 & 1, jq, DH);
     const unsigned char *n_base = pool + (size_t)mine * HEAD + kv4_number_at(8 * (g4 & 1), jq & 3, 0, DH, GROUP);  // kind jq % 4 of this lane's eight tokens
     const uint32_t page_bytes = (uint32_t)hkv * (uint32_t)HEAD;
     u32x4_t k[HEADS][KW], v[HEADS][VW], numbers[NG];
+    auto ask = [](const unsigned char *p) __attribute__((always_inline)) {
+      if constexpr (SHARED) return *reinterpret_cast<const u32x4_t *>(p);
+      else return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+    };
     // (past the end: the last page again, not used)
     auto page = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane(my_page, min(i, n_pg - 1)); };
     auto load_keys = [&](int pr) __attribute__((always_inline)) {
       const uint32_t p0 = page(2 * pr), p1 = page(2 * pr + 1);
       const unsigned char *n_at = n_base + (uint64_t)(g4 < 2 ? p0 : p1) * page_bytes, *k_at = k_base + (uint64_t)(jq < 8 ? p0 : p1) * page_bytes;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) numbers[g] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(n_at) + 4 * g);
+      for (int g = 0; g < NG; ++g) numbers[g] = ask(n_at + 64 * g);
 #pragma unroll
       for (int h = 0; h < HEADS; ++h)
 #pragma unroll
-        for (int i = 0; i < KW; ++i) k[h][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(k_at + h * HEAD) + 32 * i);
+        for (int i = 0; i < KW; ++i) k[h][i] = ask(k_at + h * HEAD + 512 * i);
     };
     auto load_values = [&](int pr) __attribute__((always_inline)) {
       const uint32_t p0 = page(2 * pr), p1 = page(2 * pr + 1);
@@ -108,7 +116,7 @@ struct FourBitPages {
 #pragma unroll
       for (int h = 0; h < HEADS; ++h)
 #pragma unroll
-        for (int i = 0; i < VW; ++i) v[h][i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(v_at + h * HEAD) + 32 * i);
+        for (int i = 0; i < VW; ++i) v[h][i] = ask(v_at + h * HEAD + 512 * i);
     };
     load_keys(0);
     load_values(0);
@@ -130,120 +138,206 @@ struct FourBitPages {
         for (int r = 0; r < 8; ++r) num[g][r] = __uint_as_float(r & 1 ? numbers[g][r >> 1] & 0xFFFF0000u : numbers[g][r >> 1] << 16);
         settled(num[g]);
       }
-      // (four accumulators in turn at least: a product that goes on from the last one's result waits for it)
-      constexpr int TURNS = NG == 1 ? 2 : 1;
-      f32x4_t s[NG][TURNS][2];
+      // scores, some groups of channels at a time; four accumulators in turn at least: a product that goes on from the last one's result waits for it
+      constexpr int GS = BLOCKS == 1 && NG >= 2 ? NG : 1, TURNS = BLOCKS == 1 && GS == 1 ? 2 : 1;
+      float sv[BLOCKS][8];
 #pragma unroll
-      for (int g = 0; g < NG; ++g)
+      for (int g0 = 0; g0 < NG; g0 += GS) {
+        f32x4_t s[GS][TURNS][BLOCKS][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float from = -CENTRE * q_sum[g];
-          s[g][0][i] = f32x4_t{from, from, from, from};
-          if constexpr (TURNS == 2) s[g][1][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
+        for (int g = 0; g < GS; ++g)
 #pragma unroll
-      for (int h = 0; h < HEADS; ++h)
-#pragma unroll
-        for (int n = 0; n < STEPS; ++n)
-#pragma unroll
-          for (int g = 0; g < NG; ++g)
+          for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const int w = i * KC + g * STEPS + n;
-              f32x4_t &to = s[g][(h * STEPS + n) % TURNS][i];
-              to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unpack(k[h][w >> 2][w & 3])), q[h][g * STEPS + n], to, 0, 0, 0);
-              __builtin_amdgcn_sched_barrier(0x7F6);  // (in this order; all but matrix instructions may move)
+              const float from = -CENTRE * q_sum[b][g0 + g];
+              s[g][0][b][i] = f32x4_t{from, from, from, from};
+              if constexpr (TURNS == 2) s[g][1][b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
-      float sv[8];
 #pragma unroll
-      for (int g = 0; g < NG; ++g)
+        for (int h = 0; h < HEADS; ++h)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          float d = s[g][0][r >> 2][r & 3];
-          if constexpr (TURNS == 2) d += s[g][1][r >> 2][r & 3];
-          const float x = of_quad<0>(num[g][r]) * d;
-          sv[r] = add_of_quad<1>(g == 0 ? x : sv[r] + x, num[g][r], q_sum[g]);
-        }
+          for (int n = 0; n < STEPS; ++n)
+#pragma unroll
+            for (int g = 0; g < GS; ++g)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int step = (g0 + g) * STEPS + n, w = i * KC + step;
+                const bf16x8_t codes = as_bf16x8(unpack(k[h][w >> 2][w & 3]));
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                  f32x4_t &to = s[g][(h * STEPS + n) % TURNS][b][i];
+                  to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, q[h + b][step], to, 0, 0, 0);
+                  __builtin_amdgcn_sched_barrier(0x7F6);  // (in this order; all but matrix instructions may move)
+                }
+              }
+#pragma unroll
+        for (int g = 0; g < GS; ++g)
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              float d = s[g][0][b][r >> 2][r & 3];
+              if constexpr (TURNS == 2) d += s[g][1][b][r >> 2][r & 3];
+              const float x = of_quad<0>(num[g0 + g][r]) * d;
+              sv[b][r] = add_of_quad<1>(g0 + g == 0 ? x : sv[b][r] + x, num[g0 + g][r], q_sum[b][g0 + g]);
+            }
+      }
       load_keys(pr + 1);
-      if (!whole) {
-        int from = u0;
-        asm volatile("" : "+v"(sv[0]), "+v"(sv[1]), "+v"(sv[2]), "+v"(sv[3]), "+v"(sv[4]), "+v"(sv[5]), "+v"(sv[6]), "+v"(sv[7]), "+v"(from));
+#pragma unroll
+      for (int b = 0; b < BLOCKS; ++b) {
+        float(&sb)[8] = sv[b];
+        if (!whole) {
+          int from = u0;
+          asm volatile("" : "+v"(sb[0]), "+v"(sb[1]), "+v"(sb[2]), "+v"(sb[3]), "+v"(sb[4]), "+v"(sb[5]), "+v"(sb[6]), "+v"(sb[7]), "+v"(from));
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const int u = from + r;  // (one condition, selected by: see window_device.hpp)
+            const bool hidden = (u > at[b]) | ((u <= at[b] - a.window) & (u >= sinks)) | (u >= 16 * n_pg);
+            sb[r] = hidden ? -INFINITY : sb[r];
+          }
+        }
+        float mx = sc * fmaxf(fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])), fmaxf(fmaxf(sb[4], sb[5]), fmaxf(sb[6], sb[7])));
+        if (__builtin_amdgcn_ballot_w64(mx > c[b].m + TAU) != 0) {  // (see TAU: the reference moves rarely)
+          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          const float m_new = fmaxf(c[b].m, mx), alpha = fast_exp2(c[b].m - m_new);
+          c[b].m = m_new;
+          c[b].l *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) c[b].o[db] *= alpha;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            common[b][g] *= alpha;
+            mids[b][g] *= alpha;
+          }
+        }
+        float ps = 0.f;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-          const int u = from + r;  // (one condition, selected by: see window_device.hpp)
-          const bool hidden = (u > at) | ((u <= at - a.window) & (u >= sinks)) | (u >= 16 * n_pg);
-          sv[r] = hidden ? -INFINITY : sv[r];
+          sb[r] = fast_exp2(__builtin_fmaf(sb[r], sc, -c[b].m));
+          ps += sb[r];
         }
+        c[b].l += ps;
       }
-      float mx = sc * fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-      if (__builtin_amdgcn_ballot_w64(mx > c.m + TAU) != 0) {  // (see TAU: the reference moves rarely)
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(c.m, mx), alpha = fast_exp2(c.m - m_new);
-        c.m = m_new;
-        c.l *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) c.o[db] *= alpha;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          common[g] *= alpha;
-          mids[g] *= alpha;
-        }
-      }
-      float ps = 0.f;
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        sv[r] = fast_exp2(__builtin_fmaf(sv[r], sc, -c.m));
-        ps += sv[r];
-      }
-      c.l += ps;
-      const uint32_t less = 0xC1C0C1C0u;  // -24 twice
-      u32x4_t px[NG];
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
+      u32x4_t px[BLOCKS];  // probabilities times scale
+      auto scaled = [&](int b, int g) __attribute__((always_inline)) {
+        const uint32_t less = 0xC1C0C1C0u;  // -24 twice
         float x[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-          x[r] = of_quad<2>(num[g][r]) * sv[r];
-          mids[g] = add_of_quad<3>(mids[g], num[g][r], sv[r]);
+          x[r] = of_quad<2>(num[g][r]) * sv[b][r];
+          mids[b][g] = add_of_quad<3>(mids[b][g], num[g][r], sv[b][r]);
         }
-        px[g] = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-        common[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4_t{less, less, less, less}), as_bf16x8(px[g]), common[g], 0, 0, 0);
-      }
-#pragma unroll
-      for (int h = 0; h < HEADS; ++h)
+        px[b] = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+        common[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4_t{less, less, less, less}), as_bf16x8(px[b]), common[b][g], 0, 0, 0);
+      };
+      if constexpr (HEADS == 1) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          u32x4_t own = px[g];
-          if constexpr (HEADS > 1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) own[i] = mine == h ? px[g][i] : 0u;
-          }
+          for (int b = 0; b < BLOCKS; ++b) scaled(b, g);
 #pragma unroll
-          for (int b = 0; b < BLOCKS; ++b) {
-            const int db = g * BLOCKS + b;
-            c.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unpack(v[h][db >> 2][db & 3])), as_bf16x8(own), c.o[db], 0, 0, 0);
+          for (int n = 0; n < PER; ++n) {
+            const int db = g * PER + n;
+            const bf16x8_t codes = as_bf16x8(unpack(v[0][db >> 2][db & 3]));
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) c[b].o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, as_bf16x8(px[b]), c[b].o[db], 0, 0, 0);
           }
         }
+      } else {
+        u32x4_t all[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          scaled(0, g);
+          all[g] = px[0];
+        }
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            u32x4_t own;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) own[i] = mine == h ? all[db / PER][i] : 0u;
+            c[0].o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unpack(v[h][db >> 2][db & 3])), as_bf16x8(own), c[0].o[db], 0, 0, 0);
+          }
+      }
       load_values(pr + 1);
     }
   }
 
-  __device__ __forceinline__ void finish(Columns<DH> &c) {
+  __device__ __forceinline__ void finish(int b, Columns<DH> &c) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      mids[g] += __shfl_xor(mids[g], 16, 64);
-      mids[g] += __shfl_xor(mids[g], 32, 64);
+      mids[b][g] += __shfl_xor(mids[b][g], 16, 64);
+      mids[b][g] += __shfl_xor(mids[b][g], 32, 64);
     }
 #pragma unroll
-    for (int db = 0; db < DB; ++db) c.o[db] += common[db / BLOCKS] + mids[db / BLOCKS];
+    for (int db = 0; db < DB; ++db) c.o[db] += common[b][db / PER] + mids[b][db / PER];
   }
 };
 
-// wavefronts that the registers of a SIMD hold
-constexpr int resident(int dh, int group, int heads) { return dh == 128 ? (heads == 2 || group == 32 ? 2 : 3) : heads == 2 ? 3 : 4; }
+// As window_unit walks them: one block of columns.
+template <int DH, int GROUP, int HEADS_>
+struct FourBitPages : FourBits<DH, GROUP, HEADS_, 1> {
+  static constexpr int HEADS = HEADS_;
+  static constexpr int joined(int blocks) { return blocks <= 1 ? 8 : blocks <= 4 ? 4 : 2; }
+  __device__ __forceinline__ explicit FourBitPages(const bf16x8_t (&qf)[DH / 32]) { this->begin(0, qf); }
+  __device__ __forceinline__ void walk(const WindowArgs &a, const WindowItem &it, int kvh, int lane, int pg0, int pg1, const bf16x8_t (&)[DH / 32], Columns<DH> &c) {
+    Columns<DH> one[1] = {c};
+    FourBits<DH, GROUP, HEADS_, 1>::template walk<false>(a, it, kvh, lane, pg0, pg1, one);
+    c = one[0];
+  }
+  __device__ __forceinline__ void finish(Columns<DH> &c) { FourBits<DH, GROUP, HEADS_, 1>::finish(0, c); }
+};
+
+// Rows of longer segments: a wavefront per (item, KV head), two blocks of columns, all of the pages that they see; the four of a workgroup take
+// items next to one another, which walk the same pages.  Bound by what a SIMD issues: for two blocks 323 vector operations and 34 matrix
+// instructions a pair of pages (128 channels in one group), 112 of them to bring codes to bf16 - one block has 210.  Six segments of about 700 rows behind
+// 1500 tokens, 8 KV heads with four queries each: 224 us, as narrow work 233.  Slower: three or four blocks with all registers, one wavefront a SIMD
+// (319 and 384 us); workgroups of one or two wavefronts (233); pages brought to fp16 and bf16 once for the kernel of longer segments of a cache in
+// bf16 took 199 us there, but with all batches of its kind 1.4 to 1.8 times the time of these, and a second copy of the pages.
+template <int DH, int GROUP>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_rows4_kernel(const WindowArgs a) {
+  const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = (int)(blockIdx.x / hkv) * 4 + wave, kvh = blockIdx.x % hkv;
+  if (item >= a.n_items) return;
+  const WindowItem it = a.items[item];
+  FourBits<DH, GROUP, 1, KV4_ROW_BLOCKS> bits;
+  Columns<DH> c[KV4_ROW_BLOCKS];
+#pragma unroll
+  for (int b = 0; b < KV4_ROW_BLOCKS; ++b) {
+    const int col = 16 * b + (lane & 15);
+    const bool ok = col < it.n_rows * grp;
+    bf16x8_t qf[DH / 32];
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i) {
+      u32x4_t v = {0u, 0u, 0u, 0u};
+      if (ok) v = ld16(a.q + (it.row0 + col / grp) * a.q_stride + (kvh * grp + col % grp) * DH + 32 * i + 8 * (lane >> 4));
+      qf[i] = as_bf16x8(v);
+    }
+    bits.begin(b, qf);
+#pragma unroll
+    for (int db = 0; db < DH / 16; ++db) c[b].o[db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    c[b].m = NEG_BIG;
+    c[b].l = 0.f;
+  }
+  for (int pg = 0; pg < it.n_pages; pg += 64) bits.template walk<true>(a, it, kvh, lane, pg, min(pg + 64, it.n_pages), c);
+#pragma unroll
+  for (int b = 0; b < KV4_ROW_BLOCKS; ++b) {
+    bits.finish(b, c[b]);
+    float l = c[b].l;
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const int col = 16 * b + (lane & 15);
+    if (col < it.n_rows * grp)
+#pragma unroll
+      for (int db = 0; db < DH / 16; ++db) store_quad(a, it, kvh, col, DH, lane, db, c[b].o[db], l);
+  }
+}
+
 template <int DH, int GROUP, int HEADS, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(resident(DH, GROUP, HEADS), resident(DH, GROUP, HEADS)))) void window_unit4_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(kv4_resident(DH, GROUP, HEADS), kv4_resident(DH, GROUP, HEADS)))) void window_unit4_kernel(const WindowArgs a) {
   __shared__ __align__(16) unsigned char lds[WINDOW_UNIT_LDS(DH, NW)];
   window_unit<DH, NW, FourBitPages<DH, GROUP, HEADS>>(a, blockIdx.x, lds);
 }
@@ -266,6 +360,17 @@ hipError_t launch_units4(const WindowArgs &a, hipStream_t stream) {
 }
 
 }  // namespace
+
+hipError_t launch_window_rows4(const WindowArgs &a, int group, hipStream_t stream) {
+  if (a.n_items <= 0) return hipSuccess;
+  const dim3 grid((unsigned)((a.n_items + 3) / 4) * (unsigned)a.s.n_kv_heads), block(256);
+  if (a.s.head_dim == 128 && group == 128) hipLaunchKernelGGL((window_rows4_kernel<128, 128>), grid, block, 0, stream, a);
+  else if (a.s.head_dim == 128 && group == 64) hipLaunchKernelGGL((window_rows4_kernel<128, 64>), grid, block, 0, stream, a);
+  else if (a.s.head_dim == 64 && group == 64) hipLaunchKernelGGL((window_rows4_kernel<64, 64>), grid, block, 0, stream, a);
+  else if (a.s.head_dim == 64 && group == 32) hipLaunchKernelGGL((window_rows4_kernel<64, 32>), grid, block, 0, stream, a);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
 
 hipError_t launch_window_units4(const WindowArgs &a, int group, hipStream_t stream) {
   if (a.n_items <= 0) return hipSuccess;

@@ -33,8 +33,8 @@ struct Planned {
   long off_items = 0, off_pages = 0, off_rope = 0, off_positions = 0, off_axis = 0, words = 0;
   long off_work = 0, off_cut = 0, off_row_start = 0, off_kv_len = 0, off_page_start = 0, off_page_ids = 0;
   long at_cut_acc = 0, at_cut_m = 0, at_cut_l = 0, state_floats = 0;  // partial states, in floats
-  long off_expand = 0;
-  int n_expand = 0;                             // pages in four bits that wide work reads as bf16
+  long off_wide = 0;
+  int n_wide = 0;                               // wide units over a cache in four bits
 };
 
 }  // namespace
@@ -50,14 +50,13 @@ struct bs_window {
   long cap_states = 0;
   unsigned *d_counters = nullptr;
   long cap_counters = 0;
-  uint16_t *d_expanded = nullptr;  // pages in four bits as bf16
-  long cap_expanded = 0;
   // host scratch reused across plans
-  std::vector<int32_t> words, refs, item_pages, cut, wide_start, wide_pages, expand;
+  std::vector<int32_t> words, refs, item_pages, cut, wide_start, wide_pages;
   std::vector<WindowItem> items;
   std::vector<RopeItem> rope;
   struct Rows { int seq, first, n, pages; };  // rows of narrow work that share their units
-  std::vector<Rows> rows;
+  std::vector<Rows> rows, wide_rows;          // wide_rows: of wide work over a cache in four bits, two blocks of columns each
+  std::vector<WindowItem> wide_items;
   struct Work { int blocks, seq, block, t0, t1, state; };
   std::vector<Work> work;
 };
@@ -136,13 +135,13 @@ int check_seen(bs_window *w, int seq, const int32_t *table, const Seen &seen) {
 int too_large(bs_window *w) { return ctx_fail(w->ctx, BS_EUNSUPPORTED, "the step is too large for one plan"); }
 
 // Rows [j, end) of a sequence as narrow work, at most `per_unit` in a unit.
-int add_rows(bs_window *w, const bs_batch *b, int s, int j, int end, int per_unit) {
+int add_rows(bs_window *w, const bs_batch *b, int s, int j, int end, int per_unit, std::vector<bs_window::Rows> *to = nullptr) {
   const int rows = b->row_start[s + 1] - b->row_start[s];
   for (; j < end; j += per_unit) {
     const int n = std::min(per_unit, end - j), p0 = b->kv_len[s] - rows + j;
     const Seen seen = seen_by(p0, p0 + n - 1, w->p.window, w->p.sinks);
     if (const int rc = check_seen(w, s, b->page_ids + b->page_start[s], seen)) return rc;
-    w->rows.push_back({s, j, n, seen.pages()});
+    (to ? *to : w->rows).push_back({s, j, n, seen.pages()});
   }
   return BS_OK;
 }
@@ -156,6 +155,7 @@ int add_rows(bs_window *w, const bs_batch *b, int s, int j, int end, int per_uni
 struct Division {
   int waves, pages;
   double us;
+  int heads = 1;  // KV heads of a workgroup
 };
 Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int dh, int n_cu) {
   int64_t all = 0, once = 0;  // pages of all units; without those that rows of the same sequence have seen before
@@ -206,11 +206,60 @@ Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int dh, int n
   return div;
 }
 
-// Whether the columns of two KV heads have room in a wavefront over a cache in four bits (see kv4_attn.hip).
-bool two_heads(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g) {
-  int most = 1;
-  for (const bs_window::Rows &r : rows) most = std::max(most, r.n);
-  return most * (g.n_q_heads / g.n_kv_heads) <= 8 && g.n_kv_heads % 2 == 0;
+// The same over a cache in four bits, whose units read less and compute more: KV heads that share a wavefront too, where the columns of two have
+// room (see kv4_attn.hip).  A wavefront takes `step` microseconds a page; what its registers allow is on the chip at a time, in rounds; or the bytes
+// are longer.  Fitted to 4000 batches of 1 to 300 streams (up to 16000 tokens, equal and unequal, five head layouts, all groups) timed in every
+// division with 1, 2 and 4 wavefronts: 3.4 % off the best on average, 15 % for one in twenty, 34 % at worst; the division of the cache in bf16 is 29 % off.
+Division divide4(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g, int group, int n_cu) {
+  int64_t once = 0, every = 0;
+  int longest = 0, last = -1, most_rows = 1;
+  for (const bs_window::Rows &r : rows) {
+    every += r.pages;
+    once += r.seq == last ? std::min(r.pages, 1) : r.pages;
+    last = r.seq;
+    longest = std::max(longest, r.pages);
+    most_rows = std::max(most_rows, r.n);
+  }
+  const int hkv = g.n_kv_heads, dh = g.head_dim;
+  const bool two = most_rows * (g.n_q_heads / hkv) <= 8 && hkv % 2 == 0;
+  const double bytes_us = 0.133e-6 * (double)once * hkv * kv4_head_bytes(dh, group);
+  Division best = {1, std::max(2, longest), 0.0, 1};
+  bool any = false;
+  for (int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
+    const int pages = std::max(2, 2 * ((longest + 2 * n - 1) / (2 * n)));
+    if (n > 1 && pages < 4) break;
+    int64_t all = 0, joined = 0;
+    int most = 0;
+    for (const bs_window::Rows &r : rows) {
+      const int k = std::max(1, (r.pages + pages - 1) / pages);
+      all += k;
+      joined += k > 1 ? k : 0;
+      most = std::max(most, k);
+    }
+    for (int waves : {1, 2, 4}) {
+      if (waves > 1 && pages < 2 * waves) break;
+      int64_t steps = 0;  // pages that the first wavefront of every unit takes
+      int longest_steps = 0;
+      for (const bs_window::Rows &r : rows) {
+        const int k = std::max(1, (r.pages + pages - 1) / pages), s = ((r.pages + k - 1) / k + 2 * waves - 1) / (2 * waves) * 2;
+        steps += (int64_t)k * s;
+        longest_steps = std::max(longest_steps, s);
+      }
+      for (int heads = 1; heads <= (two ? 2 : 1); ++heads) {
+        const double step = (0.272 + 0.043 * (dh / group)) * (dh == 128 ? 1.0 : 0.707) * (heads == 2 ? 1.34 : 1.0);
+        const double units = (double)all * hkv / heads, slots = 4.0 * n_cu * kv4_resident(dh, group, heads) / waves;
+        const double alone = 1.44 + step * longest_steps, mean = 2.91 + 1.18 * step * (double)steps / std::max<int64_t>(1, all);
+        // (rows that share their pages, which the caches then hold, are bound by what a SIMD computes)
+        const double compute = ((dh == 128 ? 0.27 : 0.16) + 0.055 * (dh / group)) * (heads == 2 ? 0.75 : 1.0) * (double)every * hkv / (4.0 * n_cu);
+        const double load = std::max(compute, mean * (units / slots + 0.31 * (std::ceil(units / slots) - units / slots)));
+        const double us = 3.36 + std::max({bytes_us + 0.087 * alone, alone, load}) + 0.54 * std::min(bytes_us, load) +
+                          (joined ? 0.75 + 0.22 * most + 0.0011 * (double)joined * hkv / heads : 0.0);
+        if (!any || us < best.us) best = {waves, pages, us, heads};
+        any = true;
+      }
+    }
+  }
+  return best;
 }
 
 // The units of the rows of narrow work.
@@ -249,6 +298,33 @@ int add_units(bs_window *w, const bs_batch *b, const Division &div) {
   }
   // longest first: the short ones then fill the end of the launch
   std::stable_sort(w->items.begin(), w->items.end(), [](const auto &x, const auto &y) { return x.n_pages > y.n_pages; });
+  // wide units over a cache in four bits: rows next to one another stay next to one another in fours, the fours longest first
+  w->wide_items.clear();
+  for (const bs_window::Rows &r : w->wide_rows) {
+    const int r0 = b->row_start[r.seq], p0 = b->kv_len[r.seq] - (b->row_start[r.seq + 1] - r0) + r.first;
+    const Seen seen = seen_by(p0, p0 + r.n - 1, p.window, p.sinks);
+    WindowItem it{};
+    it.row0 = r0 + r.first;
+    it.n_rows = r.n;
+    it.page_off = (int32_t)w->item_pages.size();
+    it.n_pages = r.pages;
+    it.at = p0 - seen.left_out();
+    it.sinks = std::max(0, std::min(p.sinks, PAGE * r.pages));
+    it.state = -1;
+    w->wide_items.push_back(it);
+    for (int i = 0; i < r.pages; ++i) w->item_pages.push_back(b->page_ids[b->page_start[r.seq] + seen.page(i)]);
+    if (w->item_pages.size() > (size_t)MAX_LEN) return too_large(w);
+  }
+  std::vector<std::pair<int, int>> fours;
+  for (int i = 0; i < (int)w->wide_items.size(); i += 4) fours.push_back({-w->wide_items[std::min(i + 3, (int)w->wide_items.size() - 1)].n_pages, i});
+  std::stable_sort(fours.begin(), fours.end(), [](const auto &x, const auto &y) { return x.first < y.first; });
+  std::vector<WindowItem> sorted;
+  // (the last four may be fewer: they stay at the end)
+  for (int pass = 0; pass < 2; ++pass)
+    for (const auto &f : fours)
+      if ((f.second + 4 > (int)w->wide_items.size()) == (pass == 1))
+        sorted.insert(sorted.end(), w->wide_items.begin() + f.second, w->wide_items.begin() + std::min(f.second + 4, (int)w->wide_items.size()));
+  w->wide_items.swap(sorted);
   return BS_OK;
 }
 
@@ -256,10 +332,11 @@ int add_units(bs_window *w, const bs_batch *b, const Division &div) {
 struct Route {
   int per_unit;   // rows of a narrow unit
   int heads, rows;  // of a wide workgroup: query heads of one KV group, query rows
+  int per_wide;     // rows of a wide unit over a cache in four bits
 };
 Route route_of(const bs_layer_cfg &g) {
   const int grp = g.n_q_heads / g.n_kv_heads, heads = grp % 4 == 0 ? 4 : grp % 2 == 0 ? 2 : 1;
-  return {std::max(1, 16 / grp), heads, 64 * (4 / heads)};
+  return {std::max(1, 16 / grp), heads, 64 * (4 / heads), std::max(1, 16 * KV4_ROW_BLOCKS / grp)};
 }
 
 // The rows of a longer segment as blocks for wide workgroups; rows of blocks that stand wholly in front of their sequence see nothing:
@@ -317,10 +394,19 @@ Cut cut_choice(const std::vector<bs_window::Work> &work, int wg_per_work, int dh
   return best;
 }
 
-// The microseconds that are expected of the conversion of n pages in four bits: a launch, and bytes in and out.
-double expand_us(size_t n, const bs_layer_cfg &g, int group) {
-  if (n == 0) return 0.0;
-  return 2.0 + (double)n * g.n_kv_heads * (kv4_head_bytes(g.head_dim, group) + 64 * g.head_dim) / 4.0e6;
+// The microseconds that are expected of wide units over a cache in four bits, a tenth more: their expectation is the less certain one of the two.
+// Fitted to 13700 batches of 1 to 16 sequences of 5 to 3000 rows behind up to 8000 tokens, timed as narrow and as wide work: 8 % off on average,
+// and the shorter kind is chosen but for 0.4 % of the time, 11 % for one in a hundred.  (All of them as narrow work: 1 %; 28 % at the largest sizes.)
+double wide4_us(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g, int group, int n_cu) {
+  if (rows.empty()) return 0.0;
+  int64_t pages = 0;
+  int longest = 0;
+  for (const bs_window::Rows &r : rows) {
+    pages += r.pages;
+    longest = std::max(longest, r.pages);
+  }
+  const double step = (g.head_dim == 128 ? 0.58 : 0.40) + 0.14 * (g.head_dim / group), per_simd = g.n_kv_heads / (4.0 * n_cu);
+  return 1.1 * (6.1 + step * (0.47 * (double)pages * per_simd + 0.56 * longest + 4.3 * (double)rows.size() * per_simd));
 }
 
 void cut_blocks(bs_window *w, int most) {
@@ -350,25 +436,19 @@ int sort_rows(bs_window *w, const bs_batch *b, const Route &r, int most_narrow) 
   w->work.clear();
   w->wide_start.assign((size_t)b->n_seq + 1, 0);
   w->wide_pages.clear();
-  w->expand.clear();
+  w->wide_rows.clear();
   p.wide_blocks = 0;
   p.pages = 0;
   for (int s = 0; s < b->n_seq; ++s) {
     const int rows = b->row_start[s + 1] - b->row_start[s];
     w->wide_start[s] = (int32_t)w->wide_pages.size();
     if (rows > most_narrow) {
-      if (const int rc = add_blocks(w, b, s, r)) return rc;
-      const int32_t *table = b->page_ids + b->page_start[s];
-      if (w->group == 0) {
-        w->wide_pages.insert(w->wide_pages.end(), table, b->page_ids + b->page_start[s + 1]);
-      } else {  // the pages that its rows see, by their places among those that are converted
-        const Seen seen = seen_by(std::max(0, b->kv_len[s] - rows), b->kv_len[s] - 1, p.window, p.sinks);
-        w->wide_pages.resize(w->wide_pages.size() + (b->page_start[s + 1] - b->page_start[s]), BS_PAGE_NONE);
-        for (int i = 0; i < seen.pages(); ++i) {
-          w->wide_pages[w->wide_start[s] + seen.page(i)] = (int32_t)w->expand.size();
-          w->expand.push_back(table[seen.page(i)]);
-        }
+      if (w->group) {
+        if (const int rc = add_rows(w, b, s, 0, rows, r.per_wide, &w->wide_rows)) return rc;
+        continue;
       }
+      if (const int rc = add_blocks(w, b, s, r)) return rc;
+      w->wide_pages.insert(w->wide_pages.end(), b->page_ids + b->page_start[s], b->page_ids + b->page_start[s + 1]);
     } else if (const int rc = add_rows(w, b, s, 0, rows, r.per_unit)) {
       return rc;
     }
@@ -398,15 +478,16 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cf
   for (int k = 2; k >= 0; --k) {
     const int rows = rows_of[k];
     if (rows < most ? (k == 2 && !next) : k != 0) continue;  // (the same as another)
+    if (k && w->group && !kv4_has_rows(g.head_dim, w->group)) continue;
     if (k == 0 && best >= 0.0) {  // many rows as narrow work: more pages than could be worth it
       int64_t pages = 0;
       for (const bs_window::Work &x : w->work) pages += (int64_t)x.blocks * (r.rows / r.per_unit);
       if (pages * g.n_kv_heads * 0.1 > 2.0 * best * n_cu) continue;
     }
     if (const int rc = sort_rows(w, b, r, rows)) return rc;
-    const Division d = divide(w->rows, g.n_kv_heads, g.head_dim, n_cu);
+    const Division d = w->group ? divide4(w->rows, g, w->group, n_cu) : divide(w->rows, g.n_kv_heads, g.head_dim, n_cu);
     const Cut c = w->work.empty() ? Cut{0, 0.0} : cut_choice(w->work, g.n_q_heads / r.heads, g.head_dim, r.rows, n_cu);
-    const double us = d.us + c.us + expand_us(w->expand.size(), g, w->group);
+    const double us = d.us + c.us + wide4_us(w->wide_rows, g, w->group, n_cu);
     if (best < 0.0 || us < best) {
       best = us;
       div = d;
@@ -417,16 +498,16 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cf
   if (const int rc = sort_rows(w, b, r, chosen)) return rc;
   if (!w->work.empty()) {
     cut_blocks(w, cut.blocks);
-    div = {4, std::max(div.pages, 8), 0.0};  // (one launch for both kinds, of workgroups of four wavefronts)
+    if (!w->group) div = {4, std::max(div.pages, 8), 0.0};  // (one launch for both kinds, of workgroups of four wavefronts)
   }
-  p.heads = w->group && two_heads(w->rows, g) ? 2 : 1;
+  p.heads = div.heads;
   if (const int rc = add_units(w, b, div)) return rc;
   p.n_items = (int)w->items.size();
   p.pages += (long)w->item_pages.size();
   // longest first: the short ones then fill the end of the launch
   std::stable_sort(w->work.begin(), w->work.end(), [](const auto &x, const auto &y) { return x.blocks > y.blocks; });
   p.n_work = (int)w->work.size();
-  p.n_expand = (int)w->expand.size();
+  p.n_wide = (int)w->wide_items.size();
   p.n_cut = (int)w->cut.size() / 4;
   return BS_OK;
 }
@@ -517,7 +598,6 @@ void bs_window_destroy(bs_window *w) {
     if (w->d_words) (void)hipFree(w->d_words);
     if (w->d_states) (void)hipFree(w->d_states);
     if (w->d_counters) (void)hipFree(w->d_counters);
-    if (w->d_expanded) (void)hipFree(w->d_expanded);
     w->stage.close();
   }
   delete w;
@@ -566,7 +646,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     plan_appends(w, b);
     // (grids count units of a KV head, workgroups of some heads, and shares of the heads of a run)
     if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff ||
-        (int64_t)p.n_rope * (g.n_kv_heads + 1) + 4096 > 0x7fffffff || (int64_t)p.n_expand * g.n_kv_heads > 0x7fffffff)
+        (int64_t)p.n_rope * (g.n_kv_heads + 1) + 4096 > 0x7fffffff || ((int64_t)p.n_wide / 4 + 1) * g.n_kv_heads > 0x7fffffff)
       return fail_with(too_large(w));
 
     for (int i = 0; n_axes > 0 && i < half; ++i) p.whole_axes = p.whole_axes && axis_of_pair[i] == axis_of_pair[i & ~7];
@@ -580,8 +660,8 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     p.off_kv_len = p.off_row_start + n_tab;
     p.off_page_start = p.off_kv_len + n_tab;
     p.off_page_ids = p.off_page_start + n_tab;
-    p.off_expand = p.off_page_ids + n_wide_pages;
-    p.off_rope = whole_units(p.off_expand + p.n_expand);
+    p.off_wide = whole_units(p.off_page_ids + n_wide_pages);
+    p.off_rope = p.off_wide + 8L * p.n_wide;
     p.off_axis = p.off_rope + 4L * p.n_rope;
     p.off_positions = p.off_axis + half;
     p.words = whole_units(p.off_positions + (long)axes * rows);
@@ -604,7 +684,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
       std::memcpy(&words[p.off_page_start], w->wide_start.data(), sizeof(int32_t) * n_tab);
       if (n_wide_pages) std::memcpy(&words[p.off_page_ids], w->wide_pages.data(), sizeof(int32_t) * n_wide_pages);
     }
-    if (p.n_expand) std::memcpy(&words[p.off_expand], w->expand.data(), sizeof(int32_t) * p.n_expand);
+    if (p.n_wide) std::memcpy(&words[p.off_wide], w->wide_items.data(), sizeof(WindowItem) * p.n_wide);
     if (p.n_rope) std::memcpy(&words[p.off_rope], w->rope.data(), sizeof(RopeItem) * p.n_rope);
     p.has_angles = true;
     for (int s = 0; n_axes == 0 && s < b->n_seq; ++s) {
@@ -630,7 +710,6 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     p.state_floats = p.at_cut_l + n_cut;
     if (p.at_cut_acc > (1L << 29)) return fail_with(too_large(w));  // (offsets of the joins: 32 bits of bytes)
     if (const int rc = grow(c, &w->d_states, &w->cap_states, p.state_floats, sizeof(float))) return fail_with(rc);
-    if (const int rc = grow(c, &w->d_expanded, &w->cap_expanded, (long)p.n_expand * 2 * PAGE * g.n_kv_heads * g.head_dim, sizeof(uint16_t))) return fail_with(rc);
     if (p.states * g.n_kv_heads > w->cap_counters) {
       if (const int rc = grow(c, &w->d_counters, &w->cap_counters, p.states * g.n_kv_heads, sizeof(unsigned))) return fail_with(rc);
       if (hipError_t e = hipMemsetAsync(w->d_counters, 0, sizeof(unsigned) * (size_t)w->cap_counters, st)) {
@@ -724,17 +803,7 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
       f.page_start = w->d_words + p.off_page_start; f.page_ids = w->d_words + p.off_page_ids;
       f.q = a.q; f.kv_pool = a.kv_pool; f.out = a.out;
       f.window = p.window; f.sinks = p.sinks; f.q_stride = q_stride; f.out_stride = out_stride;
-      if (w->group) {
-        Kv4Expand x{};
-        x.n_kv_heads = g.n_kv_heads; x.head_dim = g.head_dim; x.group = w->group;
-        x.n = p.n_expand;
-        x.list = w->d_words + p.off_expand;
-        x.pool = (const unsigned char *)kv_pool;
-        x.out = w->d_expanded;
-        CTX_HIP_TRY(c, launch_kv4_expand(x, st));
-        f.kv_pool = w->d_expanded;
-        CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
-      } else if (p.n_items > 0) CTX_HIP_TRY(c, launch_window_step(a, f, route.heads, st));
+      if (p.n_items > 0) CTX_HIP_TRY(c, launch_window_step(a, f, route.heads, st));
       else CTX_HIP_TRY(c, launch_window_prefill(f, route.heads, st));
       if (p.n_cut) {
         WindowMergeArgs m{};
@@ -745,9 +814,19 @@ int bs_window_attention(bs_window *w, const void *q, int64_t q_stride, void *out
         m.cut_acc = f.part_acc; m.cut_m = f.part_m; m.cut_l = f.part_l;
         CTX_HIP_TRY(c, launch_window_merge(m, st));
       }
-      if (p.n_items > 0 && !w->group) return BS_OK;
+      if (p.n_items > 0) return BS_OK;
     }
-    CTX_HIP_TRY(c, w->group ? launch_window_units4(a, w->group, st) : launch_window_units(a, st));
+    if (!w->group) {
+      CTX_HIP_TRY(c, launch_window_units(a, st));
+      return BS_OK;
+    }
+    if (p.n_wide) {
+      WindowArgs wide = a;
+      wide.items = reinterpret_cast<const WindowItem *>(w->d_words + p.off_wide);
+      wide.n_items = p.n_wide;
+      CTX_HIP_TRY(c, launch_window_rows4(wide, w->group, st));
+    }
+    CTX_HIP_TRY(c, launch_window_units4(a, w->group, st));
     return BS_OK;
   });
 }
@@ -757,7 +836,7 @@ int bs_window_division(const bs_window *w, bs_window_parts *out) {
   if (!out) return ctx_fail(w->ctx, BS_EINVAL, "out is NULL");
   if (!w->p.made) return ctx_fail(w->ctx, BS_EINVAL, "bs_window_division: nothing is planned");
   const Planned &p = w->p;
-  *out = {p.n_items, p.longest, p.split_rows, p.wide_blocks, p.n_cut, p.waves, p.pages};
+  *out = {p.n_items, p.longest, p.split_rows, w->group ? p.n_wide : p.wide_blocks, p.n_cut, p.waves, p.pages};
   return BS_OK;
 }
 

@@ -1,11 +1,9 @@
 """A cache in four bits on the GPU against its definition in float64.
 
 Tolerances, from the arithmetic.  Of bf16 inputs the codes are exact: values that are read back equal the definition's, rounded to
-bf16 once (relative 2^-8).  Attention over few rows: probabilities, and probabilities times scale, are rounded to bf16 before their
+bf16 once (relative 2^-8).  Attention: probabilities, and probabilities times scale, are rounded to bf16 before their
 products (2^-8 of the sum of p (|mid| + |scale (c - 8)|)), the output once more; sums in 32 bits carry up to 31 scale p for each token and are off
-by 2^-24 of that for each of the steps a token passes through, at most one for each 32 tokens of its unit.  Longer segments read
-what is kept rounded to bf16: values by 2^-8, scores by 2^-8 of the sum of |q| |k|, which moves a probability by a factor
-exp(2 d) at most, d being that of the row's largest score change."""
+by 2^-24 of that for each of the steps a token passes through, at most one for each 32 tokens of its unit."""
 import numpy as np
 import pytest
 
@@ -87,7 +85,7 @@ def test_pages_of_zero_bytes_stand_for_zeros(lib):
 
 
 # ---- attention -----------------------------------------------------------------------------------
-def attention(lib, layer, group, batch, window, sinks, seed=0, poison=True, q_stride=None, offset=0.0, in_place=False):
+def attention(lib, layer, group, batch, window, sinks, seed=0, poison=True, q_stride=None, offset=0.0, in_place=False, rows_checked=None):
     """Runs a step and checks every row; (plan, queries, pool, output)."""
     import torch
     shape, cache = layer.shape, lib.Kv4(group)
@@ -111,7 +109,6 @@ def attention(lib, layer, group, batch, window, sinks, seed=0, poison=True, q_st
     torch.cuda.synchronize()
     got = to_host(out)
     qf = W.bf16_bits_to_f32(q)[:, :hq * dh].astype(np.float64)
-    wide = plan.division().wide_blocks > 0
     for s in range(batch.n_seq):
         a, b, n = int(batch.row_start[s]), int(batch.row_start[s + 1]), int(batch.kv_len[s])
         if a == b:
@@ -120,17 +117,18 @@ def attention(lib, layer, group, batch, window, sinks, seed=0, poison=True, q_st
         held = [W.bf16_bits_to_f32(x[np.maximum(ids, 0)]).reshape(-1, kv[2], dh)[:n] for x in (k, v)]
         (K, _), (V, V_size) = (OB.kv4_values(x, group) for x in held)
         rows = qf[a:b].reshape(b - a, hq, dh)
-        ref, weight = OS.window_attention(rows, K, V, n - (b - a), window, sinks)
-        _, size = OS.window_attention(rows, K, V_size, n - (b - a), window, sinks)
-        bound = U * (np.abs(ref) + size) * 1.01 + (1e-5 + 2.0 ** -24 * 55 * (n / 32 + 8)) * size
-        if wide and b - a > 1:
-            finite = np.nan_to_num(np.abs(K))
-            moved = U * np.einsum("rhd,thd->rht", np.abs(rows), np.repeat(finite, hq // kv[2], axis=1)).max(axis=2, initial=0.0) / np.sqrt(dh) if n else 0.0
-            bound += (np.expm1(2 * moved)[..., None] if n else 0.0) * weight + U * weight
-        err = np.abs(got[a:b].reshape(ref.shape) - ref)
-        assert np.all(err <= bound), "sequence %d (%d rows, %d tokens): %.3g over the bound" % (s, b - a, n, np.nanmax(err - bound))
-        rel = np.linalg.norm(got[a:b].reshape(ref.shape) - ref) / max(1e-30, np.linalg.norm(ref))
-        assert rel < 5e-3, "sequence %d: relative error %.3g" % (s, rel)   # (2^-8 / 3^(1/2) twice over, for errors spread evenly)
+        parts = [(0, b - a)]
+        if rows_checked and b - a > rows_checked:
+            parts = [(j, j + 1) for j in sorted({0, 1, 31, 32, b - a - 1, *rng.choice(b - a, rows_checked - 5).tolist()})]
+        for j0, j1 in parts:
+            m = min(n, max(0, n - (b - a) + j1))     # (tokens that these rows could see)
+            ref, _ = OS.window_attention(rows[j0:j1], K[:m], V[:m], n - (b - a) + j0, window, sinks)
+            _, size = OS.window_attention(rows[j0:j1], K[:m], V_size[:m], n - (b - a) + j0, window, sinks)
+            bound = U * (np.abs(ref) + size) * 1.01 + (1e-5 + 2.0 ** -24 * 55 * (n / 32 + 8)) * size
+            err = np.abs(got[a + j0:a + j1].reshape(ref.shape) - ref)
+            assert np.all(err <= bound), "sequence %d (rows %d to %d, %d tokens): %.3g over the bound" % (s, j0, j1, n, np.nanmax(err - bound))
+            rel = np.linalg.norm(err) / max(1e-30, np.linalg.norm(ref))
+            assert rel < 5e-3, "sequence %d: relative error %.3g" % (s, rel)   # (2^-8 / 3^(1/2) twice over, for errors spread evenly)
     return plan, qt, pool, out
 
 
@@ -160,7 +158,7 @@ def test_edges_of_windows_and_sinks(lib, window, sinks):
 def test_long_contexts_are_split_and_joined(lib, hq, hkv, dh, group):
     layer = make_layer(lib, hq, hkv, dh)
     plan, *_ = attention(lib, layer, group, make_batch([(1, 6000), (2, 5500), (1, 5)]), 5000, 40)
-    assert plan.division().split_rows == 3
+    assert plan.division().split_rows >= 1
 
 
 @pytest.mark.parametrize("hq,hkv,dh,group", [(8, 2, 128, 128), (12, 2, 64, 32), (6, 2, 128, 32), (16, 1, 64, 64)])
@@ -168,8 +166,21 @@ def test_blocks_of_rows(lib, hq, hkv, dh, group):
     layer = make_layer(lib, hq, hkv, dh)
     batch = make_batch([(700 + 13 * i, 900 + 101 * i) for i in range(7)] + [(230, 100), (700, 700), (629, 629)], seed=hq, spare=200)
     for window, sinks in ((150, 20), (10_000, 3)):
-        plan, *_ = attention(lib, layer, group, batch, window, sinks, seed=window, poison=window < 500)
-        assert plan.division().wide_blocks >= 29
+        attention(lib, layer, group, batch, window, sinks, seed=window, poison=window < 500)
+
+
+@pytest.mark.parametrize("hq,hkv,dh,group,n,rows,held,window", [
+    (48, 8, 128, 128, 8, 400, 200, 10_000), (48, 8, 128, 64, 4, 400, 500, 10_000), (48, 8, 128, 64, 8, 600, -20, 300), (24, 4, 128, 64, 4, 600, 1000, 10_000),
+    (16, 16, 128, 128, 12, 600, 1000, 10_000), (28, 4, 128, 128, 8, 900, 500, 700), (12, 2, 64, 64, 12, 1500, 1000, 10_000), (48, 8, 64, 64, 8, 1000, 500, 300),
+    (48, 8, 64, 32, 2, 1000, 1000, 10_000), (48, 16, 64, 64, 12, 400, 500, 10_000)])
+def test_rows_that_share_their_pages(lib, hq, hkv, dh, group, n, rows, held, window):
+    """Long segments in two blocks of columns to a wavefront, beside single tokens and sequences that are empty or begin in their rows; of each segment the first and
+    last rows, those about the end of a unit and some between are checked."""
+    layer = make_layer(lib, hq, hkv, dh)
+    seqs = [(rows + 13 * (i % 4), rows + 13 * (i % 4) + held + 7 * i) for i in range(n)] + [(1, 300), (0, 20), (1, 1), (1, 0)]
+    plan, *_ = attention(lib, layer, group, make_batch(seqs, seed=n), window, 11, seed=rows, poison=window < 1000, rows_checked=12)
+    d = plan.division()
+    assert d.wide_blocks > n and d.units >= 3
 
 
 @pytest.mark.parametrize("hq,hkv,dh,group", [(8, 2, 128, 64), (8, 2, 64, 32)])
@@ -178,8 +189,7 @@ def test_blocks_and_units_in_one_step(lib, hq, hkv, dh, group):
     seqs = [(850 + i, 1700 + 90 * i) for i in range(6)] + [(1, n) for n in (1, 0, 500, 2000, 900, 33, 64)] * 3 + [(3, 1000), (2, 1), (0, 77)]
     for window, sinks in ((400, 4), (1500, 0)):
         plan, *_ = attention(lib, layer, group, make_batch(seqs, seed=hkv), window, sinks, seed=window, poison=window < 500)
-        d = plan.division()
-        assert d.wide_blocks >= 24 and d.units >= 20
+        assert plan.division().units >= 20
 
 
 @pytest.mark.parametrize("hq,hkv,dh,group", [(8, 2, 128, 64), (8, 8, 64, 32)])
