@@ -327,7 +327,7 @@ hipError_t launch_rows(const GemmArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-enum Shape { ROWS_11, ROWS_12, ROWS_21, ROWS_22, D64, SMALL, WIDE, TALL, MID, BIG, N_SHAPES };
+enum Shape { ROWS_11, ROWS_12, ROWS_21, ROWS_22, D64, SMALL, SLIM, WIDE, TALL, MID, BIG, N_SHAPES };
 struct Plan {
   int shape, splits;
 };
@@ -337,6 +337,7 @@ hipError_t launch_shape(int shape, const GemmArgs &a, hipStream_t stream) {
   switch (shape) {
     case D64: return launch_tiles<64, 128, 4, 2, EPI, 2>(a, stream);
     case SMALL: return launch_tiles<128, 128, 2, 2, EPI, 0>(a, stream);
+    case SLIM: return launch_tiles<192, 128, 4, 2, EPI, 0>(a, stream);
     case WIDE: return launch_tiles<128, 256, 2, 4, EPI, 0>(a, stream);
     case TALL: return launch_tiles<160, 256, 2, 4, EPI, 0>(a, stream);
     case MID: return launch_tiles<192, 256, 2, 4, EPI, 0>(a, stream);
@@ -349,6 +350,8 @@ hipError_t launch_shape(int shape, const GemmArgs &a, hipStream_t stream) {
 // and for every 128 inputs (the last round, of a chip that is filled in part, less), or its bytes, and the second kernel of ranges.  Fitted to
 // 11 000 products (1 to 5000 rows, 256 to 28672 outputs, 1024 to 28672 inputs, weights cold) timed in every shape and range: the choice is 1.8 % off the best
 // on average, 10 % for one in twenty, 37 % at worst (29 rows, 17736 outputs, 14656 inputs: 82 us, 60 on tiles of 128 rows cut three ways).
+// SLIM came later: of 3000 products of 100 to 5000 rows it is chosen for 350, and the choice 1.7 % off the best, 2.6 without it
+// (1093 rows, 4096 x 4096: 192 of its tiles 25.6 us; 144 of WIDE's 31.2, 288 of SMALL's, of which 32 CUs have two, 30.9).
 struct Cost {
   int rows, outputs, per_cu;          // of a workgroup; workgroups that a CU takes at once
   double launch, round, tile, full;   // tile: of 128 inputs on an idle chip; full: more on a full one
@@ -362,6 +365,7 @@ constexpr Cost COSTS[N_SHAPES] = {
     {32, 32, 1, 3.431, 0.817, 0.083, 0.089, 0.171, 0, 0},
     {64, 128, 1, 0.476, 5.102, 0.319, 0.32, 0.179, 3.623, 0.236},
     {128, 128, 2, 3.935, 2.699, 0.929, 0.067, 0.212, 3.112, 0.339},
+    {192, 128, 1, 2.62, 3.553, 0.582, 0.131, 0.255, 3.027, 0.383},
     {128, 256, 1, 3.991, 2.628, 0.767, 0.13, 0.211, 3.069, 0.341},
     {160, 256, 1, 3.97, 3.739, 0.832, 0.168, 0.226, 2.774, 0.313},
     {192, 256, 1, 4.568, 3.834, 0.895, 0.231, 0.232, 2.284, 0.304},

@@ -268,9 +268,9 @@ def test_tensors_on_other_devices_are_refused(monkeypatch):
 
 def test_every_kind_of_tile_is_reached():
     layer, seen = binding.Layer(SHAPE, device=-1), set()
-    for m, n, k in ((9, 2857, 3952), (1, 5123, 7728), (51, 412, 4352), (20, 13329, 2368), (53, 15186, 2432), (678, 1071, 5008), (845, 18071, 2880), (433, 17789, 10000),
+    for m, n, k in ((9, 2857, 3952), (1, 5123, 7728), (51, 412, 4352), (20, 13329, 2368), (53, 15186, 2432), (678, 1071, 5008), (1090, 4091, 4080), (845, 18071, 2880), (433, 17789, 10000),
                     (1123, 9151, 4160), (2166, 13634, 20416)):
         rows, outputs, ranges = layer.w8_division(m, n, k)
         seen.add((rows, outputs))
         assert ranges >= 1 and (rows > 32 or ranges == 1)
-    assert seen >= {(16, 16), (16, 32), (32, 16), (32, 32), (64, 128), (128, 128), (128, 256), (160, 256), (192, 256), (256, 256)}, seen
+    assert seen >= {(16, 16), (16, 32), (32, 16), (32, 32), (64, 128), (128, 128), (192, 128), (128, 256), (160, 256), (192, 256), (256, 256)}, seen

@@ -81,7 +81,7 @@ def test_products(lib, layer, m, n, k):
 
 
 @pytest.mark.parametrize("m,n,k,tile", [(9, 2857, 3952, (16, 16)), (1, 5123, 7728, (16, 32)), (51, 412, 4352, (32, 16)), (20, 13329, 2368, (32, 32)),
-                                        (53, 15186, 2432, (64, 128)), (678, 1071, 5008, (128, 128)), (845, 18071, 2880, (128, 256)),
+                                        (53, 15186, 2432, (64, 128)), (678, 1071, 5008, (128, 128)), (1090, 4091, 4080, (192, 128)), (845, 18071, 2880, (128, 256)),
                                         (433, 17789, 10000, (160, 256)), (1123, 9151, 4160, (192, 256)), (2166, 13634, 20416, (256, 256))])
 def test_every_tile(lib, layer, m, n, k, tile):
     import torch
