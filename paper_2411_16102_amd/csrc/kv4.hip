@@ -241,7 +241,8 @@ int convert(bs_ctx *c, const char *what, const void *k, const void *v, const voi
   if (view.device == BS_DEVICE_NONE) return ctx_fail(c, BS_EINVAL, "host-only context");
   const int hkv = view.cfg->n_kv_heads, dh = view.cfg->head_dim;
   if (!kv4_shape(dh, group)) return ctx_fail(c, BS_EINVAL, "%s: groups of %d channels of %d are not supported", what, group, dh);
-  if (n_pages < 0 || n_pages * hkv > 0x7fffffff || n_pages > 0x7fffffff) return ctx_fail(c, BS_EINVAL, "%s: n_pages=%lld out of range", what, (long long)n_pages);
+  // (a launch has less than 2^32 threads)
+  if (n_pages < 0 || n_pages > 0xffffff || n_pages * hkv > 0xffffff) return ctx_fail(c, BS_EINVAL, "%s: n_pages=%lld out of range", what, (long long)n_pages);
   if (n_pages > 0 && (!k || !v || !pool || ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(pool)) & 15)))
     return ctx_fail(c, BS_EINVAL, "%s: a pointer is NULL or not 16-byte aligned", what);
   CTX_HIP_TRY(c, hipSetDevice(view.device));

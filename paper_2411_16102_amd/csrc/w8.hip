@@ -104,12 +104,24 @@ __global__ __launch_bounds__(T) void w8_quantize_kernel(const QuantArgs a) {
   for (int at = (QUANT_KEPT * T + (int)threadIdx.x) * 8; at < a.k; at += T * 8) put(attn_dev::ld16(x + at), at);
 }
 
+constexpr int MOST_LAUNCH = 1 << 23;  // rows of a launch
 hipError_t launch_quantize(const QuantArgs &a, hipStream_t stream) {
   if (a.m <= 0) return hipSuccess;
   // (few long rows: more threads ask at once, 33 rows of 28672 10.3 -> 5 us)
-  if (a.k > 8192 && a.m < 1024) hipLaunchKernelGGL(w8_quantize_kernel<1024>, dim3(a.m), dim3(1024), 0, stream, a);
-  else hipLaunchKernelGGL(w8_quantize_kernel<256>, dim3(a.m), dim3(256), 0, stream, a);
-  return hipGetLastError();
+  if (a.k > 8192 && a.m < 1024) {
+    hipLaunchKernelGGL(w8_quantize_kernel<1024>, dim3(a.m), dim3(1024), 0, stream, a);
+    return hipGetLastError();
+  }
+  for (int m0 = 0; m0 < a.m; m0 += MOST_LAUNCH) {  // (a launch has less than 2^32 threads)
+    QuantArgs part = a;
+    part.x += (int64_t)m0 * a.x_stride;
+    part.q += (int64_t)m0 * a.k;
+    part.scale += m0;
+    part.m = std::min(MOST_LAUNCH, a.m - m0);
+    hipLaunchKernelGGL(w8_quantize_kernel<256>, dim3(part.m), dim3(256), 0, stream, part);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 // ------------------------------------------------------------------------------
@@ -543,13 +555,17 @@ int bs_w8_linear_rows(bs_ctx *c, const void *x, int64_t x_stride, const void *we
     if (m == 0 || n == 0) return BS_OK;
     if (!x || x_stride < k || x_stride % 8 || !aligned16(x))
       return ctx_fail(c, BS_EINVAL, "bs_w8_linear_rows: rows of %lld elements at a stride of %lld (16-byte aligned, the stride a multiple of 8)", (long long)k, (long long)x_stride);
-    if (few_rows(m, k) && n * k <= MOST_BYTES) {
-      FewArgs f{};
-      f.g = product_args(c, nullptr, nullptr, weight, weight_scales, (int)m, (int)n, k, y, y_stride);
-      f.x = (const uint16_t *)x;
-      f.x_stride = x_stride;
+    if (few_rows(m, k)) {
       CTX_HIP_TRY(c, hipSetDevice(ctx_view(c).device));
-      CTX_HIP_TRY(c, launch_few_rows(f, few_blocks(n, k, f.g.n_cu), (hipStream_t)stream));
+      const int64_t most = MOST_BYTES / k / 256 * 256;
+      for (int64_t n0 = 0; n0 < n; n0 += most) {
+        const int64_t n1 = std::min(most, n - n0);
+        FewArgs f{};
+        f.g = product_args(c, nullptr, nullptr, (const int8_t *)weight + n0 * k, weight_scales + n0, (int)m, (int)n1, k, (uint16_t *)y + n0, y_stride);
+        f.x = (const uint16_t *)x;
+        f.x_stride = x_stride;
+        CTX_HIP_TRY(c, launch_few_rows(f, few_blocks(n1, k, f.g.n_cu), (hipStream_t)stream));
+      }
       return BS_OK;
     }
     const int64_t bytes = bs_w8_scratch_bytes(m, k);

@@ -84,6 +84,16 @@ def test_pages_of_zero_bytes_stand_for_zeros(lib):
     assert tuple(k.shape) == (0, 16, 2, 64) and layer.kv4_pack(k, v, cache).numel() == 0
 
 
+def test_more_pages_than_a_launch_has_are_refused(lib):
+    import ctypes as C
+    import torch
+    layer = make_layer(lib, 8, 2, 64)
+    t = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    for f in (layer.lib.bs_kv4_pack, layer.lib.bs_kv4_unpack):
+        for n in (1 << 24, 1 << 23, 1 << 40, -1):     # (times two heads)
+            assert f(layer.h, *[C.c_void_p(t.data_ptr())] * 3, n, 32, None) < 0 and "out of range" in layer.last_error()
+
+
 # ---- attention -----------------------------------------------------------------------------------
 def attention(lib, layer, group, batch, window, sinks, seed=0, poison=True, q_stride=None, offset=0.0, in_place=False, rows_checked=None):
     """Runs a step and checks every row; (plan, queries, pool, output)."""
@@ -214,6 +224,31 @@ def test_pages_that_sequences_share(lib):
     for t in table[1:]:
         t[:5] = table[0][:5]
     attention(lib, layer, 64, batch, 1000, 0)
+
+
+def test_a_pool_of_more_than_four_gigabytes(lib):
+    # the same pages further back: the same results, and new tokens in the same places of them
+    import torch
+    layer, cache = make_layer(lib, 32, 8, 128), lib.Kv4(32)
+    size, far = layer.page_bytes(cache), 212_000
+    assert size * far > 1 << 32
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for seqs in ([(1, 700), (1, 33), (40, 90), (3, 3)], [(300, 2000), (280, 280)]):
+        batch = make_batch(seqs)
+        near_pool = torch.randint(0, 256, (batch.n_pages * size,), dtype=torch.uint8, device="cuda", generator=gen)
+        k, v = (torch.randn((batch.n_pages, 16, 8, 128), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(2))
+        near_pool.copy_(layer.kv4_pack(k, v, cache))
+        pool = torch.empty((far + batch.n_pages) * size, dtype=torch.uint8, device="cuda")
+        pool[far * size:] = near_pool
+        qkv = torch.randn((batch.n_rows, layer.shape.n_qkv), device="cuda", generator=gen).to(torch.bfloat16)
+        results = []
+        for at, where in ((0, near_pool), (far, pool)):
+            moved = make_batch(seqs)
+            moved.page_ids[:] = np.where(moved.page_ids >= 0, moved.page_ids + at, moved.page_ids)
+            plan = layer.window_plan(moved, 1000, 4, n_pages=where.numel() // size, cache=cache)
+            q = layer.rope_append(plan, qkv, where)
+            results.append((q, layer.window_attention(plan, q, where), where[at * size:]))
+        assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
 def test_a_step_repeats_itself_and_captured_steps_too(lib):

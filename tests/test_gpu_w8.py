@@ -123,6 +123,34 @@ def test_the_longest_sums(lib, layer):
         _check(layer.w8_linear(x[:m], weight), np.full((m, 40), -128.0 * k * 2.0 ** -20))
 
 
+def test_more_rows_than_a_launch_has(lib, layer):
+    import torch
+    m = (1 << 23) + 5
+    x = torch.zeros((m, 16), dtype=torch.bfloat16, device="cuda")
+    picked = torch.tensor([0, 1, (1 << 23) - 1, 1 << 23, m - 1], device="cuda")
+    x[picked, 3] = torch.tensor([127.0, 254.0, -63.5, 1.0, 508.0], dtype=torch.bfloat16, device="cuda")
+    rows = layer.w8_quantize(x)
+    assert rows.q[picked, 3].tolist() == [127, 127, -127, 127, 127] and int(rows.q.count_nonzero()) == 5
+    assert rows.scales[picked].tolist() == [1.0, 2.0, 0.5, float(np.float32(1) / np.float32(127)), 4.0]
+
+
+@pytest.mark.parametrize("m", [1, 6])
+def test_weights_beyond_four_gigabytes(lib, layer, m):
+    import torch
+    n, k = 150_100, 28_672
+    g = torch.Generator(device="cuda").manual_seed(m)
+    w = torch.randint(-128, 128, (n, k), dtype=torch.int8, device="cuda", generator=g)
+    s = 1e-3 * (0.5 + torch.rand(n, device="cuda", generator=g))
+    x = torch.randn((m, k), device="cuda", generator=g).to(torch.bfloat16)
+    y = layer.w8_linear(x, lib.W8Weight(w, s))
+    q, scale = OB.w8_rows(x.float().cpu().numpy())
+    edge = 0xFFFF0000 // k // 256 * 256     # (the first output that offsets of 32 bits do not reach)
+    at = torch.tensor([0, 1, edge - 1, edge, edge + 1, n - 1], device="cuda")
+    _check(y[:, at], _reference(q, scale, w[at].cpu().numpy(), s[at].cpu().numpy()))
+    other = torch.from_numpy(q).cuda().double() @ w[-3000:].double().t()
+    assert torch.isfinite(y.float()).all() and ((y[:, -3000:].double() != 0) == (other != 0)).all()
+
+
 def test_weights_of_rows(lib, layer):
     # a weight that was brought to integers like rows: the product is that of the integers
     rng = np.random.default_rng(1)
