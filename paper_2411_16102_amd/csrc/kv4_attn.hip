@@ -75,29 +75,185 @@ struct FourBits {
     }
   }
 
-  // pages [pg0, pg1) of the unit, at most 64, of KV heads kvh ..; pages that others read too (SHARED) stay in the caches
-  template <bool SHARED>
-  __device__ __forceinline__ void walk(const WindowArgs &a, const WindowItem &it, int kvh, int lane, int pg0, int pg1, Columns<DH> (&c)[BLOCKS]) {
+  // A pair of pages, places tb .. tb + 31 of n_pg pages: scores, probabilities and sums of all columns.  numbers: of this lane's eight tokens;
+  // keys(h, w), values(h, db): codes as bf16; then(): once numbers and keys are done with.
+  template <class Keys, class Values, class Then>
+  __device__ __forceinline__ void pair(const WindowArgs &a, int tb, int n_pg, int first, int last, int sinks, const int (&at)[BLOCKS], u32x4_t (&numbers)[NG],
+                                       Columns<DH> (&c)[BLOCKS], Keys &&keys, Values &&values, Then &&then) {
+    const float sc = a.s.scale_log2e;
+    const int u0 = tb + 8 * ((threadIdx.x & 63) >> 4), mine = (threadIdx.x & 15) / CPH;  // this lane's eight tokens; its column's head
+    // (Masks are for few pairs.  What passes through an empty asm stays in its branch: left alone, the compiler computes all of them for every pair.)
+    const bool whole = tb + 32 <= 16 * n_pg && tb + 31 <= first && (tb > last - a.window || tb + 32 <= sinks);
+    if (!whole) {  // wave-uniform: the numbers of tokens that no row sees (the codes of such tokens are numbers whatever their bits)
+      int u = u0;
+      asm volatile("" : "+v"(u));
+      const int end = min(16 * n_pg, last + 1), unseen = first - a.window + 1;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) numbers[g] = mask_between8(mask_tokens8(numbers[g], u, end), u, sinks, unseen);
+    }
+    float num[NG][8];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) num[g][r] = __uint_as_float(r & 1 ? numbers[g][r >> 1] & 0xFFFF0000u : numbers[g][r >> 1] << 16);
+      settled(num[g]);
+    }
+    // scores, some groups of channels at a time; four accumulators in turn at least: a product that goes on from the last one's result waits for it
+    constexpr int GS = BLOCKS == 1 && NG >= 2 ? NG : 1, TURNS = BLOCKS == 1 && GS == 1 ? 2 : 1;
+    float sv[BLOCKS][8];
+#pragma unroll
+    for (int g0 = 0; g0 < NG; g0 += GS) {
+      f32x4_t s[GS][TURNS][BLOCKS][2];
+#pragma unroll
+      for (int g = 0; g < GS; ++g)
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float from = -CENTRE * q_sum[b][g0 + g];
+            s[g][0][b][i] = f32x4_t{from, from, from, from};
+            if constexpr (TURNS == 2) s[g][1][b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          }
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n)
+#pragma unroll
+          for (int g = 0; g < GS; ++g)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int step = (g0 + g) * STEPS + n, w = i * KC + step;
+              const bf16x8_t codes = keys(h, w);
+#pragma unroll
+              for (int b = 0; b < BLOCKS; ++b) {
+                f32x4_t &to = s[g][(h * STEPS + n) % TURNS][b][i];
+                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, q[h + b][step], to, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0x7F6);  // (in this order; all but matrix instructions may move)
+              }
+            }
+#pragma unroll
+      for (int g = 0; g < GS; ++g)
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            float d = s[g][0][b][r >> 2][r & 3];
+            if constexpr (TURNS == 2) d += s[g][1][b][r >> 2][r & 3];
+            const float x = of_quad<0>(num[g0 + g][r]) * d;
+            sv[b][r] = add_of_quad<1>(g0 + g == 0 ? x : sv[b][r] + x, num[g0 + g][r], q_sum[b][g0 + g]);
+          }
+    }
+    then();
+    if (!whole) {
+      int from = u0;
+#pragma unroll
+      for (int b = 0; b < BLOCKS; ++b) {
+        float(&sb)[8] = sv[b];
+        asm volatile("" : "+v"(sb[0]), "+v"(sb[1]), "+v"(sb[2]), "+v"(sb[3]), "+v"(sb[4]), "+v"(sb[5]), "+v"(sb[6]), "+v"(sb[7]), "+v"(from));
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const int u = from + r;  // (one condition, selected by: see window_device.hpp)
+          const bool hidden = (u > at[b]) | ((u <= at[b] - a.window) & (u >= sinks)) | (u >= 16 * n_pg);
+          sb[r] = hidden ? -INFINITY : sb[r];
+        }
+      }
+    }
+    float mx[BLOCKS];
+    bool moves = false;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      const float(&sb)[8] = sv[b];
+      mx[b] = sc * fmaxf(fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])), fmaxf(fmaxf(sb[4], sb[5]), fmaxf(sb[6], sb[7])));
+      moves |= mx[b] > c[b].m + TAU;
+    }
+    if (__builtin_amdgcn_ballot_w64(moves) != 0) {  // (see TAU: the reference moves rarely)
+#pragma unroll
+      for (int b = 0; b < BLOCKS; ++b) {
+        mx[b] = fmaxf(mx[b], __shfl_xor(mx[b], 16, 64));
+        mx[b] = fmaxf(mx[b], __shfl_xor(mx[b], 32, 64));
+        const float m_new = fmaxf(c[b].m, mx[b]), alpha = fast_exp2(c[b].m - m_new);
+        c[b].m = m_new;
+        c[b].l *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) c[b].o[db] *= alpha;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          common[b][g] *= alpha;
+          mids[b][g] *= alpha;
+        }
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      float(&sb)[8] = sv[b];
+      float ps = 0.f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        sb[r] = fast_exp2(__builtin_fmaf(sb[r], sc, -c[b].m));
+        ps += sb[r];
+      }
+      c[b].l += ps;
+    }
+    u32x4_t px[BLOCKS];  // probabilities times scale
+    auto scaled = [&](int b, int g) __attribute__((always_inline)) {
+      const uint32_t less = 0xC1C0C1C0u;  // -24 twice
+      float x[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        x[r] = of_quad<2>(num[g][r]) * sv[b][r];
+        mids[b][g] = add_of_quad<3>(mids[b][g], num[g][r], sv[b][r]);
+      }
+      px[b] = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+      common[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4_t{less, less, less, less}), as_bf16x8(px[b]), common[b][g], 0, 0, 0);
+    };
+    if constexpr (HEADS == 1) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) scaled(b, g);
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+          const int db = g * PER + n;
+          const bf16x8_t codes = values(0, db);
+#pragma unroll
+          for (int b = 0; b < BLOCKS; ++b) c[b].o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, as_bf16x8(px[b]), c[b].o[db], 0, 0, 0);
+        }
+      }
+    } else {
+      u32x4_t all[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        scaled(0, g);
+        all[g] = px[0];
+      }
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          u32x4_t own;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) own[i] = mine == h ? all[db / PER][i] : 0u;
+          c[0].o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values(h, db), as_bf16x8(own), c[0].o[db], 0, 0, 0);
+        }
+    }
+  }
+
+  // one block of columns, pages [pg0, pg1) of the unit, at most 64, of KV heads kvh ..
+  __device__ __forceinline__ void walk(const WindowArgs &a, const WindowItem &it, int kvh, int lane, int pg0, int pg1, Columns<DH> (&c)[1]) {
     constexpr int KW = DH / 64, VW = DH / 64;  // 16-byte loads of a head's keys and of its values
     constexpr int HEAD = kv4_head_bytes(DH, GROUP);
     const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv;
     const int jq = lane & 15, g4 = lane >> 4, col = jq % CPH, mine = jq / CPH;
-    const float sc = a.s.scale_log2e;
     // places are counted from this wavefront's first page
     const int n_pg = pg1 - pg0, first = it.at - 16 * pg0, last = first + it.n_rows - 1, sinks = it.sinks - 16 * pg0;
-    int at[BLOCKS];
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) at[b] = first + (16 * b + col < it.n_rows * grp ? (16 * b + col) / grp : 0);
+    const int at[1] = {first + (col < it.n_rows * grp ? col / grp : 0)};
     const int my_page = a.item_pages[it.page_off + pg0 + min(lane, n_pg - 1)];  // lane i holds page i
     const unsigned char *pool = reinterpret_cast<const unsigned char *>(a.kv_pool) + (size_t)kvh * HEAD;
     const unsigned char *k_base = pool + 4 * kv4_keys_at(g4, jq & 7, 0, 0, DH), *v_base = pool + 4 * kv4_values_at(g4 & 1, jq, DH);
     const unsigned char *n_base = pool + (size_t)mine * HEAD + kv4_number_at(8 * (g4 & 1), jq & 3, 0, DH, GROUP);  // kind jq % 4 of this lane's eight tokens
     const uint32_t page_bytes = (uint32_t)hkv * (uint32_t)HEAD;
     u32x4_t k[HEADS][KW], v[HEADS][VW], numbers[NG];
-    auto ask = [](const unsigned char *p) __attribute__((always_inline)) {
-      if constexpr (SHARED) return *reinterpret_cast<const u32x4_t *>(p);
-      else return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
-    };
+    auto ask = [](const unsigned char *p) __attribute__((always_inline)) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p)); };
     // (past the end: the last page again, not used)
     auto page = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane(my_page, min(i, n_pg - 1)); };
     auto load_keys = [&](int pr) __attribute__((always_inline)) {
@@ -121,148 +277,85 @@ struct FourBits {
     load_keys(0);
     load_values(0);
     for (int pr = 0; 2 * pr < n_pg; ++pr) {
-      const int tb = 32 * pr, u0 = tb + 8 * g4;  // this lane's eight tokens
-      // (Masks are for few pairs.  What passes through an empty asm stays in its branch: left alone, the compiler computes all of them for every pair.)
-      const bool whole = tb + 32 <= 16 * n_pg && tb + 31 <= first && (tb > last - a.window || tb + 32 <= sinks);
-      if (!whole) {  // wave-uniform: the numbers of tokens that no row sees (the codes of such tokens are numbers whatever their bits)
-        int u = u0;
-        asm volatile("" : "+v"(u));
-        const int end = min(16 * n_pg, last + 1), unseen = first - a.window + 1;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) numbers[g] = mask_between8(mask_tokens8(numbers[g], u, end), u, sinks, unseen);
-      }
-      float num[NG][8];
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) num[g][r] = __uint_as_float(r & 1 ? numbers[g][r >> 1] & 0xFFFF0000u : numbers[g][r >> 1] << 16);
-        settled(num[g]);
-      }
-      // scores, some groups of channels at a time; four accumulators in turn at least: a product that goes on from the last one's result waits for it
-      constexpr int GS = BLOCKS == 1 && NG >= 2 ? NG : 1, TURNS = BLOCKS == 1 && GS == 1 ? 2 : 1;
-      float sv[BLOCKS][8];
-#pragma unroll
-      for (int g0 = 0; g0 < NG; g0 += GS) {
-        f32x4_t s[GS][TURNS][BLOCKS][2];
-#pragma unroll
-        for (int g = 0; g < GS; ++g)
-#pragma unroll
-          for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float from = -CENTRE * q_sum[b][g0 + g];
-              s[g][0][b][i] = f32x4_t{from, from, from, from};
-              if constexpr (TURNS == 2) s[g][1][b][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            }
-#pragma unroll
-        for (int h = 0; h < HEADS; ++h)
-#pragma unroll
-          for (int n = 0; n < STEPS; ++n)
-#pragma unroll
-            for (int g = 0; g < GS; ++g)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int step = (g0 + g) * STEPS + n, w = i * KC + step;
-                const bf16x8_t codes = as_bf16x8(unpack(k[h][w >> 2][w & 3]));
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                  f32x4_t &to = s[g][(h * STEPS + n) % TURNS][b][i];
-                  to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, q[h + b][step], to, 0, 0, 0);
-                  __builtin_amdgcn_sched_barrier(0x7F6);  // (in this order; all but matrix instructions may move)
-                }
-              }
-#pragma unroll
-        for (int g = 0; g < GS; ++g)
-#pragma unroll
-          for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-              float d = s[g][0][b][r >> 2][r & 3];
-              if constexpr (TURNS == 2) d += s[g][1][b][r >> 2][r & 3];
-              const float x = of_quad<0>(num[g0 + g][r]) * d;
-              sv[b][r] = add_of_quad<1>(g0 + g == 0 ? x : sv[b][r] + x, num[g0 + g][r], q_sum[b][g0 + g]);
-            }
-      }
-      load_keys(pr + 1);
-#pragma unroll
-      for (int b = 0; b < BLOCKS; ++b) {
-        float(&sb)[8] = sv[b];
-        if (!whole) {
-          int from = u0;
-          asm volatile("" : "+v"(sb[0]), "+v"(sb[1]), "+v"(sb[2]), "+v"(sb[3]), "+v"(sb[4]), "+v"(sb[5]), "+v"(sb[6]), "+v"(sb[7]), "+v"(from));
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            const int u = from + r;  // (one condition, selected by: see window_device.hpp)
-            const bool hidden = (u > at[b]) | ((u <= at[b] - a.window) & (u >= sinks)) | (u >= 16 * n_pg);
-            sb[r] = hidden ? -INFINITY : sb[r];
-          }
-        }
-        float mx = sc * fmaxf(fmaxf(fmaxf(sb[0], sb[1]), fmaxf(sb[2], sb[3])), fmaxf(fmaxf(sb[4], sb[5]), fmaxf(sb[6], sb[7])));
-        if (__builtin_amdgcn_ballot_w64(mx > c[b].m + TAU) != 0) {  // (see TAU: the reference moves rarely)
-          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-          const float m_new = fmaxf(c[b].m, mx), alpha = fast_exp2(c[b].m - m_new);
-          c[b].m = m_new;
-          c[b].l *= alpha;
-#pragma unroll
-          for (int db = 0; db < DB; ++db) c[b].o[db] *= alpha;
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            common[b][g] *= alpha;
-            mids[b][g] *= alpha;
-          }
-        }
-        float ps = 0.f;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          sb[r] = fast_exp2(__builtin_fmaf(sb[r], sc, -c[b].m));
-          ps += sb[r];
-        }
-        c[b].l += ps;
-      }
-      u32x4_t px[BLOCKS];  // probabilities times scale
-      auto scaled = [&](int b, int g) __attribute__((always_inline)) {
-        const uint32_t less = 0xC1C0C1C0u;  // -24 twice
-        float x[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          x[r] = of_quad<2>(num[g][r]) * sv[b][r];
-          mids[b][g] = add_of_quad<3>(mids[b][g], num[g][r], sv[b][r]);
-        }
-        px[b] = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-        common[b][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4_t{less, less, less, less}), as_bf16x8(px[b]), common[b][g], 0, 0, 0);
-      };
-      if constexpr (HEADS == 1) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-#pragma unroll
-          for (int b = 0; b < BLOCKS; ++b) scaled(b, g);
-#pragma unroll
-          for (int n = 0; n < PER; ++n) {
-            const int db = g * PER + n;
-            const bf16x8_t codes = as_bf16x8(unpack(v[0][db >> 2][db & 3]));
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) c[b].o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, as_bf16x8(px[b]), c[b].o[db], 0, 0, 0);
-          }
-        }
-      } else {
-        u32x4_t all[NG];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          scaled(0, g);
-          all[g] = px[0];
-        }
-#pragma unroll
-        for (int h = 0; h < HEADS; ++h)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            u32x4_t own;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) own[i] = mine == h ? all[db / PER][i] : 0u;
-            c[0].o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unpack(v[h][db >> 2][db & 3])), as_bf16x8(own), c[0].o[db], 0, 0, 0);
-          }
-      }
+      pair(
+          a, 32 * pr, n_pg, first, last, sinks, at, numbers, c, [&](int h, int w) __attribute__((always_inline)) { return as_bf16x8(unpack(k[h][w >> 2][w & 3])); },
+          [&](int h, int db) __attribute__((always_inline)) { return as_bf16x8(unpack(v[h][db >> 2][db & 3])); }, [&]() __attribute__((always_inline)) { load_keys(pr + 1); });
       load_values(pr + 1);
+    }
+  }
+
+  // Pages [pg0, pg1) of an item, at most 64, of KV head kvh, for the four wavefronts of a workgroup, whose rows are it's from row `from` on, n_rows of them.  Each brings a
+  // quarter of the codes of the next pair to LDS as bf16, in the order in which products take them: [keys, values][operand][lane], twice.
+  __device__ __forceinline__ void walk_shared(const WindowArgs &a, const WindowItem &it, int from, int n_rows, int kvh, int lane, int wave, int pg0, int pg1, u32x4_t *lds,
+                                              Columns<DH> (&c)[BLOCKS]) {
+    constexpr int HEAD = kv4_head_bytes(DH, GROUP), W = DH / 32, OPERANDS = DH / 16;  // W: words of a thread; operands of keys, of values
+    const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv;
+    const int jq = lane & 15, g4 = lane >> 4;
+    const int n_pg = pg1 - pg0, first = it.at + from - 16 * pg0, last = first + n_rows - 1, sinks = it.sinks - 16 * pg0;
+    int at[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) at[b] = first + (16 * b + jq < n_rows * grp ? (16 * b + jq) / grp : 0);
+    const int my_page = a.item_pages[it.page_off + pg0 + min(lane, n_pg - 1)];  // lane i holds page i
+    const unsigned char *pool = reinterpret_cast<const unsigned char *>(a.kv_pool) + (size_t)kvh * HEAD;
+    // wavefronts 0 and 1 take keys, 2 and 3 values: of the sixteen bytes of a lane's first load all, or all of its second; or a half each
+    const bool values = wave >= 2;
+    const int part = wave & 1, word0 = part * W;
+    const unsigned char *c_base = pool + 4 * (values ? kv4_values_at(g4 & 1, jq, DH) : kv4_keys_at(g4, jq & 7, 0, 0, DH)) + (DH == 128 ? 512 * part : 8 * part);
+    const unsigned char *n_base = pool + kv4_number_at(8 * (g4 & 1), jq & 3, 0, DH, GROUP);
+    const bool second = values ? g4 >= 2 : jq >= 8;  // of this lane's codes: of the pair's second page
+    const uint32_t page_bytes = (uint32_t)hkv * (uint32_t)HEAD;
+    uint32_t codes[W];
+    u32x4_t numbers[NG];
+    // (past the end: the last page again, not used)
+    auto page = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane(my_page, min(i, n_pg - 1)); };
+    auto load_codes = [&](int pr) __attribute__((always_inline)) {
+      const uint32_t p0 = page(2 * pr), p1 = page(2 * pr + 1);
+      const unsigned char *p = c_base + (uint64_t)(second ? p1 : p0) * page_bytes;
+      if constexpr (W == 4) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(p);
+#pragma unroll
+        for (int i = 0; i < W; ++i) codes[i] = x[i];
+      } else {
+        const u32x2_t x = *reinterpret_cast<const u32x2_t *>(p);
+#pragma unroll
+        for (int i = 0; i < W; ++i) codes[i] = x[i];
+      }
+    };
+    auto load_numbers = [&](int pr) __attribute__((always_inline)) {
+      const unsigned char *p = n_base + (uint64_t)(g4 < 2 ? page(2 * pr) : page(2 * pr + 1)) * page_bytes;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) numbers[g] = *reinterpret_cast<const u32x4_t *>(p + 64 * g);
+    };
+    auto put = [&](int pr) __attribute__((always_inline)) {
+      u32x4_t *to = lds + ((pr & 1) * 2 + values) * OPERANDS * 64 + word0 * 64 + lane;
+#pragma unroll
+      for (int i = 0; i < W; ++i) to[i * 64] = unpack(codes[i]);
+    };
+    auto meet = []() __attribute__((always_inline)) {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // (LDS alone: loads stay on their way)
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    load_codes(0);
+    load_numbers(0);
+    put(0);
+    load_codes(1);
+    meet();
+    for (int pr = 0; 2 * pr < n_pg; ++pr) {
+      put(pr + 1);
+      load_codes(pr + 2);
+      const int tb = 32 * pr;
+      const bool seen = n_rows > 0 && tb <= last && (tb + 31 > first - a.window || tb < sinks);  // wave-uniform
+      if (seen) {
+        const u32x4_t *own = lds + (pr & 1) * 2 * OPERANDS * 64 + lane;
+        pair(
+            a, tb, n_pg, first, last, sinks, at, numbers, c, [&](int, int w) __attribute__((always_inline)) { return as_bf16x8(own[w * 64]); },
+            [&](int, int db) __attribute__((always_inline)) { return as_bf16x8(own[(OPERANDS + db) * 64]); }, [&]() __attribute__((always_inline)) { load_numbers(pr + 1); });
+      } else {
+        load_numbers(pr + 1);
+      }
+      meet();  // the pair that was read may be overwritten, the next one is there
     }
   }
 
@@ -285,7 +378,7 @@ struct FourBitPages : FourBits<DH, GROUP, HEADS_, 1> {
   __device__ __forceinline__ explicit FourBitPages(const bf16x8_t (&qf)[DH / 32]) { this->begin(0, qf); }
   __device__ __forceinline__ void walk(const WindowArgs &a, const WindowItem &it, int kvh, int lane, int pg0, int pg1, const bf16x8_t (&)[DH / 32], Columns<DH> &c) {
     Columns<DH> one[1] = {c};
-    FourBits<DH, GROUP, HEADS_, 1>::template walk<false>(a, it, kvh, lane, pg0, pg1, one);
+    FourBits<DH, GROUP, HEADS_, 1>::walk(a, it, kvh, lane, pg0, pg1, one);
     c = one[0];
   }
   __device__ __forceinline__ void finish(Columns<DH> &c) { FourBits<DH, GROUP, HEADS_, 1>::finish(0, c); }
@@ -300,20 +393,21 @@ struct FourBitPages : FourBits<DH, GROUP, HEADS_, 1> {
 template <int DH, int GROUP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_rows4_kernel(const WindowArgs a) {
   const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int item = (int)(blockIdx.x / hkv) * 4 + wave, kvh = blockIdx.x % hkv;
-  if (item >= a.n_items) return;
-  const WindowItem it = a.items[item];
+  __shared__ u32x4_t lds[2 * 2 * (DH / 16) * 64];
+  const int kvh = blockIdx.x % hkv, rows = max(1, 16 * KV4_ROW_BLOCKS / grp), from = wave * rows;
+  const WindowItem it = a.items[blockIdx.x / hkv];
+  const int n_rows = max(0, min(rows, it.n_rows - from));
   FourBits<DH, GROUP, 1, KV4_ROW_BLOCKS> bits;
   Columns<DH> c[KV4_ROW_BLOCKS];
 #pragma unroll
   for (int b = 0; b < KV4_ROW_BLOCKS; ++b) {
     const int col = 16 * b + (lane & 15);
-    const bool ok = col < it.n_rows * grp;
+    const bool ok = col < n_rows * grp;
     bf16x8_t qf[DH / 32];
 #pragma unroll
     for (int i = 0; i < DH / 32; ++i) {
       u32x4_t v = {0u, 0u, 0u, 0u};
-      if (ok) v = ld16(a.q + (it.row0 + col / grp) * a.q_stride + (kvh * grp + col % grp) * DH + 32 * i + 8 * (lane >> 4));
+      if (ok) v = ld16(a.q + (it.row0 + from + col / grp) * a.q_stride + (kvh * grp + col % grp) * DH + 32 * i + 8 * (lane >> 4));
       qf[i] = as_bf16x8(v);
     }
     bits.begin(b, qf);
@@ -322,7 +416,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     c[b].m = NEG_BIG;
     c[b].l = 0.f;
   }
-  for (int pg = 0; pg < it.n_pages; pg += 64) bits.template walk<true>(a, it, kvh, lane, pg, min(pg + 64, it.n_pages), c);
+  for (int pg = 0; pg < it.n_pages; pg += 64) bits.walk_shared(a, it, from, n_rows, kvh, lane, wave, pg, min(pg + 64, it.n_pages), lds, c);
 #pragma unroll
   for (int b = 0; b < KV4_ROW_BLOCKS; ++b) {
     bits.finish(b, c[b]);
@@ -330,9 +424,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     const int col = 16 * b + (lane & 15);
-    if (col < it.n_rows * grp)
+    if (col < n_rows * grp)
 #pragma unroll
-      for (int db = 0; db < DH / 16; ++db) store_quad(a, it, kvh, col, DH, lane, db, c[b].o[db], l);
+      for (int db = 0; db < DH / 16; ++db) store_quad(a, it, kvh, from * grp + col, DH, lane, db, c[b].o[db], l);
   }
 }
 
@@ -363,7 +457,7 @@ hipError_t launch_units4(const WindowArgs &a, hipStream_t stream) {
 
 hipError_t launch_window_rows4(const WindowArgs &a, int group, hipStream_t stream) {
   if (a.n_items <= 0) return hipSuccess;
-  const dim3 grid((unsigned)((a.n_items + 3) / 4) * (unsigned)a.s.n_kv_heads), block(256);
+  const dim3 grid((unsigned)a.n_items * (unsigned)a.s.n_kv_heads), block(256);
   if (a.s.head_dim == 128 && group == 128) hipLaunchKernelGGL((window_rows4_kernel<128, 128>), grid, block, 0, stream, a);
   else if (a.s.head_dim == 128 && group == 64) hipLaunchKernelGGL((window_rows4_kernel<128, 64>), grid, block, 0, stream, a);
   else if (a.s.head_dim == 64 && group == 64) hipLaunchKernelGGL((window_rows4_kernel<64, 64>), grid, block, 0, stream, a);

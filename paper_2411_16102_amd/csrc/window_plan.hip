@@ -298,7 +298,7 @@ int add_units(bs_window *w, const bs_batch *b, const Division &div) {
   }
   // longest first: the short ones then fill the end of the launch
   std::stable_sort(w->items.begin(), w->items.end(), [](const auto &x, const auto &y) { return x.n_pages > y.n_pages; });
-  // wide units over a cache in four bits: rows next to one another stay next to one another in fours, the fours longest first
+  // wide units over a cache in four bits
   w->wide_items.clear();
   for (const bs_window::Rows &r : w->wide_rows) {
     const int r0 = b->row_start[r.seq], p0 = b->kv_len[r.seq] - (b->row_start[r.seq + 1] - r0) + r.first;
@@ -315,16 +315,7 @@ int add_units(bs_window *w, const bs_batch *b, const Division &div) {
     for (int i = 0; i < r.pages; ++i) w->item_pages.push_back(b->page_ids[b->page_start[r.seq] + seen.page(i)]);
     if (w->item_pages.size() > (size_t)MAX_LEN) return too_large(w);
   }
-  std::vector<std::pair<int, int>> fours;
-  for (int i = 0; i < (int)w->wide_items.size(); i += 4) fours.push_back({-w->wide_items[std::min(i + 3, (int)w->wide_items.size() - 1)].n_pages, i});
-  std::stable_sort(fours.begin(), fours.end(), [](const auto &x, const auto &y) { return x.first < y.first; });
-  std::vector<WindowItem> sorted;
-  // (the last four may be fewer: they stay at the end)
-  for (int pass = 0; pass < 2; ++pass)
-    for (const auto &f : fours)
-      if ((f.second + 4 > (int)w->wide_items.size()) == (pass == 1))
-        sorted.insert(sorted.end(), w->wide_items.begin() + f.second, w->wide_items.begin() + std::min(f.second + 4, (int)w->wide_items.size()));
-  w->wide_items.swap(sorted);
+  std::stable_sort(w->wide_items.begin(), w->wide_items.end(), [](const auto &x, const auto &y) { return x.n_pages > y.n_pages; });
   return BS_OK;
 }
 
@@ -336,7 +327,7 @@ struct Route {
 };
 Route route_of(const bs_layer_cfg &g) {
   const int grp = g.n_q_heads / g.n_kv_heads, heads = grp % 4 == 0 ? 4 : grp % 2 == 0 ? 2 : 1;
-  return {std::max(1, 16 / grp), heads, 64 * (4 / heads), std::max(1, 16 * KV4_ROW_BLOCKS / grp)};
+  return {std::max(1, 16 / grp), heads, 64 * (4 / heads), 4 * std::max(1, 16 * KV4_ROW_BLOCKS / grp)};
 }
 
 // The rows of a longer segment as blocks for wide workgroups; rows of blocks that stand wholly in front of their sequence see nothing:
@@ -646,7 +637,7 @@ int bs_window_plan(bs_window *w, const bs_batch *b, int64_t n_pages, int32_t win
     plan_appends(w, b);
     // (grids count units of a KV head, workgroups of some heads, and shares of the heads of a run)
     if ((int64_t)p.n_items * g.n_kv_heads > 0x7fffffff || (int64_t)p.n_work * g.n_q_heads > 0x7fffffff ||
-        (int64_t)p.n_rope * (g.n_kv_heads + 1) + 4096 > 0x7fffffff || ((int64_t)p.n_wide / 4 + 1) * g.n_kv_heads > 0x7fffffff)
+        (int64_t)p.n_rope * (g.n_kv_heads + 1) + 4096 > 0x7fffffff || (int64_t)p.n_wide * g.n_kv_heads > 0x7fffffff)
       return fail_with(too_large(w));
 
     for (int i = 0; n_axes > 0 && i < half; ++i) p.whole_axes = p.whole_axes && axis_of_pair[i] == axis_of_pair[i & ~7];
