@@ -38,7 +38,7 @@ int64_t bs_kv4_page_bytes(const bs_ctx *ctx, int32_t group);
  * that blendstep_stream.h says of them holds, but:
  *   - probabilities are rounded to bf16 after a multiplication with the scales of values
  *   - a query with an infinity gives NaN
- *   - the wide_blocks of bs_window_division are units of one KV head too, of twice the rows of a narrow unit, with all of their pages. */
+ *   - the wide_blocks of bs_window_division are units of one KV head too, of about eight times the rows of a narrow unit, with all of their pages. */
 int bs_window_cache(bs_window *w, int32_t bits, int32_t group);
 
 /* k, v: device bf16, token-major [n_pages][16][n_kv_heads][head_dim], 16-byte aligned; kv_pool: n_pages pages in four bits.  kv4_unpack gives what the

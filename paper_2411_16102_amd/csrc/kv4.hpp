@@ -44,8 +44,8 @@ hipError_t launch_kv4_unpack(const Kv4Pages &p, hipStream_t stream);
 // The narrow work of window attention over such a cache (a.kv_pool), and the wavefronts of it that the registers of a SIMD hold.
 constexpr int kv4_resident(int head_dim, int group, int heads) { return head_dim == 128 ? (heads == 2 || group == 32 ? 2 : 3) : heads == 2 ? 3 : 4; }
 hipError_t launch_window_units4(const WindowArgs &a, int group, hipStream_t stream);
-// Rows of longer segments: items of up to KV4_ROW_BLOCKS blocks of sixteen columns with all of their pages.  Four groups to a head leave no
-// registers for two blocks (62 spilled): at 1.3 to 2.7 times the time of narrow work from the largest to the smallest sizes, these stay narrow work.
+// Rows of longer segments: items of up to KV4_ROW_BLOCKS blocks of sixteen columns for each of four wavefronts, with all of their pages.  Four groups to a head
+// leave no registers for two blocks (62 spilled): at 1.3 to 2.7 times the time of narrow work from the largest to the smallest sizes, these stay narrow work.
 constexpr int KV4_ROW_BLOCKS = 2;
 inline bool kv4_has_rows(int head_dim, int group) { return head_dim / group <= 2; }
 hipError_t launch_window_rows4(const WindowArgs &a, int group, hipStream_t stream);

@@ -40,7 +40,8 @@ __device__ __forceinline__ void settled(float (&v)[8]) {
 // and in its probabilities.  A lane's numbers are those of its column's head: four lanes have the four kinds (scale and mid of keys, of values) of
 // a group in one load, and take them from one another.
 //
-// The rows of a longer segment share their pages too: BLOCKS blocks of sixteen columns to a wavefront, for which a code is brought to 16 + code once.
+// The rows of a longer segment share their pages too: BLOCKS blocks of sixteen columns to a wavefront, and four wavefronts for which a code is brought
+// to 16 + code once.
 template <int DH, int GROUP, int HEADS, int BLOCKS>
 struct FourBits {
   static_assert(HEADS == 1 || BLOCKS == 1, "columns of several heads, or several blocks of them");
@@ -384,12 +385,13 @@ struct FourBitPages : FourBits<DH, GROUP, HEADS_, 1> {
   __device__ __forceinline__ void finish(Columns<DH> &c) { FourBits<DH, GROUP, HEADS_, 1>::finish(0, c); }
 };
 
-// Rows of longer segments: a wavefront per (item, KV head), two blocks of columns, all of the pages that they see; the four of a workgroup take
-// items next to one another, which walk the same pages.  Bound by what a SIMD issues: for two blocks 323 vector operations and 34 matrix
-// instructions a pair of pages (128 channels in one group), 112 of them to bring codes to bf16 - one block has 210.  Six segments of about 700 rows behind
-// 1500 tokens, 8 KV heads with four queries each: 224 us, as narrow work 233.  Slower: three or four blocks with all registers, one wavefront a SIMD
-// (319 and 384 us); workgroups of one or two wavefronts (233); pages brought to fp16 and bf16 once for the kernel of longer segments of a cache in
-// bf16 took 199 us there, but with all batches of its kind 1.4 to 1.8 times the time of these, and a second copy of the pages.
+// Rows of longer segments: a workgroup per (item, KV head), two blocks of columns to a wavefront, all of the pages that the item's rows see.  Codes are
+// brought to bf16 once for the four, which takes 28 vector operations a pair of pages of each instead of 112; 16 reads of LDS give them back.  Bound by
+// what a SIMD issues and waits for: 230 vector operations and 34 matrix instructions a pair and wavefront (128 channels in one group), vector pipes 51 % busy over the
+// launch and matrix pipes 24 %, a fifth of it the last round.  Six segments of about 700 rows behind 1500 tokens, 8 KV heads with four queries each: 211 us, as narrow
+// work 230.  Slower: every wavefront its own codes (224; with three or four blocks and one wavefront a SIMD 319 and 384, with queries in LDS for three
+// wavefronts 217); pages brought to fp16 and bf16 once for the kernel of longer segments of a cache in bf16 took 199 us there, but with all batches of its kind 1.4 to 1.8 times the
+// time of these, and a second copy of the pages.
 template <int DH, int GROUP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_rows4_kernel(const WindowArgs a) {
   const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

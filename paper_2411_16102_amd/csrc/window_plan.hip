@@ -385,9 +385,9 @@ Cut cut_choice(const std::vector<bs_window::Work> &work, int wg_per_work, int dh
   return best;
 }
 
-// The microseconds that are expected of wide units over a cache in four bits, a tenth more: their expectation is the less certain one of the two.
-// Fitted to 13700 batches of 1 to 16 sequences of 5 to 3000 rows behind up to 8000 tokens, timed as narrow and as wide work: 8 % off on average,
-// and the shorter kind is chosen but for 0.4 % of the time, 11 % for one in a hundred.  (All of them as narrow work: 1 %; 28 % at the largest sizes.)
+// The microseconds that are expected of wide units over a cache in four bits: what all of them take of the chip's SIMDs, or the longest.
+// Fitted to 27 600 batches of 1 to 16 sequences of 5 to 3000 rows behind up to 8000 tokens, timed as narrow and as wide work: 6 % off on average,
+// and the kind that is chosen 0.23 % off the shorter, 7 % for one in a hundred.  (All of them as narrow work: 1.5 %; the largest 20 to 30 %.)
 double wide4_us(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g, int group, int n_cu) {
   if (rows.empty()) return 0.0;
   int64_t pages = 0;
@@ -396,8 +396,9 @@ double wide4_us(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g,
     pages += r.pages;
     longest = std::max(longest, r.pages);
   }
-  const double step = (g.head_dim == 128 ? 0.58 : 0.40) + 0.14 * (g.head_dim / group), per_simd = g.n_kv_heads / (4.0 * n_cu);
-  return 1.1 * (6.1 + step * (0.47 * (double)pages * per_simd + 0.56 * longest + 4.3 * (double)rows.size() * per_simd));
+  const double step = g.head_dim == 128 ? 1.58 + 0.197 * (128 / group) : 1.045 + 0.25 * (64 / group), per_simd = g.n_kv_heads / (4.0 * n_cu);
+  const double all = per_simd * (0.88 * (double)pages + 10.0 * (double)rows.size()), alone = 0.345 * longest;
+  return 6.6 + 1.05 * step * std::pow(std::pow(all, 3.6) + std::pow(alone, 3.6), 1.0 / 3.6);
 }
 
 void cut_blocks(bs_window *w, int most) {
