@@ -46,7 +46,12 @@ template <int DH, int GROUP, int HEADS, int BLOCKS>
 struct FourBits {
   static_assert(HEADS == 1 || BLOCKS == 1, "columns of several heads, or several blocks of them");
   static constexpr int CPH = 16 / HEADS, KC = DH / 32, DB = DH / 16, NG = DH / GROUP, STEPS = GROUP / 32, PER = GROUP / 16;
-  bf16x8_t q[HEADS * BLOCKS][KC];
+  // What brings a third wavefront of several blocks to a SIMD: queries in LDS, and, beside those of 128 channels, codes once instead of twice.
+  static constexpr bool Q_LDS = BLOCKS > 1 && ((DH == 128 && GROUP == 128) || (DH == 64 && GROUP == 32)), TWICE = !Q_LDS || DH == 64;
+  static constexpr int WAVES = DH == 128 && GROUP == 64 ? 2 : 3;  // of several blocks, on a SIMD
+  typedef __attribute__((address_space(3))) bf16x8_t Lds;
+  bf16x8_t q[Q_LDS ? 1 : HEADS * BLOCKS][KC];
+  Lds *q_lds;  // this lane's, [block][32 channels], 64 apart
   f32x4_t common[BLOCKS][NG];  // of all channels of a group
   float q_sum[BLOCKS][NG], mids[BLOCKS][NG];
   Unpack unpack;
@@ -59,7 +64,8 @@ struct FourBits {
       for (int i = 0; i < KC; ++i) {
         u32x4_t v = __builtin_bit_cast(u32x4_t, qf[i]);
         if (HEADS > 1 && mine != h) v = u32x4_t{0u, 0u, 0u, 0u};
-        q[h + b][i] = as_bf16x8(v);
+        if constexpr (Q_LDS) q_lds[(b * KC + i) * 64] = as_bf16x8(v);
+        else q[h + b][i] = as_bf16x8(v);
       }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -101,6 +107,8 @@ struct FourBits {
     }
     // scores, some groups of channels at a time; four accumulators in turn at least: a product that goes on from the last one's result waits for it
     constexpr int GS = BLOCKS == 1 && NG >= 2 ? NG : 1, TURNS = BLOCKS == 1 && GS == 1 ? 2 : 1;
+    const Lds *q_now = q_lds;
+    if constexpr (Q_LDS) asm volatile("" : "+v"(q_now));  // (read here every time)
     float sv[BLOCKS][8];
 #pragma unroll
     for (int g0 = 0; g0 < NG; g0 += GS) {
@@ -120,18 +128,25 @@ struct FourBits {
 #pragma unroll
         for (int n = 0; n < STEPS; ++n)
 #pragma unroll
-          for (int g = 0; g < GS; ++g)
+          for (int g = 0; g < GS; ++g) {
+            const int step = (g0 + g) * STEPS + n;
+            bf16x8_t qs[BLOCKS];
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+              if constexpr (Q_LDS) qs[b] = q_now[(b * KC + step) * 64];
+              else qs[b] = q[h + b][step];
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const int step = (g0 + g) * STEPS + n, w = i * KC + step;
-              const bf16x8_t codes = keys(h, w);
+              const bf16x8_t codes = keys(h, i * KC + step);
 #pragma unroll
               for (int b = 0; b < BLOCKS; ++b) {
                 f32x4_t &to = s[g][(h * STEPS + n) % TURNS][b][i];
-                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, q[h + b][step], to, 0, 0, 0);
+                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes, qs[b], to, 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0x7F6);  // (in this order; all but matrix instructions may move)
               }
             }
+          }
 #pragma unroll
       for (int g = 0; g < GS; ++g)
 #pragma unroll
@@ -286,7 +301,8 @@ struct FourBits {
   }
 
   // Pages [pg0, pg1) of an item, at most 64, of KV head kvh, for the four wavefronts of a workgroup, whose rows are it's from row `from` on, n_rows of them.  Each brings a
-  // quarter of the codes of the next pair to LDS as bf16, in the order in which products take them: [keys, values][operand][lane], twice.
+  // quarter of the codes of the next pair to LDS as bf16, in the order in which products take them: [keys, values][operand][lane], twice; or once,
+  // keys when all have read the last pair's and values when they have read those.
   __device__ __forceinline__ void walk_shared(const WindowArgs &a, const WindowItem &it, int from, int n_rows, int kvh, int lane, int wave, int pg0, int pg1, u32x4_t *lds,
                                               Columns<DH> (&c)[BLOCKS]) {
     constexpr int HEAD = kv4_head_bytes(DH, GROUP), W = DH / 32, OPERANDS = DH / 16;  // W: words of a thread; operands of keys, of values
@@ -328,7 +344,7 @@ struct FourBits {
       for (int g = 0; g < NG; ++g) numbers[g] = *reinterpret_cast<const u32x4_t *>(p + 64 * g);
     };
     auto put = [&](int pr) __attribute__((always_inline)) {
-      u32x4_t *to = lds + ((pr & 1) * 2 + values) * OPERANDS * 64 + word0 * 64 + lane;
+      u32x4_t *to = lds + ((TWICE ? pr & 1 : 0) * 2 + values) * OPERANDS * 64 + word0 * 64 + lane;
 #pragma unroll
       for (int i = 0; i < W; ++i) to[i * 64] = unpack(codes[i]);
     };
@@ -344,19 +360,35 @@ struct FourBits {
     load_codes(1);
     meet();
     for (int pr = 0; 2 * pr < n_pg; ++pr) {
-      put(pr + 1);
-      load_codes(pr + 2);
+      if constexpr (TWICE) {
+        put(pr + 1);
+        load_codes(pr + 2);
+      }
+      auto keys_read = [&]() __attribute__((always_inline)) {
+        load_numbers(pr + 1);
+        if constexpr (!TWICE) {
+          meet();  // (and this pair's values are there)
+          if (!values) {
+            put(pr + 1);
+            load_codes(pr + 2);
+          }
+        }
+      };
       const int tb = 32 * pr;
       const bool seen = n_rows > 0 && tb <= last && (tb + 31 > first - a.window || tb < sinks);  // wave-uniform
       if (seen) {
-        const u32x4_t *own = lds + (pr & 1) * 2 * OPERANDS * 64 + lane;
+        const u32x4_t *own = lds + (TWICE ? pr & 1 : 0) * 2 * OPERANDS * 64 + lane;
         pair(
             a, tb, n_pg, first, last, sinks, at, numbers, c, [&](int, int w) __attribute__((always_inline)) { return as_bf16x8(own[w * 64]); },
-            [&](int, int db) __attribute__((always_inline)) { return as_bf16x8(own[(OPERANDS + db) * 64]); }, [&]() __attribute__((always_inline)) { load_numbers(pr + 1); });
+            [&](int, int db) __attribute__((always_inline)) { return as_bf16x8(own[(OPERANDS + db) * 64]); }, keys_read);
       } else {
-        load_numbers(pr + 1);
+        keys_read();
       }
-      meet();  // the pair that was read may be overwritten, the next one is there
+      meet();  // what was read may be overwritten, what was written is there
+      if (!TWICE && values) {
+        put(pr + 1);
+        load_codes(pr + 2);
+      }
     }
   }
 
@@ -393,13 +425,19 @@ struct FourBitPages : FourBits<DH, GROUP, HEADS_, 1> {
 // wavefronts 217); pages brought to fp16 and bf16 once for the kernel of longer segments of a cache in bf16 took 199 us there, but with all batches of its kind 1.4 to 1.8 times the
 // time of these, and a second copy of the pages.
 template <int DH, int GROUP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void window_rows4_kernel(const WindowArgs a) {
+using RowBits = FourBits<DH, GROUP, 1, KV4_ROW_BLOCKS>;
+template <int DH, int GROUP>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowBits<DH, GROUP>::WAVES, RowBits<DH, GROUP>::WAVES))) void window_rows4_kernel(const WindowArgs a) {
+  typedef RowBits<DH, GROUP> Bits;
+  constexpr int QUERIES = Bits::Q_LDS ? KV4_ROW_BLOCKS * (DH / 32) * 64 : 1;  // of a wavefront
   const int hkv = a.s.n_kv_heads, grp = a.s.n_q_heads / hkv, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  __shared__ u32x4_t lds[2 * 2 * (DH / 16) * 64];
+  __shared__ u32x4_t lds[(Bits::TWICE ? 2 : 1) * 2 * (DH / 16) * 64];
+  __shared__ bf16x8_t queries[4 * QUERIES];
   const int kvh = blockIdx.x % hkv, rows = max(1, 16 * KV4_ROW_BLOCKS / grp), from = wave * rows;
   const WindowItem it = a.items[blockIdx.x / hkv];
   const int n_rows = max(0, min(rows, it.n_rows - from));
-  FourBits<DH, GROUP, 1, KV4_ROW_BLOCKS> bits;
+  Bits bits;
+  bits.q_lds = (typename Bits::Lds *)(queries + (Bits::Q_LDS ? wave * QUERIES + lane : 0));
   Columns<DH> c[KV4_ROW_BLOCKS];
 #pragma unroll
   for (int b = 0; b < KV4_ROW_BLOCKS; ++b) {
