@@ -386,8 +386,8 @@ Cut cut_choice(const std::vector<bs_window::Work> &work, int wg_per_work, int dh
 }
 
 // The microseconds that are expected of wide units over a cache in four bits: what all of them take of the chip's SIMDs, or the longest.
-// Fitted to 27 600 batches of 1 to 16 sequences of 5 to 3000 rows behind up to 8000 tokens, timed as narrow and as wide work: 6 % off on average,
-// and the kind that is chosen 0.23 % off the shorter, 7 % for one in a hundred.  (All of them as narrow work: 1.5 %; the largest 20 to 30 %.)
+// Fitted to 23 100 batches of 1 to 16 sequences of 5 to 3000 rows behind up to 8000 tokens, timed as narrow and as wide work: 7 % off on average,
+// and the kind that is chosen 0.23 % off the shorter, 8 % for one in a hundred.  (All of them as narrow work: 2.3 %; the largest 20 to 40 %.)
 double wide4_us(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g, int group, int n_cu) {
   if (rows.empty()) return 0.0;
   int64_t pages = 0;
@@ -396,9 +396,9 @@ double wide4_us(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g,
     pages += r.pages;
     longest = std::max(longest, r.pages);
   }
-  const double step = g.head_dim == 128 ? 1.58 + 0.197 * (128 / group) : 1.045 + 0.25 * (64 / group), per_simd = g.n_kv_heads / (4.0 * n_cu);
-  const double all = per_simd * (0.88 * (double)pages + 10.0 * (double)rows.size()), alone = 0.345 * longest;
-  return 6.6 + 1.05 * step * std::pow(std::pow(all, 3.6) + std::pow(alone, 3.6), 1.0 / 3.6);
+  const double step = g.head_dim == 128 ? 1.77 : 0.856 + 0.228 * (64 / group), per_simd = g.n_kv_heads / (4.0 * n_cu);
+  const double all = per_simd * (0.89 * (double)pages + 10.0 * (double)rows.size()), alone = 0.407 * longest;
+  return 6.5 + step * std::pow(std::pow(all, 2.9) + std::pow(alone, 2.9), 1.0 / 2.9);
 }
 
 void cut_blocks(bs_window *w, int most) {
