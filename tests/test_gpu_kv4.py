@@ -129,7 +129,7 @@ def attention(lib, layer, group, batch, window, sinks, seed=0, poison=True, q_st
         rows = qf[a:b].reshape(b - a, hq, dh)
         parts = [(0, b - a)]
         if rows_checked and b - a > rows_checked:
-            parts = [(j, j + 1) for j in sorted({0, 1, 31, 32, b - a - 1, *rng.choice(b - a, rows_checked - 5).tolist()})]
+            parts = [(j, j + 1) for j in sorted({0, 1, 31, 32, b - a - 1, *rng.choice(b - a, rows_checked - 5).tolist()}) if j < b - a]
         for j0, j1 in parts:
             m = min(n, max(0, n - (b - a) + j1))     # (tokens that these rows could see)
             ref, _ = OS.window_attention(rows[j0:j1], K[:m], V[:m], n - (b - a) + j0, window, sinks)
@@ -273,6 +273,25 @@ def test_a_step_repeats_itself_and_captured_steps_too(lib):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(again, want)
+
+
+def test_shared_rows_repeat_themselves_in_a_graph_and_in_place(lib):
+    import torch
+    layer = make_layer(lib, 48, 8, 128)
+    batch = make_batch([(400 + i, 900 + 7 * i) for i in range(4)] + [(1, 200)])
+    for group in (128, 64):
+        plan, q, pool, out = attention(lib, layer, group, batch, 100_000, 0, rows_checked=8)
+        assert plan.division().wide_blocks > 0
+        again, graph, side = torch.empty_like(out), torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            layer.window_attention(plan, q, pool, out=again, stream=side)
+        for _ in range(3):
+            again.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(again, out) and torch.equal(layer.window_attention(plan, q, pool), out)
+        assert torch.equal(layer.window_attention(plan, q, pool, out=q), out)
 
 
 def test_plans_of_either_cache_in_turn(lib):
