@@ -104,24 +104,28 @@ __global__ __launch_bounds__(T) void w8_quantize_kernel(const QuantArgs a) {
   for (int at = (QUANT_KEPT * T + (int)threadIdx.x) * 8; at < a.k; at += T * 8) put(attn_dev::ld16(x + at), at);
 }
 
-constexpr int MOST_LAUNCH = 1 << 23;  // rows of a launch
+constexpr int MOST_LAUNCH = 1 << 30, FEW_LONG_ROWS = 256;  // threads; rows of more than 8192 inputs
 hipError_t launch_quantize(const QuantArgs &a, hipStream_t stream) {
   if (a.m <= 0) return hipSuccess;
-  // (few long rows: more threads ask at once, 33 rows of 28672 10.3 -> 5 us)
-  if (a.k > 8192 && a.m < 1024) {
-    hipLaunchKernelGGL(w8_quantize_kernel<1024>, dim3(a.m), dim3(1024), 0, stream, a);
-    return hipGetLastError();
-  }
-  for (int m0 = 0; m0 < a.m; m0 += MOST_LAUNCH) {  // (a launch has less than 2^32 threads)
-    QuantArgs part = a;
-    part.x += (int64_t)m0 * a.x_stride;
-    part.q += (int64_t)m0 * a.k;
-    part.scale += m0;
-    part.m = std::min(MOST_LAUNCH, a.m - m0);
-    hipLaunchKernelGGL(w8_quantize_kernel<256>, dim3(part.m), dim3(256), 0, stream, part);
-    if (const hipError_t e = hipGetLastError()) return e;
-  }
-  return hipSuccess;
+  // About sixteen numbers a thread; of few long rows more threads ask at once.  (us with 64, 128, 256, 512 threads: 3000 rows of 1024 4.7, 5.1, 6.1, 9.0;
+  // 2560 of 4096 9.8, 9.2, 8.9, 10.4; 4000 of 14336 47, 42, 38, 30.  33 rows of 28672: 10.3 with 256, 5.2 with 1024;
+  // 120 and 600 rows of 14336: with 512 and 1024 alike, and 8.4 and 9.1.)
+  const auto rows_of = [&](auto threads) -> hipError_t {
+    for (int m0 = 0; m0 < a.m; m0 += MOST_LAUNCH / threads()) {  // (a launch has less than 2^32 threads)
+      QuantArgs part = a;
+      part.x += (int64_t)m0 * a.x_stride;
+      part.q += (int64_t)m0 * a.k;
+      part.scale += m0;
+      part.m = std::min(MOST_LAUNCH / threads(), a.m - m0);
+      hipLaunchKernelGGL((w8_quantize_kernel<threads()>), dim3(part.m), dim3(threads()), 0, stream, part);
+      if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+  };
+  if (a.k <= 1024) return rows_of(std::integral_constant<int, 64>{});
+  if (a.k <= 2048) return rows_of(std::integral_constant<int, 128>{});
+  if (a.k <= 8192) return rows_of(std::integral_constant<int, 256>{});
+  return a.m <= FEW_LONG_ROWS ? rows_of(std::integral_constant<int, 1024>{}) : rows_of(std::integral_constant<int, 512>{});
 }
 
 // ------------------------------------------------------------------------------

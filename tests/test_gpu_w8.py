@@ -43,7 +43,7 @@ def _check(got, ref):
     assert same.all(), "%d of %d, worst %.3g" % ((~same).sum(), same.size, np.nanmax(np.abs(got - ref) / np.maximum(np.abs(ref), 1e-30)))
 
 
-@pytest.mark.parametrize("m,k", [(1, 16), (3, 48), (5, 256), (2, 4096), (7, 8192 + 16), (1, 28672), (300, 688)])
+@pytest.mark.parametrize("m,k", [(1, 16), (3, 48), (5, 256), (2, 4096), (7, 8192 + 16), (1, 28672), (300, 688), (40, 1536), (300, 9232)])
 def test_rows_as_integers(layer, m, k):
     rng = np.random.default_rng(m + k)
     x = W.f32_to_bf16_bits((rng.standard_normal((m, k + 8)) * np.exp(20 * rng.standard_normal((m, 1)))).astype(np.float32))
