@@ -274,3 +274,12 @@ def test_every_kind_of_tile_is_reached():
         seen.add((rows, outputs))
         assert ranges >= 1 and (rows > 32 or ranges == 1)
     assert seen >= {(16, 16), (16, 32), (32, 16), (32, 32), (64, 128), (128, 128), (192, 128), (128, 256), (160, 256), (192, 256), (256, 256)}, seen
+
+
+def test_every_kind_of_tile_takes_ranges_too():
+    layer, seen = binding.Layer(SHAPE, device=-1), set()
+    for m, n, k in ((127, 465, 3616), (340, 1133, 7376), (133, 5923, 7760), (199, 8826, 5952), (799, 2509, 7696), (541, 6409, 11040), (995, 5415, 10832)):
+        rows, outputs, ranges = layer.w8_division(m, n, k)
+        assert ranges > 1
+        seen.add((rows, outputs))
+    assert seen == {(64, 128), (128, 128), (192, 128), (128, 256), (160, 256), (192, 256), (256, 256)}, seen

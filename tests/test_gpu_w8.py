@@ -189,3 +189,37 @@ def test_captured_products(lib, layer, m, n, k):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, layer.w8_linear(x, weight))
+
+
+def _whole_numbers(layer, lib, m, n, k, seed, chunk=8192):
+    """A product of any integers, with every result against whole numbers, some rows and outputs at a time."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q, w = (torch.randint(-128, 128, (i, k), dtype=torch.int8, device="cuda", generator=g) for i in (m, n))
+    scales, s = (1e-3 * (0.5 + torch.rand(i, device="cuda", generator=g)) for i in (m, n))
+    y = layer.w8_linear(lib.W8Rows(q, scales), lib.W8Weight(w, s))
+    for m0 in range(0, m, chunk):
+        rows = q[m0:m0 + chunk].double()
+        for n0 in range(0, n, chunk):
+            # (below 2^53: exact in float64 in any order)
+            ref = (rows @ w[n0:n0 + chunk].double().t()) * scales[m0:m0 + chunk].double()[:, None] * s[n0:n0 + chunk].double()[None]
+            wrong = (y[m0:m0 + chunk, n0:n0 + chunk].double() - ref).abs() > BOUND * ref.abs() + 1e-37
+            assert not wrong.any(), "%d wrong, the first at %s of part (%d, %d)" % (int(wrong.sum()), wrong.nonzero()[0].tolist(), m0, n0)
+
+
+@pytest.mark.parametrize("m,n,k,division", [
+    (127, 465, 3616, (64, 128, 6)), (84, 328, 11200, (64, 128, 16)), (340, 1133, 7376, (128, 128, 8)), (69, 7397, 7552, (128, 128, 4)), (133, 5923, 7760, (192, 128, 4)),
+    (672, 2081, 8640, (192, 128, 3)), (199, 8826, 5952, (128, 256, 3)), (799, 2509, 7696, (160, 256, 4)), (269, 3145, 13504, (160, 256, 8)), (541, 6409, 11040, (192, 256, 3)),
+    (995, 5415, 10832, (256, 256, 2)), (408, 7606, 10288, (256, 256, 4))])
+def test_ranges_of_every_tile(lib, layer, m, n, k, division):
+    assert layer.w8_division(m, n, k) == division
+    _whole_numbers(layer, lib, m, n, k, m)
+
+
+def test_rows_beyond_four_gigabytes(lib, layer):
+    _whole_numbers(layer, lib, 150_100, 40, 28_672, 1)
+
+
+def test_tiles_of_weights_beyond_four_gigabytes(lib, layer):
+    assert layer.w8_division(129, 149_760, 28_672) == (160, 256, 1) and layer.w8_division(129, 340, 28_672)[2] > 1    # (the two parts of it)
+    _whole_numbers(layer, lib, 129, 150_100, 28_672, 2)
