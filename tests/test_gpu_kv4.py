@@ -431,3 +431,38 @@ def test_copies_and_compaction(lib):
     assert live == 4 and list(tables) == [3, -1, 2, 0, 3, 1]
     for old, new in zip([19, 2, 5, 17], [tables[0], tables[2], tables[3], tables[5]]):
         assert torch.equal(pools.view(3, 20, size)[:, new], want[:, old])
+
+
+@pytest.mark.parametrize("hq,hkv,dh,group", SHAPES)
+def test_appended_keys_by_their_own_scale(lib, hq, hkv, dh, group):
+    """Every key of a step where it belongs.  What is kept is within half a scale of the turned key, and rounded to bf16 when it is read back; the
+    reference's angles may be off by the last of 24 bits, which moves the turned key by 2^-23 of its two terms, and what is kept by no more than both halves."""
+    import torch
+    layer, cache, rng = make_layer(lib, hq, hkv, dh), lib.Kv4(group), np.random.default_rng([hq, dh, group])
+    batch = make_batch([(1, 1), (1, 16), (2, 40), (5, 21), (9, 24), (16, 16), (40, 77), (130, 131), (4, 2), (0, 9), (1, 100)], seed=group)
+    x = _bits(rng, (batch.n_rows, (hq + 2 * hkv) * dh))
+    x[7, (hq + 1) * dh - 1] = 0x7FC0
+    pool = torch.zeros(batch.n_pages * layer.page_bytes(cache), dtype=torch.uint8, device="cuda")
+    layer.rope_append(layer.window_plan(batch, 5, 0, cache=cache), to_gpu(x), pool)
+    got = to_host(layer.kv4_unpack(pool, cache)[0])
+    seq = np.repeat(np.arange(batch.n_seq), np.diff(batch.row_start))
+    at = batch.kv_len[seq] - batch.row_start[seq + 1] + np.arange(batch.n_rows)
+    angle = np.maximum(at, 0)[:, None] * layer.shape.rope_theta ** (-2.0 * np.arange(dh // 2) / dh)
+    cos, sin = np.cos(angle).astype(np.float32)[:, None], np.sin(angle).astype(np.float32)[:, None]
+    key = W.bf16_bits_to_f32(x).reshape(batch.n_rows, -1, dh)[:, hq:hq + hkv]
+    lo, hi = key[..., :dh // 2], key[..., dh // 2:]
+    with np.errstate(invalid="ignore"):
+        turned = np.concatenate([lo * cos - hi * sin, hi * cos + lo * sin], axis=-1)
+        moves = 2.0 ** -23 * np.concatenate([np.abs(lo * cos) + np.abs(hi * sin), np.abs(hi * cos) + np.abs(lo * sin)], axis=-1)
+    rows = np.flatnonzero(at >= 0)
+    pages = batch.page_ids[batch.page_start[seq[rows]] + at[rows] // 16]
+    have, near = got[pages, at[rows] % 16], W.bf16_bits_to_f32(_kept_bits(turned[rows], group)).astype(np.float64)
+    assert np.array_equal(np.isnan(have), np.isnan(near)) and np.isnan(near).sum() == min(2 * group, dh)   # (a pair's two channels)
+    scale = np.repeat(OB.kv4_numbers(turned[rows], group)[0].astype(np.float64), group, axis=-1)
+    bound = scale * (1 + U) + U / 2 * (np.abs(have) + np.abs(near)) + 2 * moves[rows]
+    wrong = ~(np.abs(have - near) <= bound) & ~np.isnan(near)
+    assert not wrong.any(), "%d of %d" % (wrong.sum(), wrong.size)
+    assert (~_equal_or_nan(have, near)).sum() <= max(group, 1e-4 * near.size)
+    touched = np.zeros(got.shape[:2], dtype=bool)
+    touched[pages, at[rows] % 16] = True
+    assert (got[~touched] == 0).all()
