@@ -62,7 +62,7 @@ int bs_kv4_compact(bs_ctx *ctx, void *const *pools, int32_t n_pools, int64_t n_p
  * float [m]. */
 int bs_w8_quantize(bs_ctx *ctx, const void *x, int64_t x_stride, int64_t m, int64_t k, void *q, float *scales, void *stream);
 
-/* q: device int8 [m, k], weight: device int8 [n, k] (any values, -128 included), 16-byte aligned; scales: device float [m], weight_scales: device float [n];
+/* q: device int8 [m, k], weight: device int8 [n, k] (any values of either, -128 included), 16-byte aligned; scales: device float [m], weight_scales: device float [n];
  * y: device bf16, row i at y + i * y_stride, rounded once.  The calls on one context share a workspace and must not overlap in time on
  * different streams. */
 int bs_w8_linear(bs_ctx *ctx, const void *q, const float *scales, const void *weight, const float *weight_scales, int64_t m, int64_t n, int64_t k, void *y,

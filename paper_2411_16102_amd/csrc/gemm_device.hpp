@@ -126,6 +126,15 @@ __device__ __forceinline__ void gemm_mfma(i32x4_t &c, bf16x8_t w, bf16x8_t x) {
 }
 constexpr bool gemm_in_integers(int epi) { return epi == EPI_W8 || epi == EPI_W8_PARTIAL; }
 
+// Sums of products of 8-bit integers as 32-bit numbers.  131072 products of -128 and -128 are 2^31, which 32 bits hold as -2^31; every other sum
+// is more than that by 2^24 at least (127 * 128 * 131072), and so is what it is rounded to.
+__device__ __forceinline__ f32x4_t w8_sums(i32x4_t s) {
+  f32x4_t v = __builtin_convertvector(s, f32x4_t);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = v[e] == -0x1p31f ? 0x1p31f : v[e];
+  return v;
+}
+
 // four neighbouring results of a row, of which those below n_lim exist
 __device__ __forceinline__ void store_scaled4(uint16_t *p, f32x4_t v, int n, int n_lim, bool aligned) {
   if (aligned && n + 4 <= n_lim) {
@@ -524,7 +533,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
       for (int ni = 0; ni < NI; ++ni)
         if (c + j < MI) {
           auto *to = turned + (j * 16 + lr) * RS + (ni * 16 + 4 * lg) * 4;
-          if constexpr (EPI == EPI_W8) *reinterpret_cast<f32x4_t *>(to) = __builtin_convertvector(acc[ni][c + j], f32x4_t) * row_scale[c + j];
+          if constexpr (EPI == EPI_W8) *reinterpret_cast<f32x4_t *>(to) = w8_sums(acc[ni][c + j]) * row_scale[c + j];
           else *reinterpret_cast<Acc *>(to) = acc[ni][c + j];
         }
     __builtin_amdgcn_wave_barrier();
@@ -974,7 +983,7 @@ __global__ __launch_bounds__(512) void gemm_rows_kernel(const GemmArgs a, const 
         if constexpr (I8) {
           const int n0 = (blk * NI + ni) * 16 + 4 * lg;
           if (!ok || n0 >= a.N) continue;
-          f32x4_t v = __builtin_convertvector(total_of(lane), f32x4_t) * a.row_scale[ml];
+          f32x4_t v = w8_sums(total_of(lane)) * a.row_scale[ml];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] *= a.col_scale[min(n0 + e, a.N - 1)];
           store_scaled4(a.C + (size_t)ml * a.ldc + n0, v, n0, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);

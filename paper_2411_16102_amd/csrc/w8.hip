@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void w8_reduce_kernel(const GemmArgs a) {
   i32x4_t s = {0, 0, 0, 0};
 #pragma unroll 8
   for (int k = 0; k < a.k_splits; ++k) s += p[k * plane];
-  f32x4_t v = __builtin_convertvector(s, f32x4_t) * a.row_scale[m];
+  f32x4_t v = w8_sums(s) * a.row_scale[m];
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= a.col_scale[min(n + e, a.N - 1)];
   store_scaled4(a.C + (size_t)m * a.ldc + n, v, n, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(512) void w8_few_kernel(const FewArgs f, const int 
       i32x4_t sum = red[lane];
 #pragma unroll
       for (int v = 1; v < 8; ++v) sum += red[v * 64 + lane];
-      f32x4_t v = __builtin_convertvector(sum, f32x4_t) * row_scale;
+      f32x4_t v = __builtin_convertvector(sum, f32x4_t) * row_scale;  // (rows within -127 .. 127: every sum stays in 32 bits)
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= a.col_scale[min(n0 + e, a.N - 1)];
       store_scaled4(a.C + (size_t)lr * a.ldc + n0, v, n0, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
@@ -444,7 +444,7 @@ hipError_t launch_product(GemmArgs a, size_t ws_floats, hipStream_t stream) {
 }
 
 constexpr int64_t MOST_BYTES = 0xFFFF0000;  // of an operand that a launch sees (offsets are 32 bits)
-constexpr int64_t MOST_K = 131072;          // 127 * 128 k stays in 32 bits
+constexpr int64_t MOST_K = 131072;          // 128 * 128 k stays in 32 bits, but for one sum (see w8_sums)
 constexpr int64_t MOST_ROWS = 1 << 30;
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }

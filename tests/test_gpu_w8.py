@@ -223,3 +223,15 @@ def test_rows_beyond_four_gigabytes(lib, layer):
 def test_tiles_of_weights_beyond_four_gigabytes(lib, layer):
     assert layer.w8_division(129, 149_760, 28_672) == (160, 256, 1) and layer.w8_division(129, 340, 28_672)[2] > 1    # (the two parts of it)
     _whole_numbers(layer, lib, 129, 150_100, 28_672, 2)
+
+
+@pytest.mark.parametrize("m,n", [(1, 40), (1, 2692), (32, 4017), (40, 520), (300, 700), (523, 10848), (700, 1500), (3934, 2579)])
+def test_the_greatest_sum_of_all(lib, layer, m, n):
+    # 131072 products of -128 and -128 are 2^31, one more than an integer of 32 bits holds; of -127 in a row they stay below, of 127 they are the least of all
+    import torch
+    k = 131072
+    row = torch.tensor([-128, 127, -127, 0], dtype=torch.int8, device="cuda")[torch.arange(m, device="cuda") % 4]
+    q = row[:, None].expand(m, k).contiguous()
+    weight = lib.W8Weight(torch.full((n, k), -128, dtype=torch.int8, device="cuda"), torch.full((n,), 2.0 ** -20, device="cuda"))
+    y = layer.w8_linear(lib.W8Rows(q, torch.ones(m, device="cuda")), weight)
+    _check(y, np.broadcast_to((row.cpu().numpy().astype(np.float64) * -128.0 * k * 2.0 ** -20)[:, None], (m, n)))
