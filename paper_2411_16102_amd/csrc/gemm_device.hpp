@@ -128,12 +128,24 @@ constexpr bool gemm_in_integers(int epi) { return epi == EPI_W8 || epi == EPI_W8
 
 // Sums of products of 8-bit integers as 32-bit numbers.  131072 products of -128 and -128 are 2^31, which 32 bits hold as -2^31; every other sum
 // is more than that by 2^24 at least (127 * 128 * 131072), and so is what it is rounded to.
+constexpr int W8_LONG = 131072 / 2;  // GemmArgs::K of such sums
 __device__ __forceinline__ f32x4_t w8_sums(i32x4_t s) {
   f32x4_t v = __builtin_convertvector(s, f32x4_t);
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = v[e] == -0x1p31f ? 0x1p31f : v[e];
   return v;
 }
+
+// A row's scale as its sums are multiplied by it, and what a result is multiplied by last: a sum is up to 2^31, so that times a scale of 2^96 and more
+// leaves the range of 32 bits where the result, with an output's scale, need not.
+struct W8RowScale {
+  float scale, back;
+  __device__ __forceinline__ explicit W8RowScale(float s) {
+    const bool far = fabsf(s) >= 0x1p96f;
+    scale = far ? s * 0x1p-32f : s;
+    back = far ? 0x1p32f : 1.f;
+  }
+};
 
 // four neighbouring results of a row, of which those below n_lim exist
 __device__ __forceinline__ void store_scaled4(uint16_t *p, f32x4_t v, int n, int n_lim, bool aligned) {
@@ -524,17 +536,26 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) row_scale[mi] = a.row_scale[min(m0 + wm0 + mi * 16 + lr, a.M - 1)];
   }
-  // blocks [c, c + CM) of rows into LDS (read and written by this wavefront alone, whose LDS operations complete in order)
-  auto turn = [&](int c) {
+  constexpr int BACK = 64 * 4;  // where W8RowScale::back of a turned row stands, behind its numbers
+  // blocks [c, c + CM) of rows into LDS (read and written by this wavefront alone, whose LDS operations complete in order);
+  // whole_range: sums and scales of integers of any size
+  auto turn = [&](int c, auto whole_range) {
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < CM; ++j)
 #pragma unroll
       for (int ni = 0; ni < NI; ++ni)
         if (c + j < MI) {
-          auto *to = turned + (j * 16 + lr) * RS + (ni * 16 + 4 * lg) * 4;
-          if constexpr (EPI == EPI_W8) *reinterpret_cast<f32x4_t *>(to) = w8_sums(acc[ni][c + j]) * row_scale[c + j];
-          else *reinterpret_cast<Acc *>(to) = acc[ni][c + j];
+          unsigned char *row = turned + (j * 16 + lr) * RS, *to = row + (ni * 16 + 4 * lg) * 4;
+          if constexpr (EPI == EPI_W8 && decltype(whole_range)::value) {
+            const W8RowScale by(row_scale[c + j]);
+            *reinterpret_cast<f32x4_t *>(to) = w8_sums(__builtin_bit_cast(i32x4_t, acc[ni][c + j])) * by.scale;
+            if (ni == 0 && lg == 0) *reinterpret_cast<float *>(row + BACK) = by.back;
+          } else if constexpr (EPI == EPI_W8) {
+            *reinterpret_cast<f32x4_t *>(to) = __builtin_convertvector(acc[ni][c + j], f32x4_t) * row_scale[c + j];
+          } else {
+            *reinterpret_cast<Acc *>(to) = acc[ni][c + j];
+          }
         }
     __builtin_amdgcn_wave_barrier();
   };
@@ -565,7 +586,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
     }
 #pragma unroll
     for (int c = 0; c < MI; c += CM) {
-      turn(c);
+      turn(c, No{});
 #pragma unroll 1
       for (int g = 0; g < rows_in(c); g += 4 * U) {
         f32x4_t v[U];
@@ -613,18 +634,33 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
 #pragma unroll
       for (int e = 0; e < 4; ++e) scale[e] = a.col_scale[min(n + e, a.N - 1)];
     }
+    const auto store = [&](auto whole_range) {
 #pragma unroll
-    for (int c = 0; c < MI; c += CM) {
-      turn(c);
+      for (int c = 0; c < MI; c += CM) {
+        turn(c, whole_range);
 #pragma unroll 4
-      for (int g = 0; g < rows_in(c); g += 4) {
-        const int m = m0 + wm0 + c * 16 + g + r16;
-        const auto *from = turned + (g + r16) * RS + c16 * 4;
-        if (m >= a.M || n >= n_lim) continue;
-        if constexpr (EPI == EPI_W8) store_scaled4(a.C + (size_t)m * a.ldc + n, *reinterpret_cast<const f32x4_t *>(from) * scale, n, n_lim, aligned);
-        else *reinterpret_cast<i32x4_t *>(ws + (size_t)m * stride + n) = *reinterpret_cast<const i32x4_t *>(from);
+        for (int g = 0; g < rows_in(c); g += 4) {
+          const int m = m0 + wm0 + c * 16 + g + r16;
+          const unsigned char *row = turned + (g + r16) * RS, *from = row + c16 * 4;
+          if (m >= a.M || n >= n_lim) continue;
+          if constexpr (EPI == EPI_W8) {
+            f32x4_t v = *reinterpret_cast<const f32x4_t *>(from) * scale;
+            if constexpr (decltype(whole_range)::value) v *= *reinterpret_cast<const float *>(row + BACK);
+            store_scaled4(a.C + (size_t)m * a.ldc + n, v, n, n_lim, aligned);
+          } else {
+            *reinterpret_cast<i32x4_t *>(ws + (size_t)m * stride + n) = *reinterpret_cast<const i32x4_t *>(from);
+          }
+        }
       }
+    };
+    // (what few products need takes 2 % of the time of large ones, so it is a path of its own: 2560 x 28672 x 4096 271 against 265 us)
+    bool far = a.K >= W8_LONG;
+    if constexpr (EPI == EPI_W8) {
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) far |= W8RowScale(row_scale[mi]).back != 1.f;
     }
+    if (EPI == EPI_W8 && __builtin_amdgcn_ballot_w64(far) != 0) store(Yes{});
+    else store(No{});
   }
 
   float rstd[MI];
@@ -700,7 +736,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &a, const int bid, cons
       ask_rows(8 * U);
 #pragma unroll
       for (int c = 0; c < MI; c += CM) {
-        turn(c);
+        turn(c, No{});
 #pragma unroll 1
         for (int g = 0; g < rows_in(c); g += 8 * U) {
           f32x4_t lo[U], hi[U];
@@ -983,10 +1019,11 @@ __global__ __launch_bounds__(512) void gemm_rows_kernel(const GemmArgs a, const 
         if constexpr (I8) {
           const int n0 = (blk * NI + ni) * 16 + 4 * lg;
           if (!ok || n0 >= a.N) continue;
-          f32x4_t v = w8_sums(total_of(lane)) * a.row_scale[ml];
+          const W8RowScale by(a.row_scale[ml]);
+          f32x4_t v = w8_sums(total_of(lane)) * by.scale;
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] *= a.col_scale[min(n0 + e, a.N - 1)];
-          store_scaled4(a.C + (size_t)ml * a.ldc + n0, v, n0, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
+          store_scaled4(a.C + (size_t)ml * a.ldc + n0, v * by.back, n0, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
         } else if (paired) {
           const int u = first_row(blk * NI + ni) + 4 * (lg & 1);  // first of this lane's four rows of the lower unit
           const f32x4_t lo = total_of(lane & 31) * meta_rs[ml], hi = total_of((lane & 31) + 32) * meta_rs[ml];

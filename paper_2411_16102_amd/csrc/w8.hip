@@ -1,7 +1,7 @@
 // Products of 8-bit integers with a scale for each row of either operand, and the rows' way there.
 //
 // y[m, n] = row_scale[m] col_scale[n] sum over k of xq[m, k] w[n, k]: sums of integers in 32 bits, exact whatever their order, then two products in
-// 32 bits and one rounding.  v_mfma_i32_16x16x64_i8 takes the same 16 bytes of a row from a lane as the bf16 instruction of half the
+// 32 bits (within their range where the result is: see W8RowScale) and one rounding.  v_mfma_i32_16x16x64_i8 takes the same 16 bytes of a row from a lane as the bf16 instruction of half the
 // length, and as long, so tiles and rings are those of gemm.hip with rows of k / 2 numbers: twice the operations for every byte that moves.
 #include <hip/hip_runtime.h>
 
@@ -142,10 +142,11 @@ __global__ __launch_bounds__(256) void w8_reduce_kernel(const GemmArgs a) {
   i32x4_t s = {0, 0, 0, 0};
 #pragma unroll 8
   for (int k = 0; k < a.k_splits; ++k) s += p[k * plane];
-  f32x4_t v = w8_sums(s) * a.row_scale[m];
+  const W8RowScale by(a.row_scale[m]);
+  f32x4_t v = w8_sums(s) * by.scale;
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= a.col_scale[min(n + e, a.N - 1)];
-  store_scaled4(a.C + (size_t)m * a.ldc + n, v, n, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
+  store_scaled4(a.C + (size_t)m * a.ldc + n, v * by.back, n, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
 }
 
 // Up to four rows: rows as integers and their product in one launch.  As gemm_rows_kernel, but that the rows, brought over as they are and first,
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(512) void w8_few_kernel(const FewArgs f, const int 
     const RowScale scale = scale_of(row);
     for (int at = at0; at < k; at += step) *reinterpret_cast<u32x2_t *>(ints + row * k + at) = scale.integers(mine_raw[at / 8]);
   }
-  const float row_scale = scale_of(min(lr, a.M - 1)).scale;
+  const W8RowScale by(scale_of(min(lr, a.M - 1)).scale);
   __builtin_amdgcn_s_waitcnt(waitcnt_imm(63, true));
   __builtin_amdgcn_s_barrier();
 
@@ -283,10 +284,10 @@ __global__ __launch_bounds__(512) void w8_few_kernel(const FewArgs f, const int 
       i32x4_t sum = red[lane];
 #pragma unroll
       for (int v = 1; v < 8; ++v) sum += red[v * 64 + lane];
-      f32x4_t v = __builtin_convertvector(sum, f32x4_t) * row_scale;  // (rows within -127 .. 127: every sum stays in 32 bits)
+      f32x4_t v = __builtin_convertvector(sum, f32x4_t) * by.scale;  // (rows within -127 .. 127: every sum stays in 32 bits)
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= a.col_scale[min(n0 + e, a.N - 1)];
-      store_scaled4(a.C + (size_t)lr * a.ldc + n0, v, n0, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
+      store_scaled4(a.C + (size_t)lr * a.ldc + n0, v * by.back, n0, a.N, ((reinterpret_cast<uintptr_t>(a.C) | (uintptr_t)a.ldc * 2) & 7) == 0);
     }
   }
 }

@@ -235,3 +235,24 @@ def test_the_greatest_sum_of_all(lib, layer, m, n):
     weight = lib.W8Weight(torch.full((n, k), -128, dtype=torch.int8, device="cuda"), torch.full((n,), 2.0 ** -20, device="cuda"))
     y = layer.w8_linear(lib.W8Rows(q, torch.ones(m, device="cuda")), weight)
     _check(y, np.broadcast_to((row.cpu().numpy().astype(np.float64) * -128.0 * k * 2.0 ** -20)[:, None], (m, n)))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 333, 592), (3, 333, 592), (9, 4099, 1040), (40, 333, 4112), (60, 300, 28672), (300, 700, 7376), (523, 2050, 1040), (1093, 4099, 2064)])
+def test_rows_and_scales_of_any_size(lib, layer, m, n, k):
+    # a row's scale times its sum may be beyond 32 bits where the result is not, and the other way round a row of the least numbers keeps all of its digits
+    rng = np.random.default_rng(m + n)
+    w, s, _ = _weight(lib, rng, n, k)
+    s = (s * np.where(np.arange(n) % 3 == 0, 1e-20, np.where(np.arange(n) % 3 == 1, 1e-33, 1e-3))).astype(np.float32)
+    x = rng.standard_normal((m, k)) * 10.0 ** np.linspace(37.3, -28.0, m)[:, None]
+    x = W.f32_to_bf16_bits(x.astype(np.float32))
+    import torch
+    weight = lib.W8Weight(torch.from_numpy(w).cuda(), torch.from_numpy(s).cuda())
+    q, scale = OB.w8_rows(W.bf16_bits_to_f32(x))
+    ref = _reference(q, scale, w, s)
+    most = 2.0 ** 128 * (1 - 2.0 ** -9)     # (what rounds to more than bf16 holds is an infinity)
+    sure = (np.abs(ref) < most * (1 - 2.0 ** -20)) | (np.abs(ref) > most * (1 + 2.0 ** -20))
+    for rows in (to_gpu(x), layer.w8_quantize(to_gpu(x))):
+        got = layer.w8_linear(rows, weight).float().cpu().numpy().astype(np.float64)
+        want = np.where(np.abs(ref) >= most, np.copysign(np.inf, ref), ref)
+        same = (got == want) | (np.abs(got - want) <= BOUND * np.abs(want) + 2.0 ** -133) | ~sure
+        assert same.all(), "%d of %d, the first at %s" % ((~same).sum(), same.size, np.argwhere(~same)[0])
