@@ -20,16 +20,17 @@ from typing import Sequence
 import numpy as np
 
 from . import workloads as W
+from .binding import W8Rows, W8Weight
 
 
 class Streams:
     """Sequences over `n_pages` pages of every layer, each of up to the layer's max_positions tokens (positions count from a sequence's
-    first token).  weights: (Wqkv, Wo) of each layer, from Layer.w4_pack or W8Weights.  cache: Kv4(group) for pages in four bits."""
+    first token).  weights: (Wqkv, Wo) of each layer, from Layer.w4_pack or in 8-bit integers (W8Weight, or what Layer.w8_quantize
+    gives).  cache: Kv4(group) for pages in four bits."""
 
     def __init__(self, api, layer, weights, n_pages: int, window: int, sinks: int, cache=None):
         import torch
         self.torch, self.layer, self.weights, self.cache = torch, layer, list(weights), cache
-        self.w8 = api.W8Weight
         self.window, self.sinks = window, sinks
         self.pages = api.Pages(n_pages)
         size, kind = (layer.page_bytes() // 2, torch.bfloat16) if cache is None else (layer.page_bytes(cache), torch.uint8)
@@ -46,7 +47,7 @@ class Streams:
                        seq_leaf_node=np.full(n, -1, dtype=np.int32), n_pages=self.pages.n_pages)
 
     def linear(self, x, weight):
-        return self.layer.w8_linear(x, weight) if isinstance(weight, self.w8) else self.layer.w4_linear(x, weight)
+        return self.layer.w8_linear(x, weight) if isinstance(weight, W8Rows) else self.layer.w4_linear(x, weight)
 
     def step(self, ids: Sequence[int], rows: Sequence[int], x):
         """x: bf16 [sum(rows), d_model], the rows of ids[0] first.  What the layers make of it, [sum(rows), d_model]."""
@@ -80,8 +81,6 @@ class Streams:
 def synthetic_weights(layer, n_layers: int, group: int = 128, seed: int = 0, bits: int = 4):
     """Seeded weights (Wqkv, Wo) of unit gain for each layer, in 4 bits, laid out, or in 8."""
     import torch
-
-    from .binding import W8Weight
     dev, gen = "cuda:%d" % layer.device, torch.Generator(device="cuda:%d" % layer.device).manual_seed(seed)
     s, out = layer.shape, []
     wide = s.n_q_heads * s.head_dim

@@ -283,3 +283,13 @@ def test_every_kind_of_tile_takes_ranges_too():
         assert ranges > 1
         seen.add((rows, outputs))
     assert seen == {(64, 128), (128, 128), (192, 128), (128, 256), (160, 256), (192, 256), (256, 256)}, seen
+
+
+def test_streams_take_weights_from_rows():
+    from types import SimpleNamespace
+
+    from paper_2411_16102_amd.streams import Streams
+    q, s = torch.zeros((4, 32), dtype=torch.int8), torch.zeros(4)
+    st = Streams.__new__(Streams)
+    st.layer = SimpleNamespace(w8_linear=lambda x, w: "eight", w4_linear=lambda x, w: "four")
+    assert [st.linear(None, w) for w in (binding.W8Rows(q, s), binding.W8Weight(q, s), binding.W4Weight)] == ["eight", "eight", "four"]

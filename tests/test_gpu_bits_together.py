@@ -156,3 +156,20 @@ def test_steps_on_another_stream(lib):
             results.append([st.step(ids, [len(x) - 1, 1], x) for x in inputs])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(*results)) and torch.equal(both[0].pools, both[1].pools)
+
+
+def test_weights_from_rows(lib):
+    # weights that Layer.w8_quantize made are those of their integers
+    import torch
+    from paper_2411_16102_amd.streams import Streams
+    layer, gen = lib.Layer(W.LayerShape(256, 8, 2, 64, 256), device=0), torch.Generator(device="cuda").manual_seed(3)
+    s = layer.shape
+    rows = [layer.w8_quantize((0.06 * torch.randn((n, k), device="cuda", generator=gen)).to(torch.bfloat16)) for n, k in ((s.n_qkv, 256), (256, 512))]
+    both = [Streams(lib, layer, [tuple(pair)], 16, WINDOW, SINKS, cache=lib.Kv4(64)) for pair in (rows, [lib.W8Weight(r.q, r.scales) for r in rows])]
+    for n in (50, 1, 4):
+        x = torch.randn((n, 256), device="cuda", generator=gen).to(torch.bfloat16)
+        results = []
+        for st in both:
+            ids = [0] if n != 50 else st.pages.open(1)
+            results.append(st.step(ids, [n], x))
+        assert torch.equal(*results) and torch.isfinite(results[0]).all()
