@@ -482,7 +482,6 @@ hipError_t launch_heads4(const WindowArgs &a, hipStream_t stream) {
   if (a.waves == 1) hipLaunchKernelGGL((window_unit4_kernel<DH, GROUP, HEADS, 1>), grid, block, 0, stream, a);
   else if (a.waves == 2) hipLaunchKernelGGL((window_unit4_kernel<DH, GROUP, HEADS, 2>), grid, block, 0, stream, a);
   else if (a.waves == 4) hipLaunchKernelGGL((window_unit4_kernel<DH, GROUP, HEADS, 4>), grid, block, 0, stream, a);
-  else if (a.waves == 8) hipLaunchKernelGGL((window_unit4_kernel<DH, GROUP, HEADS, 8>), grid, block, 0, stream, a);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }

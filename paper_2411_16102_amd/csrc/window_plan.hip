@@ -490,7 +490,7 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cf
   if (const int rc = sort_rows(w, b, r, chosen)) return rc;
   if (!w->work.empty()) {
     cut_blocks(w, cut.blocks);
-    if (!w->group) div = {4, std::max(div.pages, 8), 0.0};  // (one launch for both kinds, of workgroups of four wavefronts)
+    div = {4, std::max(div.pages, 8), 0.0};  // (one launch for both kinds, of workgroups of four wavefronts)
   }
   p.heads = div.heads;
   if (const int rc = add_units(w, b, div)) return rc;

@@ -54,3 +54,13 @@ def test_the_check_sees_an_early_read():
     assert early_reads(code % "") and early_reads(code % "\tv_mov_b32_e32 v9, v8 // 000000001004: 00000000\n")
     assert not early_reads(code % "\ts_nop 1 // 000000001004: 00000000\n")
     assert not early_reads(code % ("\tv_mov_b32_e32 v9, v8 // 000000001004: 00000000\n" * 2))
+
+
+def test_units_have_the_wavefronts_that_plans_give(listings):  # noqa: F811
+    from paper_2411_16102_amd import binding, workloads as W
+    from stream_cases import make_batch
+    layer, given = binding.Layer(W.LLAMA3_8B, device=-1), set()
+    for n, tokens in ((400, 100), (200, 60), (300, 1000), (128, 4000)):
+        given |= {layer.window_plan(make_batch([(1, tokens)] * n), 1 << 20, cache=binding.Kv4(g)).division().waves for g in (32, 64, 128)}
+    built = {int(m) for t in listings for m in re.findall(r"<_ZN\S*window_unit4_kernelILi\d+ELi\d+ELi\d+ELi(\d+)E\S*>:", t)}
+    assert built == given == {1, 2, 4}
