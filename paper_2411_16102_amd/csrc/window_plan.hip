@@ -206,7 +206,13 @@ Division divide(const std::vector<bs_window::Rows> &rows, int hkv, int dh, int n
   return div;
 }
 
-// The same over a cache in four bits, whose units read less and compute more: KV heads that share a wavefront too, where the columns of two have
+// Narrow work over a cache in four bits: microseconds that the chip's SIMDs compute for so many pages of units (rows that share their pages, which the caches then hold, are bound by it)
+double compute4_us(const bs_layer_cfg &g, int group, int heads, int64_t pages, int n_cu) {
+  return ((g.head_dim == 128 ? 0.27 : 0.16) + 0.055 * (g.head_dim / group)) * (heads == 2 ? 0.75 : 1.0) * (double)pages * g.n_kv_heads / (4.0 * n_cu);
+}
+constexpr double UNITS4_US = 3.36;  // of any division
+
+// The division over a cache in four bits, whose units read less and compute more: KV heads that share a wavefront too, where the columns of two have
 // room (see kv4_attn.hip).  A wavefront takes `step` microseconds a page; what its registers allow is on the chip at a time, in rounds; or the bytes
 // are longer.  Fitted to 4000 batches of 1 to 300 streams (up to 16000 tokens, equal and unequal, five head layouts, all groups) timed in every
 // division with 1, 2 and 4 wavefronts: 3.4 % off the best on average, 15 % for one in twenty, 34 % at worst; the division of the cache in bf16 is 29 % off.
@@ -249,10 +255,8 @@ Division divide4(const std::vector<bs_window::Rows> &rows, const bs_layer_cfg &g
         const double step = (0.272 + 0.043 * (dh / group)) * (dh == 128 ? 1.0 : 0.707) * (heads == 2 ? 1.34 : 1.0);
         const double units = (double)all * hkv / heads, slots = 4.0 * n_cu * kv4_resident(dh, group, heads) / waves;
         const double alone = 1.44 + step * longest_steps, mean = 2.91 + 1.18 * step * (double)steps / std::max<int64_t>(1, all);
-        // (rows that share their pages, which the caches then hold, are bound by what a SIMD computes)
-        const double compute = ((dh == 128 ? 0.27 : 0.16) + 0.055 * (dh / group)) * (heads == 2 ? 0.75 : 1.0) * (double)every * hkv / (4.0 * n_cu);
-        const double load = std::max(compute, mean * (units / slots + 0.31 * (std::ceil(units / slots) - units / slots)));
-        const double us = 3.36 + std::max({bytes_us + 0.087 * alone, alone, load}) + 0.54 * std::min(bytes_us, load) +
+        const double load = std::max(compute4_us(g, group, heads, every, n_cu), mean * (units / slots + 0.31 * (std::ceil(units / slots) - units / slots)));
+        const double us = UNITS4_US + std::max({bytes_us + 0.087 * alone, alone, load}) + 0.54 * std::min(bytes_us, load) +
                           (joined ? 0.75 + 0.22 * most + 0.0011 * (double)joined * hkv / heads : 0.0);
         if (!any || us < best.us) best = {waves, pages, us, heads};
         any = true;
@@ -449,6 +453,21 @@ int sort_rows(bs_window *w, const bs_batch *b, const Route &r, int most_narrow) 
   return BS_OK;
 }
 
+// Whether all rows as narrow work over a cache in four bits are expected to take `us` or more, whatever their division: what they compute alone.  (A segment
+// of more rows than a unit is among them, whose units leave no room for a second KV head.)
+bool narrow4_takes(const bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cfg &g, int n_cu, double us) {
+  int64_t pages = 0;
+  for (int s = 0; s < b->n_seq; ++s) {
+    const int rows = b->row_start[s + 1] - b->row_start[s];
+    for (int j = 0; j < rows; j += r.per_unit) {
+      const int p0 = b->kv_len[s] - rows + j;
+      pages += seen_by(p0, p0 + std::min(r.per_unit, rows - j) - 1, w->p.window, w->p.sinks).pages();
+    }
+    if (UNITS4_US + compute4_us(g, w->group, 1, pages, n_cu) >= us) return true;
+  }
+  return false;
+}
+
 int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cfg &g, int n_cu) {
   Planned &p = w->p;
   w->items.clear();
@@ -471,7 +490,9 @@ int plan_work(bs_window *w, const bs_batch *b, const Route &r, const bs_layer_cf
     const int rows = rows_of[k];
     if (rows < most ? (k == 2 && !next) : k != 0) continue;  // (the same as another)
     if (k && w->group && !kv4_has_rows(g.head_dim, w->group)) continue;
-    if (k == 0 && best >= 0.0) {  // many rows as narrow work: more pages than could be worth it
+    if (k == 0 && best >= 0.0 && w->group) {
+      if (narrow4_takes(w, b, r, g, n_cu, best)) continue;
+    } else if (k == 0 && best >= 0.0) {  // many rows as narrow work: more pages than could be worth it
       int64_t pages = 0;
       for (const bs_window::Work &x : w->work) pages += (int64_t)x.blocks * (r.rows / r.per_unit);
       if (pages * g.n_kv_heads * 0.1 > 2.0 * best * n_cu) continue;

@@ -293,3 +293,32 @@ def test_streams_take_weights_from_rows():
     st = Streams.__new__(Streams)
     st.layer = SimpleNamespace(w8_linear=lambda x, w: "eight", w4_linear=lambda x, w: "four")
     assert [st.linear(None, w) for w in (binding.W8Rows(q, s), binding.W8Weight(q, s), binding.W4Weight)] == ["eight", "eight", "four"]
+
+
+@pytest.mark.parametrize("hq,hkv,dh,group,seqs,window,units,blocks,waves,pages", [
+    (32, 8, 128, 128, [(700, 2200)] * 6, 1 << 20, 0, 132, 1, 15444), (32, 8, 128, 64, [(700, 2200)] * 6, 1 << 20, 0, 132, 1, 15444),
+    (32, 8, 128, 32, [(700, 2200)] * 6, 1 << 20, 1050, 0, 1, 121932), (32, 8, 128, 128, [(300, 2200)] * 3, 1 << 20, 225, 0, 1, 28941),
+    (32, 8, 128, 128, [(400, 2200)] * 4 + [(1, 2000)] * 40, 1 << 20, 40, 52, 4, 11600), (64, 8, 128, 128, [(500, 900)] * 5, 1 << 20, 0, 160, 1, 6640),
+    (32, 8, 64, 64, [(700, 2200)] * 6, 1 << 20, 0, 132, 1, 15444), (32, 8, 64, 32, [(900, 2200)] * 6, 500, 0, 174, 1, 6078),
+    (16, 16, 128, 64, [(1000, 3000)] * 4, 1 << 20, 0, 32, 1, 5148), (16, 16, 128, 64, [(200, 300)] * 4, 64, 52, 0, 2, 360),
+    (48, 8, 128, 128, [(2000, 2000), (5, 900)], 1 << 20, 0, 101, 1, 6407)])
+def test_which_kind_of_work_longer_segments_are(hq, hkv, dh, group, seqs, window, units, blocks, waves, pages):
+    # as both kinds and every division of either are expected to take; a plan may leave out what it knows to be longer
+    layer = binding.Layer(W.LayerShape(256, hq, hkv, dh, 256), device=-1)
+    d = layer.window_plan(make_batch(seqs), window, 4, cache=binding.Kv4(group)).division()
+    assert (d.units, d.wide_blocks, d.waves, d.pages) == (units, blocks, waves, pages)
+
+
+def test_plans_leave_out_what_is_longer():
+    # four segments of 4096 rows: as units of four rows each they name eight times the pages (without looking at these 1.2 ms a plan, with them 4.7; over the
+    # cache in bf16 2.7)
+    import time
+    layer, batch = binding.Layer(W.LLAMA3_8B, device=-1), make_batch([(4096, 12000)] * 4)
+    plans = [layer.window_plan(batch, 1 << 20, cache=c) for c in (binding.Kv4(128), None)]
+    times = [[], []]
+    for _ in range(8):
+        for plan, t in zip(plans, times):
+            start = time.perf_counter()
+            plan.update(batch, 1 << 20)
+            t.append(time.perf_counter() - start)
+    assert min(times[0]) < min(times[1])
