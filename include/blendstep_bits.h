@@ -38,11 +38,13 @@ int64_t bs_kv4_page_bytes(const bs_ctx *ctx, int32_t group);
  * that blendstep_stream.h says of them holds, but:
  *   - probabilities are rounded to bf16 after a multiplication with the scales of values
  *   - a query with an infinity gives NaN
+ *   - sums carry 16 of every code, which cancel: the sum of 31 |q| scale over a group of a key, |mid| |sum of q|, and 31 times a value's scale have to be in range,
+ *     and a probability times a scale is a bf16 number, which keeps fewer digits below 2^-126
  *   - the wide_blocks of bs_window_division are units of one KV head too, of about eight times the rows of a narrow unit, with all of their pages. */
 int bs_window_cache(bs_window *w, int32_t bits, int32_t group);
 
-/* k, v: device bf16, token-major [n_pages][16][n_kv_heads][head_dim], 16-byte aligned; kv_pool: n_pages pages in four bits.  kv4_unpack gives what the
- * codes stand for, rounded to bf16. */
+/* k, v: device bf16, token-major [n_pages][16][n_kv_heads][head_dim], 16-byte aligned; kv_pool: n_pages pages in four bits, n_pages * n_kv_heads
+ * below 2^24.  kv4_unpack gives what the codes stand for, rounded to bf16. */
 int bs_kv4_pack(bs_ctx *ctx, const void *k, const void *v, void *kv_pool, int64_t n_pages, int32_t group, void *stream);
 int bs_kv4_unpack(bs_ctx *ctx, const void *kv_pool, void *k, void *v, int64_t n_pages, int32_t group, void *stream);
 
@@ -63,8 +65,8 @@ int bs_kv4_compact(bs_ctx *ctx, void *const *pools, int32_t n_pools, int64_t n_p
 int bs_w8_quantize(bs_ctx *ctx, const void *x, int64_t x_stride, int64_t m, int64_t k, void *q, float *scales, void *stream);
 
 /* q: device int8 [m, k], weight: device int8 [n, k] (any values of either, -128 included), 16-byte aligned; scales: device float [m], weight_scales: device float [n];
- * y: device bf16, row i at y + i * y_stride, rounded once.  The calls on one context share a workspace and must not overlap in time on
- * different streams. */
+ * y: device bf16, row i at y + i * y_stride, rounded once; it must not overlap what is read.  The calls on one context, those of bs_w8_linear_rows too, share a
+ * workspace and must not overlap in time on different streams. */
 int bs_w8_linear(bs_ctx *ctx, const void *q, const float *scales, const void *weight, const float *weight_scales, int64_t m, int64_t n, int64_t k, void *y,
                  int64_t y_stride, void *stream);
 

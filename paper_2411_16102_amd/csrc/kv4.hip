@@ -204,7 +204,8 @@ hipError_t with_shape(int head_dim, int group, F &&f) {
 hipError_t launch_rope_append4(const RopeArgs &a, int group, hipStream_t stream) {
   if (a.n_items <= 0) return hipSuccess;
   // Shares of the query heads: workgroups for a few rounds of the chip, of at least four heads.  Of the KV heads: as many as a pass takes of a whole
-  // page's rows (of few rows it takes them all, but a workgroup that has several waits for one after the other where others have whole pages).
+  // page's rows (of few rows it takes them all, but a workgroup that has several waits for one after the other where others have whole pages).  A step of single tokens alone pays
+  // for it: of each of eight workgroups 16 threads code, 77 rows of 8 KV heads 7.9 us where the append of bf16 takes 5.2.
   const int shares = std::max(1, std::min(2048 / a.n_items, a.n_q_heads / 4)), kv_shares = std::max(1, a.n_kv_heads * a.head_dim / 128);
   const dim3 grid((unsigned)a.n_items * (unsigned)(shares + kv_shares)), block(ROPE_THREADS);
   return with_shape(a.head_dim, group, [&](auto dh, auto g) {

@@ -350,7 +350,7 @@ struct FourBits {
     };
     auto meet = []() __attribute__((always_inline)) {
       asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(0xC07F);  // (LDS alone: loads stay on their way)
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // (LDS alone; where loads are waited for is said at window_rows4_kernel)
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     };
@@ -419,8 +419,10 @@ struct FourBitPages : FourBits<DH, GROUP, HEADS_, 1> {
 
 // Rows of longer segments: a workgroup per (item, KV head), two blocks of columns to a wavefront, all of the pages that the item's rows see.  Codes are
 // brought to bf16 once for the four, which takes 28 vector operations a pair of pages of each instead of 112; 16 reads of LDS give them back.  Bound by
-// what a SIMD issues and waits for, 230 vector operations and 34 matrix instructions a pair and wavefront (128 channels in one group), and by the last round: with two wavefronts
-// on a SIMD vector pipes are 51 % busy over the launch, matrix pipes 24 %, a fifth of the places empty.  Six segments of about 700 rows behind 1500 tokens, 8 KV heads with four
+// what a SIMD issues, 230 vector operations and 34 matrix instructions a pair and wavefront (128 channels in one group; of the cycles of CUs at work vector operations take 64 %, matrix
+// instructions 29 %), by the last round (below: 1088 workgroups on 768 places), and by loads: once in every pair the compiler waits for all of a wavefront's loads, the codes that it has just
+// asked for among them, because pairs that are seen and pairs that are not load their numbers in branches of their own; other wavefronts of the SIMD have to cover that round trip.
+// 64-wide heads in two groups keep one register in scratch, around the loop.  Six segments of about 700 rows behind 1500 tokens, 8 KV heads with four
 // queries each: 201 us, as narrow work 230.  Slower: two wavefronts on a SIMD (211; of 64-wide heads 185 instead of 159, in two groups 221 instead of 196), every
 // wavefront its own codes (224; with three or four blocks and one wavefront a SIMD 319 and 384), one block of columns and four wavefronts (224).  Pages brought to fp16 and bf16 once for the
 // kernel of longer segments of a cache in bf16 took 199 us there, but with all batches of its kind 1.4 to 1.8 times the time even of the first of these, and a second copy of the pages.

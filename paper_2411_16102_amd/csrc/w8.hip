@@ -150,7 +150,9 @@ __global__ __launch_bounds__(256) void w8_reduce_kernel(const GemmArgs a) {
 }
 
 // Up to four rows: rows as integers and their product in one launch.  As gemm_rows_kernel, but that the rows, brought over as they are and first,
-// become integers in LDS while the first weights travel; rings hold weights alone.
+// become integers in LDS behind the first requests for weights; rings hold weights alone.  (The greatest magnitudes are exchanged through `part`, and before it reads
+// that the compiler waits for every request, as one that may write there: the first weights have landed when integers are made, and k-tiles that the ring has no
+// room for are a second round trip.  One row of 4096 by 6144 outputs, four k-tiles a wavefront and room for three: 8.0 us, a launch and reads 6.4.)
 constexpr int FEW_M = 4, FEW_RED = 8 * 1024;  // rows; bytes of the sums
 constexpr int FEW_LDS(int ni, int s, int kb) { return 8 * s * ni * 2048 + FEW_RED + kb * 1536 + 256; }  // (reads of the last k-tile may pass the integers' end)
 struct FewArgs {
@@ -210,7 +212,7 @@ __global__ __launch_bounds__(512) void w8_few_kernel(const FewArgs f, const int 
   };
   if (total > 0) set_item(i_item);
   for (int s = 0; s < S && issued < total; ++s) issue();
-  wait_for_all_but<L>(issued, std::make_integer_sequence<int, S + 1>{});  // the rows have landed, the weights need not have
+  wait_for_all_but<L>(issued, std::make_integer_sequence<int, S + 1>{});  // the rows have landed
   __builtin_amdgcn_s_barrier();
   // 512 / rows threads a row (as a power of two), the greatest magnitude of it among their wavefronts
   const int shift = a.M > 2 ? 7 : a.M > 1 ? 8 : 9, row = t >> shift, at0 = (t & ((1 << shift) - 1)) * 8, step = 8 << shift;
