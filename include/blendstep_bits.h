@@ -38,8 +38,8 @@ int64_t bs_kv4_page_bytes(const bs_ctx *ctx, int32_t group);
  * that blendstep_stream.h says of them holds, but:
  *   - probabilities are rounded to bf16 after a multiplication with the scales of values
  *   - a query with an infinity gives NaN
- *   - sums carry 16 of every code, which cancel: the sum of 31 |q| scale over a group of a key, |mid| |sum of q|, and 31 times a value's scale have to be in range,
- *     and a probability times a scale is a bf16 number, which keeps fewer digits below 2^-126
+ *   - sums carry 16 of every code, which cancel: 31 times the sum of |q| over a group, the same times a key's scale, |mid| times that sum, and 31 times a value's scale
+ *     have to be in range; and a probability times a scale is a bf16 number, which keeps fewer digits below 2^-126
  *   - the wide_blocks of bs_window_division are units of one KV head too, of about eight times the rows of a narrow unit, with all of their pages. */
 int bs_window_cache(bs_window *w, int32_t bits, int32_t group);
 
